@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "internal.h"
+#include "optim.h"
 #include "radix.h"
 
 namespace gs {
@@ -516,6 +517,42 @@ void *scratch_address(hipError_t *err) {
     return g_scratch_ptr[dev];
 }
 
+// Pieces and elements of a list of tensors; false if it is malformed.
+bool adamw_sizes(const gs_adamw_tensor *tensors, int64_t count, int64_t *items, int64_t *elements) {
+    if (count < 0 || count > ((int64_t)1 << 20) || (count > 0 && !tensors)) return false;
+    for (int64_t i = 0; i < count; ++i) {
+        if (tensors[i].n < 0 || tensors[i].n >= ((int64_t)1 << 40)) return false;
+        *items += optim_items(tensors[i].n);
+        *elements += tensors[i].n;
+        if (*items >= ((int64_t)1 << 31)) return false;
+    }
+    return true;
+}
+
+struct AdamwPlanLayout {
+    OptimItem *items;
+    double *part;
+    size_t bytes;
+};
+AdamwPlanLayout adamw_plan_layout(void *work, int64_t items) {
+    Carver c(work);
+    AdamwPlanLayout l;
+    l.part = c.take<double>(optim_part_bytes() / sizeof(double));
+    l.items = c.take<OptimItem>((size_t)items);
+    l.bytes = c.off;
+    return l;
+}
+
+gs_status check_adamw(const char *who, const gs_adamw_plan *plan, const gs_adamw_params *params) {
+    if (!plan || !params) return fail(GS_ERR_INVALID_ARGUMENT, "%s: plan or settings are null", who);
+    if (plan->n_items < 0 || !plan->work || !aligned(plan->work) ||
+        plan->work_bytes < adamw_plan_layout(nullptr, plan->n_items).bytes)
+        return fail(GS_ERR_INVALID_ARGUMENT, "%s: the plan was not made by gs_plan_adamw", who);
+    if (!(params->beta1 >= 0.0 && params->beta1 < 1.0 && params->beta2 >= 0.0 && params->beta2 < 1.0))
+        return fail(GS_ERR_INVALID_ARGUMENT, "%s: beta1 and beta2 must lie in [0, 1)", who);
+    return GS_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1014,6 +1051,126 @@ gs_status gs_densify(const gs_params *in, int64_t n_in, const float *weight, con
     if (*n_out > capacity)
         return fail(GS_ERR_CAPACITY, "gs_densify: %lld kept Gaussians exceed the capacity %lld", (long long)*n_out,
                     (long long)capacity);
+    return GS_OK;
+}
+
+size_t gs_adamw_plan_bytes(const gs_adamw_tensor *tensors, int64_t count) {
+    int64_t items = 0, elements = 0;
+    if (!adamw_sizes(tensors, count, &items, &elements)) return (size_t)-1;
+    return adamw_plan_layout(nullptr, items).bytes;
+}
+
+gs_status gs_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, gs_adamw_plan *plan, hipStream_t stream) {
+    if (!plan) return fail(GS_ERR_INVALID_ARGUMENT, "gs_plan_adamw: plan is null");
+    plan->n_items = -1;
+    int64_t items = 0, elements = 0;
+    if (!adamw_sizes(tensors, count, &items, &elements))
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_plan_adamw: null list, or a count or size out of range");
+    bool updatable = true;
+    for (int64_t i = 0; i < count; ++i) {
+        const gs_adamw_tensor &t = tensors[i];
+        const bool pb = t.param_type == GS_TYPE_BF16, gb = t.grad_type == GS_TYPE_BF16;
+        const bool m8 = t.moments == GS_MOMENTS_MXFP8;
+        const auto bad = [&](const char *why) {
+            return fail(GS_ERR_INVALID_ARGUMENT, "gs_plan_adamw: tensor %lld: %s", (long long)i, why);
+        };
+        if ((!pb && t.param_type != GS_TYPE_F32) || (!gb && t.grad_type != GS_TYPE_F32) || (pb && !gb))
+            return bad("parameters are float32 with float32 or bfloat16 gradients, or bfloat16 with bfloat16");
+        if (!m8 && t.moments != GS_MOMENTS_F32) return bad("moments are float32 or MXFP8");
+        if (!(std::isfinite(t.lr) && t.lr >= 0.0f && std::isfinite(t.weight_decay) && t.weight_decay >= 0.0f))
+            return bad("lr and weight_decay must be finite and >= 0");
+        if (t.n == 0) continue;
+        if (!t.grad || (uintptr_t)t.grad % (gb ? 2 : 4)) return bad("grad is null or not aligned to its type");
+        if (!t.param) {
+            updatable = false;
+            continue;
+        }
+        if ((uintptr_t)t.param % (pb ? 2 : 4)) return bad("param is not aligned to its type");
+        if (!t.m || !t.v || (!m8 && (((uintptr_t)t.m | (uintptr_t)t.v) % 4)))
+            return bad("moments are null or not aligned to their type");
+        if (m8 && (!t.m_scale || !t.v_scale)) return bad("the scales of MXFP8 moments are null");
+    }
+    const AdamwPlanLayout l = adamw_plan_layout(plan->work, items);
+    if (!plan->work || plan->work_bytes < l.bytes || !aligned(plan->work))
+        return fail(GS_ERR_WORKSPACE, "gs_plan_adamw: plan needs %zu bytes, 256-byte aligned (got %zu)", l.bytes,
+                    plan->work_bytes);
+    GS_TRY(launch_plan_adamw(tensors, count, l.items, stream), "gs_plan_adamw");
+    plan->n_items = items;
+    plan->n_elements = elements;
+    plan->count = (int32_t)count;
+    plan->updatable = updatable;
+    return GS_OK;
+}
+
+gs_status gs_grad_norm(const gs_adamw_plan *plan, const gs_adamw_params *params, gs_adamw_control *control,
+                       hipStream_t stream) {
+    gs_status st = check_adamw("gs_grad_norm", plan, params);
+    if (st != GS_OK) return st;
+    if (!(params->max_norm > 0.0)) return fail(GS_ERR_INVALID_ARGUMENT, "gs_grad_norm: max_norm must be > 0");
+    if (!control || (uintptr_t)control % 8)
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_grad_norm: control is null or not 8-byte aligned");
+    const AdamwPlanLayout l = adamw_plan_layout(plan->work, plan->n_items);
+    GS_TRY(launch_grad_norm(l.items, plan->n_items, l.part,
+                            NormArgs{params->beta1, params->beta2, params->max_norm}, control, stream),
+           "gs_grad_norm");
+    return GS_OK;
+}
+
+gs_status gs_adamw(const gs_adamw_plan *plan, const gs_adamw_params *params, int64_t step,
+                   const gs_adamw_control *control, hipStream_t stream) {
+    gs_status st = check_adamw("gs_adamw", plan, params);
+    if (st != GS_OK) return st;
+    if (!plan->updatable) return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw: a tensor of the plan has no parameter");
+    if (!(std::isfinite(params->eps) && params->eps >= 0.0 && std::isfinite(params->lr_scale) &&
+          params->lr_scale >= 0.0))
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw: eps and lr_scale must be finite and >= 0");
+    if (control ? (uintptr_t)control % 8 != 0 : step < 1)
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw: without a control step must be >= 1 (a control is 8-byte "
+                                             "aligned)");
+    StepArgs a;
+    a.b1 = (float)params->beta1;
+    a.a1 = (float)(1.0 - params->beta1);
+    a.b2 = (float)params->beta2;
+    a.a2 = (float)(1.0 - params->beta2);
+    a.eps = (float)params->eps;
+    a.lr_scale = (float)params->lr_scale;
+    a.first = a.second = 1.0f;
+    a.step = (uint64_t)step;
+    a.seed = params->seed;
+    if (!control) {
+        a.first = (float)(1.0 / (1.0 - std::pow(params->beta1, (double)step)));
+        a.second = (float)(1.0 / std::sqrt(1.0 - std::pow(params->beta2, (double)step)));
+    }
+    const AdamwPlanLayout l = adamw_plan_layout(plan->work, plan->n_items);
+    GS_TRY(launch_adamw(l.items, plan->n_items, a, control, stream), "gs_adamw");
+    return GS_OK;
+}
+
+gs_status gs_adamw_carry(const gs_adamw_rows *arrays, int32_t count, int64_t n_in, const int32_t *source,
+                         int64_t n_out, hipStream_t stream) {
+    if (count < 0 || count > GS_ADAMW_ROWS_MAX || (count > 0 && !arrays))
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw_carry: null arrays, or a count outside [0, %d]",
+                    GS_ADAMW_ROWS_MAX);
+    if (n_in < 0 || n_in >= ((int64_t)1 << 31) || n_out < 0 || n_out >= ((int64_t)1 << 31))
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw_carry: counts out of range");
+    for (int32_t k = 0; k < count; ++k) {
+        const gs_adamw_rows &a = arrays[k];
+        if (a.width < 1 || a.width > 64)
+            return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw_carry: array %d: width must lie in [1, 64]", k);
+        const bool m8 = a.moments == GS_MOMENTS_MXFP8;
+        if (!m8 && a.moments != GS_MOMENTS_F32)
+            return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw_carry: array %d: moments are float32 or MXFP8", k);
+        if (n_out == 0) continue;
+        if (!a.m_out || !a.v_out || (m8 && (!a.m_scale_out || !a.v_scale_out)) ||
+            (n_in > 0 && (!a.m || !a.v || (m8 && (!a.m_scale || !a.v_scale)))))
+            return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw_carry: array %d: null array", k);
+        if (!m8 && (((uintptr_t)a.m | (uintptr_t)a.v | (uintptr_t)a.m_out | (uintptr_t)a.v_out) % 4))
+            return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw_carry: array %d: not aligned to its type", k);
+    }
+    if (n_out == 0 || count == 0) return GS_OK;
+    if (!source || (uintptr_t)source % 4)
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw_carry: source is null or not aligned to its type");
+    GS_TRY(launch_adamw_carry(arrays, count, n_in, source, n_out, stream), "gs_adamw_carry");
     return GS_OK;
 }
 

@@ -1,0 +1,77 @@
+// Internal declarations of the optimiser step (optim.hip, api.cpp): the
+// pieces of a list of tensors, and the launchers' arguments.
+#pragma once
+
+#include "../../include/gs_optim.h"
+#include "internal.h"
+
+namespace gs {
+
+constexpr int64_t kOptimChunk = 1024;  // elements of an item at most: a multiple of 32 that divides 2^32
+constexpr int64_t kCarryChunk = 1024;  // output elements of a workgroup of the carry
+
+// Flags of a tensor and its items.
+constexpr uint32_t kParamBf16 = 1, kGradBf16 = 2, kMoments8 = 4;
+constexpr uint32_t kVectors = 8;  // every array allows loads of four elements
+
+struct OptimTensor {
+    void *p;
+    const void *g;
+    void *m, *v;
+    uint8_t *ms, *vs;
+    int64_t n;
+    uint32_t place, flags;
+    float lr, wd;
+};
+
+// A piece of a tensor: its arrays from the piece's first element on.
+struct alignas(16) OptimItem {
+    void *p;
+    const void *g;
+    void *m, *v;
+    uint8_t *ms, *vs;
+    int64_t base;     // index of the first element in its tensor
+    int32_t count;
+    uint32_t place;   // of the tensor in the list
+    float lr, wd;
+    uint32_t flags, pad;
+};
+
+struct StepArgs {
+    float b1, a1, b2, a2, eps, lr_scale, first, second;
+    uint64_t step, seed;
+};
+struct NormArgs {
+    double beta1, beta2, max_norm;
+};
+struct CarryArgs {
+    gs_adamw_rows rows[GS_ADAMW_ROWS_MAX];
+    uint32_t first[GS_ADAMW_ROWS_MAX + 1];  // first workgroup of each array
+    uint32_t block0;                        // the launch's first workgroup
+    int64_t n_in, n_out;
+};
+
+inline int64_t optim_items(int64_t n) { return (n + kOptimChunk - 1) / kOptimChunk; }
+inline uint32_t optim_flags(const gs_adamw_tensor &t) {
+    uint32_t f = 0;
+    const bool pb = t.param_type == GS_TYPE_BF16, gb = t.grad_type == GS_TYPE_BF16;
+    const bool m8 = t.moments == GS_MOMENTS_MXFP8;
+    if (pb) f |= kParamBf16;
+    if (gb) f |= kGradBf16;
+    if (m8) f |= kMoments8;
+    const uintptr_t pm = pb ? 7 : 15, gm = gb ? 7 : 15, mm = m8 ? 3 : 15;
+    if (!((uintptr_t)t.param & pm) && !((uintptr_t)t.grad & gm) && !(((uintptr_t)t.m | (uintptr_t)t.v) & mm))
+        f |= kVectors;
+    return f;
+}
+
+size_t optim_part_bytes();
+hipError_t launch_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, OptimItem *items, hipStream_t s);
+hipError_t launch_grad_norm(const OptimItem *items, int64_t n_items, double *part, const NormArgs &a,
+                            gs_adamw_control *control, hipStream_t s);
+hipError_t launch_adamw(const OptimItem *items, int64_t n_items, const StepArgs &a, const gs_adamw_control *control,
+                        hipStream_t s);
+hipError_t launch_adamw_carry(const gs_adamw_rows *arrays, int count, int64_t n_in, const int32_t *source,
+                              int64_t n_out, hipStream_t s);
+
+}  // namespace gs

@@ -1,4 +1,5 @@
-"""Python binding of the C-ABI in include/gs.h and include/gs_train.h (ctypes).
+"""Python binding of the C-ABI in include/gs.h, include/gs_train.h and
+include/gs_optim.h (ctypes).
 
 Argument marshalling only: every step of sampling runs in the HIP library
 libgsq.so. torch provides device memory and the stream. Importing this module
@@ -34,7 +35,15 @@ EXPORTED = ("gs_query_size", "gs_index_work_bytes", "gs_build_index", "gs_plan_b
             "gs_profile_select", "gs_profile_reset", "gs_profile_read", "gs_activate", "gs_activate_backward",
             "gs_loss_work_bytes", "gs_loss", "gs_densify_work_bytes", "gs_densify",
             "gs_sample_gaussian_major_work_bytes", "gs_sample_gaussian_major", "gs_backward_pair_count",
-            "gs_sample_pair_counts", "gs_sample_backward_noalloc", "gs_plan_queries", "gs_sample_planned")
+            "gs_sample_pair_counts", "gs_sample_backward_noalloc", "gs_plan_queries", "gs_sample_planned", "gs_adamw_plan_bytes",
+            "gs_plan_adamw", "gs_grad_norm", "gs_adamw", "gs_adamw_carry")
+
+GS_TYPE_F32 = 0
+GS_TYPE_BF16 = 1
+GS_MOMENTS_F32 = 0
+GS_MOMENTS_MXFP8 = 1
+GS_ADAMW_ROWS_MAX = 16
+MOMENT_BLOCK = 32  # elements that share a scale of MXFP8 moments
 
 
 class GsLibraryMissing(RuntimeError):
@@ -82,6 +91,31 @@ class GsDensifyParams(ctypes.Structure):
                 ("new_weight_logit", ctypes.c_float), ("max_new", ctypes.c_int64)]
 
 
+class GsAdamwTensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("param_type", ctypes.c_int32), ("grad_type", ctypes.c_int32),
+                ("moments", ctypes.c_int32), ("lr", ctypes.c_float), ("weight_decay", ctypes.c_float)]
+
+
+class GsAdamwPlan(ctypes.Structure):
+    _fields_ = [("work", ctypes.c_void_p), ("work_bytes", ctypes.c_size_t), ("n_items", ctypes.c_int64),
+                ("n_elements", ctypes.c_int64), ("count", ctypes.c_int32), ("updatable", ctypes.c_int32)]
+
+
+class GsAdamwParams(ctypes.Structure):
+    _fields_ = [("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("lr_scale", ctypes.c_double), ("max_norm", ctypes.c_double), ("seed", ctypes.c_uint64)]
+
+
+class GsAdamwRows(ctypes.Structure):
+    _fields_ = [("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("m_out", ctypes.c_void_p), ("v_out", ctypes.c_void_p),
+                ("m_scale_out", ctypes.c_void_p), ("v_scale_out", ctypes.c_void_p), ("width", ctypes.c_int32),
+                ("moments", ctypes.c_int32)]
+
+
+ADAM_CONTROL_BYTES = 64  # gs_adamw_control: two int64, four float32, eight uint32
 LOSS_TERMS_BYTES = 64  # gs_loss_terms: four float64 values, then four int64 counts
 
 _LIB = None
@@ -153,6 +187,16 @@ def load_library():
     L.gs_densify.restype = ctypes.c_int
     L.gs_densify.argtypes = [P(GsParams), i64, vp, P(GsGrid), P(GsQuery), vp, vp, vp, vp, P(GsDensifyParams),
                              P(GsParams), i64, vp, P(i64), vp, sz, vp]
+    L.gs_adamw_plan_bytes.restype = sz
+    L.gs_adamw_plan_bytes.argtypes = [P(GsAdamwTensor), i64]
+    L.gs_plan_adamw.restype = ctypes.c_int
+    L.gs_plan_adamw.argtypes = [P(GsAdamwTensor), i64, P(GsAdamwPlan), vp]
+    L.gs_grad_norm.restype = ctypes.c_int
+    L.gs_grad_norm.argtypes = [P(GsAdamwPlan), P(GsAdamwParams), vp, vp]
+    L.gs_adamw.restype = ctypes.c_int
+    L.gs_adamw.argtypes = [P(GsAdamwPlan), P(GsAdamwParams), i64, vp, vp]
+    L.gs_adamw_carry.restype = ctypes.c_int
+    L.gs_adamw_carry.argtypes = [P(GsAdamwRows), ctypes.c_int32, i64, vp, i64, vp]
     _LIB = L
     return L
 
@@ -668,6 +712,195 @@ def gs_densify(params_in: ParamSet, n_in: int, weight: torch.Tensor, domain: GsG
         raise GsError(st, load_library().gs_last_error().decode(errors="replace") + f" (kept {n_out.value})")
     _check(st)
     return int(n_out.value)
+
+
+def moment_scales(n: int) -> int:
+    """Scales of MXFP8 moments of n elements."""
+    return (int(n) + MOMENT_BLOCK - 1) // MOMENT_BLOCK
+
+
+@dataclass
+class AdamTensor:
+    """A tensor of an optimiser's list (include/gs_optim.h): param and grad
+    float32 or bfloat16 (param None: it only counts for the norm), moments m
+    and v float32, or uint8 with scales m_scale and v_scale (MXFP8; v then
+    holds sqrt(v)). All contiguous, on one device."""
+    param: Optional[torch.Tensor]
+    grad: torch.Tensor
+    m: Optional[torch.Tensor] = None
+    v: Optional[torch.Tensor] = None
+    m_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+    lr: float = 1e-3
+    weight_decay: float = 0.0
+
+    @staticmethod
+    def new(param: torch.Tensor, grad: torch.Tensor, lr: float, weight_decay: float = 0.0,
+            moments: int = GS_MOMENTS_F32) -> "AdamTensor":
+        """A tensor with moments of its own, as before the first step."""
+        n, dev = param.numel(), param.device
+        if moments == GS_MOMENTS_F32:
+            return AdamTensor(param, grad, torch.zeros(n, dtype=torch.float32, device=dev),
+                              torch.zeros(n, dtype=torch.float32, device=dev), lr=lr, weight_decay=weight_decay)
+        if moments != GS_MOMENTS_MXFP8:
+            raise ValueError("moments must be GS_MOMENTS_F32 or GS_MOMENTS_MXFP8")
+        z = lambda k: torch.zeros(k, dtype=torch.uint8, device=dev)  # noqa: E731
+        return AdamTensor(param, grad, z(n), z(n), z(moment_scales(n)), z(moment_scales(n)), lr, weight_decay)
+
+    def c(self) -> GsAdamwTensor:
+        types = {torch.float32: GS_TYPE_F32, torch.bfloat16: GS_TYPE_BF16}
+        n = self.grad.numel()
+        for t, nm in ((self.param, "param"), (self.grad, "grad")):
+            if t is not None and (not t.is_cuda or not t.is_contiguous() or t.dtype not in types or t.numel() != n):
+                raise ValueError(f"{nm} must be a contiguous float32 or bfloat16 device tensor of the gradient's size")
+        moments = GS_MOMENTS_F32
+        if self.param is not None:
+            moments = _moments_of(self.m, self.v, self.m_scale, self.v_scale, n, "")
+        return GsAdamwTensor(_ptr(self.param), self.grad.data_ptr(), _ptr(self.m), _ptr(self.v), _ptr(self.m_scale),
+                             _ptr(self.v_scale), n, types[self.grad.dtype if self.param is None else self.param.dtype],
+                             types[self.grad.dtype], moments, float(self.lr), float(self.weight_decay))
+
+
+def _moments_of(m, v, m_scale, v_scale, n: int, label: str) -> int:
+    """Checks the moments of n elements and returns their form."""
+    if m is None or v is None or m.dtype != v.dtype or m.dtype not in (torch.float32, torch.uint8):
+        raise ValueError(f"m{label} and v{label} must both be float32 or both uint8")
+    for t, nm in ((m, "m"), (v, "v")):
+        if not t.is_cuda or not t.is_contiguous() or t.numel() < n:
+            raise ValueError(f"{nm}{label} must be a contiguous device tensor of {n} elements")
+    if m.dtype == torch.float32:
+        return GS_MOMENTS_F32
+    for t, nm in ((m_scale, "m_scale"), (v_scale, "v_scale")):
+        if t is None or not t.is_cuda or t.dtype != torch.uint8 or not t.is_contiguous() or \
+                t.numel() < moment_scales(n):
+            raise ValueError(f"{nm}{label} must be a contiguous uint8 device tensor of {moment_scales(n)} elements")
+    return GS_MOMENTS_MXFP8
+
+
+def moment_values(m: torch.Tensor, m_scale: torch.Tensor) -> torch.Tensor:
+    """The numbers that MXFP8 moments stand for, in float32 (of v: sqrt(v))."""
+    n = m.numel()
+    two = ((m_scale.to(torch.int32) << 23).clamp_min(0x400000)).view(torch.float32)
+    return m.view(torch.float8_e4m3fn).float().view(-1) * two.repeat_interleave(MOMENT_BLOCK)[:n]
+
+
+class AdamPlan:
+    """A list of tensors laid out on the device for gs_grad_norm and
+    gs_adamw. It holds the tensors' addresses, learning rates and decays:
+    make a new one when these change."""
+
+    def __init__(self, tensors: Sequence[AdamTensor], device=None, stream=None):
+        L = load_library()
+        self.tensors = list(tensors)
+        rows = (GsAdamwTensor * max(len(self.tensors), 1))(*[t.c() for t in self.tensors])
+        if device is None:
+            device = self.tensors[0].grad.device if self.tensors else torch.device("cuda")
+        for t in self.tensors:
+            if t.grad.device != self.tensors[0].grad.device:
+                raise ValueError("all tensors of a list must be on one device")
+        need = L.gs_adamw_plan_bytes(rows, len(self.tensors))
+        if need == ctypes.c_size_t(-1).value:
+            raise GsError(GS_ERR_INVALID_ARGUMENT, "malformed list of tensors")
+        self.work = _alloc_bytes(need, device)
+        self.c = GsAdamwPlan(self.work.data_ptr(), int(self.work.numel()), -1, 0, 0, 0)
+        _check(L.gs_plan_adamw(rows, len(self.tensors), ctypes.byref(self.c), _stream(stream)))
+
+
+def alloc_adam_control(device) -> torch.Tensor:
+    """The device-side state of a training run's steps, as before the first."""
+    return torch.zeros(ADAM_CONTROL_BYTES, dtype=torch.uint8, device=device)
+
+
+def adam_control_views(control: torch.Tensor) -> dict:
+    """Views of a control's fields: step, skipped (int64), norm, clip
+    (float32), apply (int32), as the last gs_grad_norm left them."""
+    return {"step": control[0:8].view(torch.int64)[0], "skipped": control[8:16].view(torch.int64)[0],
+            "norm": control[16:20].view(torch.float32)[0], "clip": control[20:24].view(torch.float32)[0],
+            "apply": control[32:36].view(torch.int32)[0]}
+
+
+def read_adam_control(control: torch.Tensor) -> dict:
+    """The fields of a control (copies to the host)."""
+    return {k: v.item() for k, v in adam_control_views(control.cpu()).items()}
+
+
+def _control_ptr(control: torch.Tensor) -> int:
+    if not control.is_cuda or control.numel() * control.element_size() < ADAM_CONTROL_BYTES or \
+            control.data_ptr() % 8:
+        raise ValueError("control must be a device buffer of at least 64 bytes, 8-byte aligned")
+    return control.data_ptr()
+
+
+def gs_grad_norm(plan: AdamPlan, control: torch.Tensor, max_norm: float = float("inf"), beta1: float = 0.9,
+                 beta2: float = 0.999, stream=None) -> None:
+    """The global gradient norm of a list, which opens a step of the control:
+    clip factor, step count and bias corrections, or a skipped step when the
+    norm is not finite."""
+    p = GsAdamwParams(beta1, beta2, 0.0, 1.0, max_norm, 0)
+    _check(load_library().gs_grad_norm(ctypes.byref(plan.c), ctypes.byref(p), _control_ptr(control),
+                                       _stream(stream)))
+
+
+def gs_adamw(plan: AdamPlan, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, lr_scale: float = 1.0,
+             step: Optional[int] = None, control: Optional[torch.Tensor] = None, seed: int = 0, stream=None) -> None:
+    """One AdamW step of all tensors of a list: step number `step` (1, 2,
+    ...), or the step that gs_grad_norm opened in `control`."""
+    if (step is None) == (control is None):
+        raise ValueError("give either step or control")
+    p = GsAdamwParams(beta1, beta2, eps, lr_scale, 1.0, seed)
+    _check(load_library().gs_adamw(ctypes.byref(plan.c), ctypes.byref(p), 0 if step is None else step,
+                                   None if control is None else _control_ptr(control), _stream(stream)))
+
+
+@dataclass
+class AdamRows:
+    """The moments of an array of per-Gaussian parameters before and after a
+    densification: rows of `width` elements, float32, or uint8 with scales
+    (MXFP8)."""
+    width: int
+    m: torch.Tensor
+    v: torch.Tensor
+    m_out: torch.Tensor
+    v_out: torch.Tensor
+    m_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
+    m_scale_out: Optional[torch.Tensor] = None
+    v_scale_out: Optional[torch.Tensor] = None
+
+
+class AdamCarry:
+    """Arrays for gs_adamw_carry, checked once. in_rows and out_rows are the
+    rows that every input and output array has room for."""
+
+    def __init__(self, arrays: Sequence[AdamRows]):
+        self.arrays = list(arrays)
+        if len(self.arrays) > GS_ADAMW_ROWS_MAX:
+            raise ValueError(f"at most {GS_ADAMW_ROWS_MAX} arrays")
+        rows = []
+        self.in_rows = self.out_rows = (1 << 31) - 1
+        for a in self.arrays:
+            w = int(a.width)
+            if not 1 <= w <= 64:
+                raise ValueError("width must lie in [1, 64]")
+            n_in, n_out = a.m.numel() // w, a.m_out.numel() // w
+            form = _moments_of(a.m, a.v, a.m_scale, a.v_scale, n_in * w, "")
+            if _moments_of(a.m_out, a.v_out, a.m_scale_out, a.v_scale_out, n_out * w, "_out") != form:
+                raise ValueError("input and output moments must have the same form")
+            self.in_rows, self.out_rows = min(self.in_rows, n_in), min(self.out_rows, n_out)
+            rows.append(GsAdamwRows(_ptr(a.m), _ptr(a.v), _ptr(a.m_scale), _ptr(a.v_scale), _ptr(a.m_out),
+                                    _ptr(a.v_out), _ptr(a.m_scale_out), _ptr(a.v_scale_out), w, form))
+        self.c = (GsAdamwRows * max(len(rows), 1))(*rows)
+
+
+def gs_adamw_carry(carry: AdamCarry, n_in: int, source: torch.Tensor, n_out: int, stream=None) -> None:
+    """Moments through gs_densify's source map: output row j is input row
+    source[j], or 0 for a new Gaussian."""
+    if n_in > carry.in_rows or n_out > carry.out_rows:
+        raise ValueError("the arrays hold fewer rows")
+    if not source.is_cuda or source.dtype != torch.int32 or not source.is_contiguous() or source.numel() < n_out:
+        raise ValueError("source must be a contiguous int32 device tensor with a slot per output row")
+    _check(load_library().gs_adamw_carry(carry.c, len(carry.arrays), n_in, source.data_ptr(), n_out,
+                                         _stream(stream)))
 
 
 def backward_pair_count(index: Index, query: Query, plan: Optional[torch.Tensor], work: torch.Tensor,

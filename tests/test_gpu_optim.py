@@ -1,0 +1,570 @@
+"""The optimiser step on the device (include/gs_optim.h) against the float64
+oracle of tests/optim_oracle.py: every type of parameter and gradient, both
+forms of the moments, sizes around blocks of 32 and pieces of 1024, lists,
+alignments, values at the ends of the ranges, the control with skipped steps
+and captured graphs, and moments through a densification.
+
+Tolerances are the oracle's: the size of each term times the unit roundoff
+of float32 and the number of operations behind it."""
+import math
+
+import numpy as np
+import pytest
+
+import optim_oracle as oo
+from harness import log
+
+pytestmark = pytest.mark.gpu
+
+B1, B2, EPS = 0.9, 0.999, 1e-8
+TYPES = [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16")]
+FORMS = ["f32", "mxfp8"]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2607_01164_amd as gs
+    gs.load_library()
+
+
+def dtype(name):
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16}[name]
+
+
+def host(t):
+    import torch
+    t = t.detach().reshape(-1)
+    return (t.double() if t.dtype in (torch.bfloat16, torch.float32) else t).cpu().numpy()
+
+
+def make(n, types, form, seed, lr=0.01, wd=0.1, offset=0, spread=3.0):
+    """A tensor with gradients and moments over a wide range: blocks of their
+    own sizes, zeros among them. offset: elements by which every array is off
+    its allocation's start."""
+    import torch
+    import paper_2607_01164_amd as gs
+    r = np.random.default_rng(seed)
+    size = np.exp(np.repeat(r.normal(size=(n + 31) // 32) * spread - 4, 32)[:n])
+    g = size * r.normal(size=n) * (r.random(n) > 0.1)
+    m = size * r.normal(size=n) * 0.3 * (r.random(n) > 0.1)
+    s = size * np.exp(r.normal(size=n)) * (r.random(n) > 0.05)
+
+    def dev(a, dt):
+        t = torch.empty(n + offset, dtype=dt, device="cuda")[offset:]
+        t.copy_(torch.from_numpy(np.ascontiguousarray(a)).to(dt))
+        return t
+
+    p = dev(r.normal(size=n).astype(np.float32), dtype(types[0]))
+    g = dev(g.astype(np.float32), dtype(types[1]))
+    if form == "f32":
+        return gs.AdamTensor(p, g, dev(m.astype(np.float32), torch.float32), dev((s * s).astype(np.float32), torch.float32),
+                             lr=lr, weight_decay=wd)
+    k = gs.moment_scales(n)
+    codes = lambda x, e: oo.magnitude_code(  # noqa: E731
+        np.abs(oo.e4m3(torch.from_numpy((np.abs(x) * np.exp2(-np.repeat(e, 32)[:n])).astype(np.float32))
+                       .to(torch.float8_e4m3fn).view(torch.uint8).numpy())))
+    em, es = (oo.exponents(oo.blocks(np.abs(x)).max(1)).astype(np.float64) for x in (m, s))
+    qm = codes(m, em).astype(np.uint8) | ((m < 0) * 128).astype(np.uint8)
+    qs = codes(s, es).astype(np.uint8)
+    # torch.empty(n + offset) of bytes: the codes are off their allocation too
+    return gs.AdamTensor(p, g, dev(qm, torch.uint8), dev(qs, torch.uint8), dev_bytes(em + 127, k), dev_bytes(es + 127, k),
+                         lr=lr, weight_decay=wd)
+
+
+def dev_bytes(a, k):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a[:k].astype(np.uint8))).cuda()
+
+
+def snapshot(t):
+    out = {"p": host(t.param), "g": host(t.grad), "m": host(t.m), "v": host(t.v)}
+    if t.m_scale is not None:
+        out["m"], out["v"] = oo.values(out["m"], host(t.m_scale)), oo.values(out["v"], host(t.v_scale)) ** 2
+    return out
+
+
+def check(t, before, place, step, seed=0, clip=1.0, lr_scale=1.0, beta1=B1, beta2=B2, eps=EPS, first=0, sharp=True, label=""):
+    """The tensor after a step against the oracle's step from `before`.
+    first: the index of the first element looked at."""
+    import torch
+    p, m, v, s, dp, dm, ds = oo.step(before["p"], before["g"], before["m"], before["v"], lr=t.lr, wd=t.weight_decay,
+                                     beta1=beta1, beta2=beta2, eps=eps, t=step, clip=clip, lr_scale=lr_scale)
+    if clip != 1.0:  # the factor itself is rounded
+        dm, ds = dm + oo.U * np.abs(before["g"]) * clip, ds * 1.5 + 2 * oo.U * s
+        dp = dp * 1.5
+    bits = oo.random_bits(first + np.arange(len(p)), place, step, seed)
+    got = host(t.param)
+    if t.param.dtype == torch.bfloat16:
+        r = ((bits * np.uint64(0x9E3779B1)) & np.uint64(oo.M32)) >> np.uint64(16)
+        oo.check_bf16(got, p, dp, r.astype(np.float64), label + " param")
+    else:
+        bad = ~((np.abs(got - p) <= dp) | (np.isnan(p) & np.isnan(got)) | (got == p))
+        assert not bad.any(), f"{label} param: {bad.sum()} off, {got[bad][:3]} for {p[bad][:3]} within {dp[bad][:3]}"
+    if t.m_scale is None:
+        for nm, x, y, d in (("m", host(t.m), m, dm), ("v", host(t.v), v, 7 * oo.U * v * (2 if clip != 1.0 else 1) + 3 * oo.TINY)):
+            bad = ~((np.abs(x - y) <= d) | (np.isnan(x) & np.isnan(y)) | (x == y) | (np.isinf(x) & (y > 3.4e38)))
+            assert not bad.any(), f"{label} {nm}: {bad.sum()} off, {x[bad][:3]} for {y[bad][:3]}"
+    else:
+        um = ((bits & np.uint64(0xFFFF)).astype(np.float64) + 0.5) / 65536
+        us = ((bits >> np.uint64(16)).astype(np.float64) + 0.5) / 65536
+        oo.check_mxfp8(host(t.m), host(t.m_scale), m, dm, um, sharp=sharp, label=label + " m")
+        oo.check_mxfp8(host(t.v), host(t.v_scale), s, ds, us, positive=True, sharp=sharp,
+                       label=label + " s")
+
+
+def run(tensors, step, **k):
+    import torch
+    import paper_2607_01164_amd as gs
+    plan = gs.AdamPlan(tensors)
+    gs.gs_adamw(plan, beta1=B1, beta2=B2, eps=EPS, step=step, **k)
+    torch.cuda.synchronize()
+    return plan
+
+
+SIZES = [1, 3, 4, 31, 32, 33, 63, 1000, 1023, 1024, 1025, 4097, 16387, 300007]
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("types", TYPES, ids=["-".join(t) for t in TYPES])
+@pytest.mark.parametrize("n", SIZES)
+def test_step_follows_the_definition(n, types, form):
+    """Three steps, each from the state that the kernel's last one left."""
+    t = make(n, types, form, seed=n)
+    for k in (1, 2, 1000):
+        before = snapshot(t)
+        run([t], k, seed=77)
+        check(t, before, 0, k, seed=77, label=f"{n} {types} {form} step {k}")
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("types", TYPES, ids=["-".join(t) for t in TYPES])
+@pytest.mark.parametrize("offset", [1, 2, 3, 5])
+def test_alignment_does_not_change_bits(offset, types, form):
+    n = 5003
+    a, b = make(n, types, form, 5), make(n, types, form, 5, offset=offset)
+    run([a], 9, seed=3)
+    run([b], 9, seed=3)
+    for x, y in ((a.param, b.param), (a.m, b.m), (a.v, b.v)):
+        np.testing.assert_array_equal(host(x), host(y))
+    if form == "mxfp8":
+        np.testing.assert_array_equal(host(a.m_scale), host(b.m_scale))
+        np.testing.assert_array_equal(host(a.v_scale), host(b.v_scale))
+
+
+def guarded(n, types, form, seed):
+    """Arrays inside larger ones whose rest must stay as it is."""
+    import torch
+    import paper_2607_01164_amd as gs
+    src = make(n, types, form, seed)
+    whole = {}
+
+    def inside(nm, t, pad=64):
+        if t is None:
+            return None
+        w = torch.full((t.numel() + 2 * pad,), 5, dtype=t.dtype, device="cuda")
+        w[pad:pad + t.numel()] = t
+        whole[nm] = (w, pad, t.numel())
+        return w[pad:pad + t.numel()]
+
+    t = gs.AdamTensor(inside("p", src.param), inside("g", src.grad), inside("m", src.m), inside("v", src.v),
+                      inside("ms", src.m_scale), inside("vs", src.v_scale), src.lr, src.weight_decay)
+    return t, whole
+
+
+def test_a_mixed_list_in_one_launch_and_nothing_beside_it():
+    """Tensors of every type and form, empty and tiny ones among them: each
+    follows the definition under its own place, and no byte around any array
+    changes."""
+    r = np.random.default_rng(4)
+    sizes = [0, 1, 7, 32, 0, 1024, 2049, 33, 5, 70001] + [int(x) for x in r.integers(1, 3000, 60)] + [0]
+    ts, wholes, kinds = [], [], []
+    for i, n in enumerate(sizes):
+        types, form = TYPES[i % 3], FORMS[(i // 3) % 2]
+        t, w = guarded(n, types, form, 100 + i)
+        t.lr, t.weight_decay = 0.001 * (1 + i % 5), 0.05 * (i % 3)
+        ts.append(t)
+        wholes.append(w)
+        kinds.append((n, types, form))
+    before = [snapshot(t) for t in ts]
+    run(ts, 12, seed=1 << 40, lr_scale=0.5)
+    for i, t in enumerate(ts):
+        if sizes[i]:
+            check(t, before[i], i, 12, seed=1 << 40, lr_scale=0.5, label=str((i,) + kinds[i]))
+        for nm, (w, pad, n) in wholes[i].items():
+            x = host(w)
+            assert np.all(x[:pad] == 5) and np.all(x[pad + n:] == 5), (i, nm)
+        np.testing.assert_array_equal(host(t.grad), before[i]["g"])
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_extreme_values(form):
+    """Gradients from the denormals to 1e18, alone in their blocks and beside
+    small ones, and blocks of zeros."""
+    import torch
+    import paper_2607_01164_amd as gs
+    n = 32 * 12
+    g = np.zeros(n)
+    for b, x in enumerate([0.0, 1e-45, 1e-38, 1e-30, 1e-20, 1e-10, 1.0, 1e10, 1e18]):
+        g[32 * b] = x
+        g[32 * b + 5] = -x / 3
+        g[32 * b + 9] = x * 2.0 ** -12
+    g[32 * 9:32 * 10] = 448.0
+    g[32 * 10:32 * 11] = np.exp2(np.linspace(-30, 30, 32))
+    g[32 * 11:] = -np.exp2(np.linspace(-140, -100, 32))
+    t = gs.AdamTensor.new(torch.ones(n, device="cuda"), torch.from_numpy(g.astype(np.float32)).cuda(), 0.01, 0.0,
+                          gs.GS_MOMENTS_F32 if form == "f32" else gs.GS_MOMENTS_MXFP8)
+    for k in (1, 2, 3):
+        before = snapshot(t)
+        run([t], k, seed=2)
+        check(t, before, 0, k, seed=2, sharp=False, label=f"{form} step {k}")
+    zero = slice(0, 32)
+    assert np.all(host(t.param)[zero] == 1) and np.all(snapshot(t)["m"][zero] == 0)
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("form", FORMS)
+def test_a_gradient_that_is_not_finite_stays_alone(form, bad):
+    """Without a control: its own element is lost, the block's others are
+    what they are without it."""
+    import torch
+    a, b = make(100, ("f32", "f32"), form, 8), make(100, ("f32", "f32"), form, 8)
+    with torch.no_grad():
+        a.grad[40] = bad
+        b.grad[40] = 0.0
+        for t in (a, b):  # so that element 40 has no part in the block's scale
+            t.m[40] = 0
+            t.v[40] = 0
+    run([a], 3)
+    run([b], 3)
+    others = np.arange(100) != 40
+    for x, y in ((a.param, b.param), (a.m, b.m), (a.v, b.v)):
+        np.testing.assert_array_equal(host(x)[others], host(y)[others])
+    if form == "mxfp8":
+        assert host(a.m)[40] & 0x7F == 0x7F and host(a.v)[40] & 0x7F == 0x7F
+        run([a], 4)
+        assert np.isnan(snapshot(a)["m"][40]) and np.isfinite(np.delete(snapshot(a)["m"], 40)).all()
+    else:
+        assert not np.isfinite(host(a.m)[40])
+
+
+def test_bfloat16_parameters_that_are_not_finite():
+    import torch
+    t = make(64, ("bf16", "bf16"), "f32", 3)
+    t.param[3], t.param[4], t.param[5] = float("inf"), float("nan"), 3.38e38
+    t.grad[7] = float("nan")
+    t.lr, t.weight_decay = 0.01, 0.0
+    run([t], 1)
+    p = host(t.param)
+    # 0 * infinity in the decay's term: an infinite parameter becomes NaN
+    assert np.isnan(p[3]) and np.isnan(p[4]) and p[5] > 3.3e38 and np.isnan(p[7])
+    assert np.isfinite(np.delete(p, [3, 4, 7])).all()
+
+
+def test_list_of_nothing():
+    import torch
+    import paper_2607_01164_amd as gs
+    empty = torch.empty(0, device="cuda")
+    for ts in ([], [gs.AdamTensor.new(empty, empty, 0.1)]):
+        plan = gs.AdamPlan(ts, device="cuda")
+        control = gs.alloc_adam_control("cuda")
+        gs.gs_grad_norm(plan, control)
+        gs.gs_adamw(plan, control=control)
+        assert gs.read_adam_control(control) == {"step": 1, "skipped": 0, "norm": 0.0, "clip": 1.0, "apply": 1}
+
+
+# ---- norm and control -------------------------------------------------------
+
+@pytest.mark.parametrize("gtype", ["f32", "bf16"])
+@pytest.mark.parametrize("sizes", [[1], [5, 0, 1024], [1025, 3, 4096, 77], [3000017], [1] * 300],
+                         ids=["one", "three", "four", "large", "many"])
+def test_norm(sizes, gtype):
+    import torch
+    import paper_2607_01164_amd as gs
+    r = np.random.default_rng(sum(sizes))
+    gsl = [torch.from_numpy((r.normal(size=n) * np.exp(r.normal(size=n) * 2)).astype(np.float32)).to(dtype(gtype)).cuda()
+           for n in sizes]
+    plan = gs.AdamPlan([gs.AdamTensor(None, g) for g in gsl])
+    want = math.sqrt(math.fsum(float(x) for g in gsl for x in np.square(host(g))))
+    for max_norm in (float("inf"), want * 2, want / 3):
+        control = gs.alloc_adam_control("cuda")
+        got = []
+        for k in range(3):
+            gs.gs_grad_norm(plan, control, max_norm=max_norm, beta1=B1, beta2=B2)
+            got.append(host(control).copy())
+        c = gs.read_adam_control(control)
+        # float64 sums of at most 2^24 squares: 2^-29 at most of the sum
+        assert abs(c["norm"] - want) <= want * (oo.U + 2.0 ** -29) and c["step"] == 3 and c["skipped"] == 0
+        clip = max_norm / want if want > max_norm else 1.0
+        assert abs(c["clip"] - clip) <= clip * (oo.U + 2.0 ** -29)
+        assert np.array_equal(got[0][16:24], got[1][16:24]) and np.array_equal(got[1][16:24], got[2][16:24])
+        first, second = control[24:32].view(torch.float32).tolist()
+        assert abs(first * (1 - B1 ** 3) - 1) <= 2 * oo.U and abs(second * math.sqrt(1 - B2 ** 3) - 1) <= 2 * oo.U
+
+
+def test_norm_of_large_and_small_gradients():
+    import torch
+    import paper_2607_01164_amd as gs
+    for x in (3e38, 1e25, 1e-30, 1e-44):
+        g = torch.full((1000,), x, device="cuda")
+        control = gs.alloc_adam_control("cuda")
+        gs.gs_grad_norm(gs.AdamPlan([gs.AdamTensor(None, g)]), control, max_norm=1.0)
+        c = gs.read_adam_control(control)
+        want = float(g[0].double()) * math.sqrt(1000)
+        assert (c["norm"] == math.inf if want > 3.5e38 else abs(c["norm"] - want) <= 2 * oo.U * want + oo.TINY), x
+        assert c["step"] == 1 and abs(c["clip"] * max(want, 1.0) - 1.0) < 1e-6 + (1.0 if want > 1e38 else 0.0)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("types", TYPES, ids=["-".join(t) for t in TYPES])
+def test_clipped_steps_and_skipped_ones(types, form):
+    import torch
+    import paper_2607_01164_amd as gs
+    ts = [make(n, types, form, 40 + n) for n in (3000, 12, 1025)]
+    plan, control = gs.AdamPlan(ts), gs.alloc_adam_control("cuda")
+    done = 0
+    for k in range(5):
+        bad = k in (1, 3)
+        if bad:
+            keep = ts[k % 2].grad[7].clone()
+            ts[k % 2].grad[7] = float("inf") if k == 1 else float("nan")
+        before = [snapshot(t) for t in ts]
+        raw = [[host(x).copy() for x in (t.param, t.m, t.v)] for t in ts]
+        gs.gs_grad_norm(plan, control, max_norm=0.5, beta1=B1, beta2=B2)
+        gs.gs_adamw(plan, beta1=B1, beta2=B2, eps=EPS, control=control, seed=6)
+        c = gs.read_adam_control(control)
+        if bad:
+            assert c["apply"] == 0 and c["step"] == done and not math.isfinite(c["norm"])
+            for t, want in zip(ts, raw):
+                for x, y in zip((t.param, t.m, t.v), want):
+                    np.testing.assert_array_equal(host(x), y)
+            ts[k % 2].grad[7] = keep
+            continue
+        done += 1
+        norm = math.sqrt(math.fsum(float(x) for b in before for x in np.square(b["g"])))
+        assert c["apply"] == 1 and c["step"] == done and c["clip"] < 1 and abs(c["norm"] / norm - 1) < 1e-6
+        for i, t in enumerate(ts):
+            check(t, before[i], i, done, seed=6, clip=0.5 / norm, label=f"{types} {form} call {k} tensor {i}")
+    assert c["skipped"] == 2
+
+
+def test_captured_steps_replay_as_eager_ones():
+    """Norm and step in a graph: replays, with other work and waits between
+    them, give the eager steps' bits (each step has its own random bits)."""
+    import torch
+    import paper_2607_01164_amd as gs
+
+    def lists():
+        return [make(2000, ("f32", "f32"), "mxfp8", 1), make(77, ("bf16", "bf16"), "f32", 2),
+                make(5000, ("f32", "bf16"), "f32", 3)]
+
+    def once(plan, control):
+        gs.gs_grad_norm(plan, control, max_norm=0.3)
+        gs.gs_adamw(plan, control=control, seed=5)
+
+    eager, replayed = lists(), lists()
+    pe, pr = gs.AdamPlan(eager), gs.AdamPlan(replayed)
+    ce, cr = gs.alloc_adam_control("cuda"), gs.alloc_adam_control("cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        once(pr, cr)
+    for k in range(5):
+        once(pe, ce)
+        if k % 2:
+            torch.cuda.synchronize()
+        graph.replay()
+        noise = torch.randn(1 << 20, device="cuda").sum()
+        for a, b in zip(eager, replayed):
+            a.grad.mul_(0.9)
+            b.grad.mul_(0.9)
+        torch.cuda.synchronize()
+        assert torch.isfinite(noise)
+        assert gs.read_adam_control(ce) == gs.read_adam_control(cr) and gs.read_adam_control(cr)["step"] == k + 1
+        for a, b in zip(eager, replayed):
+            for x, y in ((a.param, b.param), (a.m, b.m), (a.v, b.v), (a.m_scale, b.m_scale)):
+                if x is not None:
+                    np.testing.assert_array_equal(host(x), host(y))
+
+
+def test_on_a_stream_of_its_own():
+    import torch
+    import paper_2607_01164_amd as gs
+    a, b = make(100003, ("f32", "f32"), "mxfp8", 11), make(100003, ("f32", "f32"), "mxfp8", 11)
+    run([a], 4, seed=9)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    plan = gs.AdamPlan([b], stream=s)
+    gs.gs_adamw(plan, step=4, beta1=B1, beta2=B2, eps=EPS, seed=9, stream=s)
+    s.synchronize()
+    np.testing.assert_array_equal(host(a.param), host(b.param))
+    np.testing.assert_array_equal(host(a.m), host(b.m))
+
+
+def test_elements_past_32_bits():
+    """A tensor of 2^32 + 999 elements: the last ones use their own random
+    bits and addresses."""
+    import torch
+    import paper_2607_01164_amd as gs
+    n, tail = (1 << 32) + 999, 1500
+    log("case: 2^32 + 999 elements, bf16 with 8-bit moments")
+    free, _ = torch.cuda.mem_get_info()
+    if free < 40 << 30:
+        pytest.skip("needs 40 GiB")
+    p = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    t = gs.AdamTensor.new(p, g, 0.01, 0.1, gs.GS_MOMENTS_MXFP8)
+    src = make(tail, ("bf16", "bf16"), "f32", 6)
+    # the tail starts inside a block of 32 (2^32 + 999 - 1500 = 32 k + 11)
+    start = (n - tail) // 32 * 32
+    at = n - start
+    p[n - tail:], g[n - tail:] = src.param, src.grad
+    last = lambda x: x[start:]  # noqa: E731
+    view = gs.AdamTensor(last(p), last(g), last(t.m), last(t.v), t.m_scale[start // 32:], t.v_scale[start // 32:],
+                         t.lr, t.weight_decay)
+    for k in (1, 2):
+        before = snapshot(view)
+        run([t], k, seed=31)
+        assert view.grad.numel() == at
+        check(view, before, 0, k, seed=31, first=start, label=f"tail step {k}")
+    control = gs.alloc_adam_control("cuda")
+    gs.gs_grad_norm(gs.AdamPlan([gs.AdamTensor(None, g)]), control)
+    want = math.sqrt(math.fsum(float(x) for x in np.square(host(src.grad))))
+    assert abs(gs.read_adam_control(control)["norm"] / want - 1) <= 2 * oo.U
+    assert not p[:1 << 20].any() and not t.m[(1 << 31):(1 << 31) + 4096].any()
+
+
+# ---- the rounding as a whole ------------------------------------------------
+
+def test_averages_move_although_a_step_is_below_the_grid():
+    """A steady m and v whose gradients stop: after 2000 steps sqrt(v) has
+    fallen by 0.999^1000, on average over many elements, as in 32 bits;
+    rounding to the nearest would leave every code where it is."""
+    import torch
+    import paper_2607_01164_amd as gs
+    n = 1 << 16
+    r = np.random.default_rng(3)
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    t = gs.AdamTensor.new(p, g, 0.0, 0.0, gs.GS_MOMENTS_MXFP8)
+    codes = r.integers(72, 120, n)  # within a factor of 64, away from the grid's end
+    codes[::32] = 0x7E
+    t.v.copy_(torch.from_numpy(codes.astype(np.uint8)))
+    t.v_scale.fill_(127)
+    start = snapshot(t)["v"].copy()
+    plan = gs.AdamPlan([t])
+    for k in range(2000):
+        gs.gs_adamw(plan, beta1=0.9, beta2=0.999, step=k + 1, seed=4)
+    got = np.sqrt(snapshot(t)["v"] / start)
+    want = 0.999 ** 1000
+    # E[s] is kept by each rounding, and s s exceeds the mean's square by the
+    # variance of one rounding, at most (1/8 s)^2 / 4 = 0.4 % of v, acting on
+    # a rate of 1e-3: a walk of 2000 steps whose variance is below 2000 *
+    # 5e-4 * 1/8 = 0.125 of s^2; the mean over 2^16 elements stands to 1 %
+    # beside the drift of the rounded square, 2000 * 5e-4 / 8 / 2 = 6 %
+    log(f"  sqrt(v) after 2000 steps: {got.mean():.4f} of the start, in 32 bits {want:.4f}")
+    assert abs(got.mean() / want - 1) < 0.08
+
+
+def test_training_with_8_bit_moments_keeps_up():
+    """Noisy quadratic: the loss after 600 steps with MXFP8 moments is
+    within a tenth of the one with float32 moments."""
+    import torch
+    import paper_2607_01164_amd as gs
+    n = 1 << 15
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    target = torch.randn(n, generator=gen, device="cuda")
+    curve = torch.exp(torch.randn(n, generator=gen, device="cuda") * 2)
+    loss = {}
+    for form in (gs.GS_MOMENTS_F32, gs.GS_MOMENTS_MXFP8):
+        noise = torch.Generator(device="cuda").manual_seed(2)
+        p, g = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+        plan = gs.AdamPlan([gs.AdamTensor.new(p, g, 0.01, 0.0, form)])
+        for k in range(600):
+            g.copy_(curve * (p - target + 0.3 * torch.randn(n, generator=noise, device="cuda")))
+            gs.gs_adamw(plan, step=k + 1, seed=8)
+        loss[form] = float((p - target).square().mean())
+    log(f"  mean squared error: 32 bits {loss[0]:.5f}, 8 bits {loss[1]:.5f}")
+    assert loss[0] < 0.05 and loss[1] < 1.1 * loss[0] + 1e-3
+
+
+# ---- moments through a densification ----------------------------------------
+
+def carried(width, form, n_in, source, seed, extra=0):
+    import torch
+    import paper_2607_01164_amd as gs
+    t = make(max(n_in * width, 1), ("f32", "f32"), form, seed)
+    n_out = len(source)
+    full = lambda k, dt: torch.full((k + 64 + extra,), 9, dtype=dt, device="cuda")[extra:]  # noqa: E731
+    dt = torch.float32 if form == "f32" else torch.uint8
+    out = {"m": full(n_out * width, dt), "v": full(n_out * width, dt)}
+    if form == "mxfp8":
+        out["ms"], out["vs"] = full(gs.moment_scales(n_out * width), dt), full(gs.moment_scales(n_out * width), dt)
+    rows = gs.AdamRows(width, t.m, t.v, out["m"], out["v"], t.m_scale, t.v_scale, out.get("ms"), out.get("vs"))
+    return t, rows, out
+
+
+def check_carried(t, rows, out, width, form, n_in, source, label):
+    import paper_2607_01164_amd as gs
+    n_out, b = len(source), snapshot(t)
+    src = np.asarray(source, dtype=np.int64)
+    live = (src >= 0) & (src < n_in)
+    n = n_out * width
+    for k, x in (("m", b["m"]), ("v", b["v"])):
+        if form == "mxfp8" and k == "v":
+            x = np.sqrt(x)
+        want = np.where(live[:, None], x[:n_in * width].reshape(n_in, width)[np.where(live, src, 0)] if n_in else 0.0,
+                        0.0).reshape(-1)
+        got = host(out[k])
+        assert np.all(got[n:n + 64] == 9), label
+        if form == "f32":
+            np.testing.assert_array_equal(got[:n], want)
+        else:
+            sc, k8 = host(out[k + "s"]), gs.moment_scales(n)
+            assert np.all(sc[k8:k8 + 64] == 9), label
+            oo.check_mxfp8(got[:n], sc[:k8], want, 0.0 * want, positive=k == "v", label=f"{label} {k}")
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("width", [1, 2, 3, 4, 7, 33, 64])
+@pytest.mark.parametrize("kind", ["kept", "shuffled", "one", "new", "outside"])
+def test_carry(width, kind, form):
+    import torch
+    import paper_2607_01164_amd as gs
+    r = np.random.default_rng(width)
+    n_in = 1237
+    source = {"kept": np.concatenate([np.flatnonzero(r.random(n_in) < 0.8), -1 - np.arange(200)]),
+              "shuffled": r.permutation(n_in)[:1000], "one": np.array([1236]), "new": -1 - np.arange(77),
+              "outside": np.array([0, n_in, 5, -2 ** 31, 2 ** 31 - 1, n_in - 1, -1])}[kind]
+    t, rows, out = carried(width, form, n_in, source, 60 + width, extra=width % 3)
+    src = torch.from_numpy(source.astype(np.int32)).cuda()
+    gs.gs_adamw_carry(gs.AdamCarry([rows]), n_in, src, len(source))
+    torch.cuda.synchronize()
+    check_carried(t, rows, out, width, form, n_in, source, f"{width} {kind} {form}")
+
+
+def test_carry_of_a_set_in_one_launch():
+    """The five arrays of a set of Gaussians in both forms, ten in all, and
+    sets without rows."""
+    import torch
+    import paper_2607_01164_amd as gs
+    r = np.random.default_rng(9)
+    n_in = 20011
+    source = np.concatenate([np.flatnonzero(r.random(n_in) < 0.9), -1 - np.arange(4001)])
+    arrays = [(w, f) for f in FORMS for w in (3, 3, 4, 1, 1)]
+    made = [carried(w, f, n_in, source, 70 + i) for i, (w, f) in enumerate(arrays)]
+    src = torch.from_numpy(source.astype(np.int32)).cuda()
+    carry = gs.AdamCarry([x[1] for x in made])
+    gs.gs_adamw_carry(carry, n_in, src, len(source))
+    torch.cuda.synchronize()
+    for (w, f), (t, rows, out) in zip(arrays, made):
+        check_carried(t, rows, out, w, f, n_in, source, f"{w} {f}")
+    gs.gs_adamw_carry(carry, n_in, src, 0)
+    gs.gs_adamw_carry(carry, 0, src, 100)  # from nothing: every row is new
+    torch.cuda.synchronize()
+    for (w, f), (t, rows, out) in zip(arrays, made):
+        assert np.all(host(out["m"])[:100 * w] == 0) and np.all(host(out["v"])[:100 * w] == 0)
+    with pytest.raises(ValueError):
+        gs.gs_adamw_carry(carry, n_in + 1, src, 10)
