@@ -8,9 +8,10 @@
  * gs_status codes with gs_last_error(), no device memory allocated by the
  * library. Every call may be captured into a HIP graph.
  *
- * The update of one parameter, in float32 with every operation rounded, at
- * step t = 1, 2, ... (lr' = lr lr_scale; the 1 / (1 - beta^t) terms and
- * 1 - beta are formed in float64 and rounded once; g' = clip g):
+ * The update of one parameter, in float32, at step t = 1, 2, ... (lr' = lr
+ * lr_scale; the 1 / (1 - beta^t) terms and 1 - beta are formed in float64
+ * and rounded once; g' = clip g; products and sums round once each or are
+ * fused, root and reciprocal are good to an ulp):
  *   m <- beta1 m + (1 - beta1) g'
  *   v <- beta2 v + ((1 - beta2) g') g'
  *   p <- p - ( lr' / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)  +  lr wd lr_scale p )
@@ -82,10 +83,12 @@ typedef struct gs_adamw_plan {
     void *work; /* gs_adamw_plan_bytes() bytes, 256-byte aligned; kept while the plan is in use */
     size_t work_bytes;
     /* filled by gs_plan_adamw */
-    int64_t n_items;    /* pieces that the tensors are cut into */
-    int64_t n_elements; /* of all tensors */
-    int32_t count;      /* tensors */
-    int32_t updatable;  /* whether every tensor with elements has a parameter */
+    int64_t n_items;      /* pieces that the tensors are cut into for the step */
+    int64_t n_norm_items; /* and for the norm */
+    int64_t step_bytes;   /* what a step reads and writes */
+    int64_t norm_bytes;   /* what the norm reads */
+    int32_t count;        /* tensors */
+    int32_t updatable;    /* whether every tensor with elements has a parameter */
 } gs_adamw_plan;
 
 /* What a training run keeps on the device between steps: 64 bytes, 8-byte

@@ -517,36 +517,53 @@ void *scratch_address(hipError_t *err) {
     return g_scratch_ptr[dev];
 }
 
-// Pieces and elements of a list of tensors; false if it is malformed.
-bool adamw_sizes(const gs_adamw_tensor *tensors, int64_t count, int64_t *items, int64_t *elements) {
+// Pieces and sizes of a list of tensors; false if it is malformed.
+struct AdamwSizes {
+    int64_t items = 0, norm_items = 0, elements = 0, step_bytes = 0, norm_bytes = 0;
+};
+bool adamw_sizes(const gs_adamw_tensor *tensors, int64_t count, AdamwSizes *z) {
     if (count < 0 || count > ((int64_t)1 << 20) || (count > 0 && !tensors)) return false;
     for (int64_t i = 0; i < count; ++i) {
-        if (tensors[i].n < 0 || tensors[i].n >= ((int64_t)1 << 40)) return false;
-        *items += optim_items(tensors[i].n);
-        *elements += tensors[i].n;
-        if (*items >= ((int64_t)1 << 31)) return false;
+        const gs_adamw_tensor &t = tensors[i];
+        if (t.n < 0 || t.n >= ((int64_t)1 << 40)) return false;
+        const int64_t ps = t.param_type == GS_TYPE_BF16 ? 2 : 4, gs = t.grad_type == GS_TYPE_BF16 ? 2 : 4;
+        const int64_t ms = t.moments == GS_MOMENTS_MXFP8 ? 1 : 4;
+        z->elements += t.n;
+        z->norm_bytes += t.n * gs;
+        if (t.param) {
+            z->items += optim_items(t.n);
+            z->step_bytes += t.n * (2 * ps + gs + 4 * ms);
+        }
+        if (z->items >= ((int64_t)1 << 31)) return false;
     }
-    return true;
+    for (int64_t i = 0; i < count; ++i) z->norm_items += norm_items(tensors[i].n, norm_chunk(z->elements));
+    return z->norm_items < ((int64_t)1 << 31);
 }
 
 struct AdamwPlanLayout {
     OptimItem *items;
+    NormItem *norms;
     double *part;
     size_t bytes;
 };
-AdamwPlanLayout adamw_plan_layout(void *work, int64_t items) {
+AdamwPlanLayout adamw_plan_layout(void *work, int64_t items, int64_t norms) {
     Carver c(work);
     AdamwPlanLayout l;
     l.part = c.take<double>(optim_part_bytes() / sizeof(double));
+    l.norms = c.take<NormItem>((size_t)norms);
     l.items = c.take<OptimItem>((size_t)items);
     l.bytes = c.off;
     return l;
 }
 
+// Sizes from which a call's data are past the 256 MB of the last-level
+// cache, so that keeping them there only drives out what could be read again.
+constexpr int64_t kOnceBytes = (int64_t)256 << 20;
+
 gs_status check_adamw(const char *who, const gs_adamw_plan *plan, const gs_adamw_params *params) {
     if (!plan || !params) return fail(GS_ERR_INVALID_ARGUMENT, "%s: plan or settings are null", who);
-    if (plan->n_items < 0 || !plan->work || !aligned(plan->work) ||
-        plan->work_bytes < adamw_plan_layout(nullptr, plan->n_items).bytes)
+    if (plan->n_items < 0 || plan->n_norm_items < 0 || !plan->work || !aligned(plan->work) ||
+        plan->work_bytes < adamw_plan_layout(nullptr, plan->n_items, plan->n_norm_items).bytes)
         return fail(GS_ERR_INVALID_ARGUMENT, "%s: the plan was not made by gs_plan_adamw", who);
     if (!(params->beta1 >= 0.0 && params->beta1 < 1.0 && params->beta2 >= 0.0 && params->beta2 < 1.0))
         return fail(GS_ERR_INVALID_ARGUMENT, "%s: beta1 and beta2 must lie in [0, 1)", who);
@@ -1055,16 +1072,16 @@ gs_status gs_densify(const gs_params *in, int64_t n_in, const float *weight, con
 }
 
 size_t gs_adamw_plan_bytes(const gs_adamw_tensor *tensors, int64_t count) {
-    int64_t items = 0, elements = 0;
-    if (!adamw_sizes(tensors, count, &items, &elements)) return (size_t)-1;
-    return adamw_plan_layout(nullptr, items).bytes;
+    AdamwSizes z;
+    if (!adamw_sizes(tensors, count, &z)) return (size_t)-1;
+    return adamw_plan_layout(nullptr, z.items, z.norm_items).bytes;
 }
 
 gs_status gs_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, gs_adamw_plan *plan, hipStream_t stream) {
     if (!plan) return fail(GS_ERR_INVALID_ARGUMENT, "gs_plan_adamw: plan is null");
-    plan->n_items = -1;
-    int64_t items = 0, elements = 0;
-    if (!adamw_sizes(tensors, count, &items, &elements))
+    plan->n_items = plan->n_norm_items = -1;
+    AdamwSizes z;
+    if (!adamw_sizes(tensors, count, &z))
         return fail(GS_ERR_INVALID_ARGUMENT, "gs_plan_adamw: null list, or a count or size out of range");
     bool updatable = true;
     for (int64_t i = 0; i < count; ++i) {
@@ -1090,13 +1107,15 @@ gs_status gs_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, gs_adamw_
             return bad("moments are null or not aligned to their type");
         if (m8 && (!t.m_scale || !t.v_scale)) return bad("the scales of MXFP8 moments are null");
     }
-    const AdamwPlanLayout l = adamw_plan_layout(plan->work, items);
+    const AdamwPlanLayout l = adamw_plan_layout(plan->work, z.items, z.norm_items);
     if (!plan->work || plan->work_bytes < l.bytes || !aligned(plan->work))
         return fail(GS_ERR_WORKSPACE, "gs_plan_adamw: plan needs %zu bytes, 256-byte aligned (got %zu)", l.bytes,
                     plan->work_bytes);
-    GS_TRY(launch_plan_adamw(tensors, count, l.items, stream), "gs_plan_adamw");
-    plan->n_items = items;
-    plan->n_elements = elements;
+    GS_TRY(launch_plan_adamw(tensors, count, z.elements, l.items, l.norms, stream), "gs_plan_adamw");
+    plan->n_items = z.items;
+    plan->n_norm_items = z.norm_items;
+    plan->step_bytes = z.step_bytes;
+    plan->norm_bytes = z.norm_bytes;
     plan->count = (int32_t)count;
     plan->updatable = updatable;
     return GS_OK;
@@ -1109,8 +1128,8 @@ gs_status gs_grad_norm(const gs_adamw_plan *plan, const gs_adamw_params *params,
     if (!(params->max_norm > 0.0)) return fail(GS_ERR_INVALID_ARGUMENT, "gs_grad_norm: max_norm must be > 0");
     if (!control || (uintptr_t)control % 8)
         return fail(GS_ERR_INVALID_ARGUMENT, "gs_grad_norm: control is null or not 8-byte aligned");
-    const AdamwPlanLayout l = adamw_plan_layout(plan->work, plan->n_items);
-    GS_TRY(launch_grad_norm(l.items, plan->n_items, l.part,
+    const AdamwPlanLayout l = adamw_plan_layout(plan->work, plan->n_items, plan->n_norm_items);
+    GS_TRY(launch_grad_norm(l.norms, plan->n_norm_items, plan->norm_bytes >= kOnceBytes, l.part,
                             NormArgs{params->beta1, params->beta2, params->max_norm}, control, stream),
            "gs_grad_norm");
     return GS_OK;
@@ -1141,8 +1160,8 @@ gs_status gs_adamw(const gs_adamw_plan *plan, const gs_adamw_params *params, int
         a.first = (float)(1.0 / (1.0 - std::pow(params->beta1, (double)step)));
         a.second = (float)(1.0 / std::sqrt(1.0 - std::pow(params->beta2, (double)step)));
     }
-    const AdamwPlanLayout l = adamw_plan_layout(plan->work, plan->n_items);
-    GS_TRY(launch_adamw(l.items, plan->n_items, a, control, stream), "gs_adamw");
+    const AdamwPlanLayout l = adamw_plan_layout(plan->work, plan->n_items, plan->n_norm_items);
+    GS_TRY(launch_adamw(l.items, plan->n_items, plan->step_bytes >= kOnceBytes, a, control, stream), "gs_adamw");
     return GS_OK;
 }
 

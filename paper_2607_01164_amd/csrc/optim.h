@@ -37,6 +37,13 @@ struct alignas(16) OptimItem {
     uint32_t flags, pad;
 };
 
+// A piece of a tensor for the norm, longer than an OptimItem.
+struct alignas(16) NormItem {
+    const void *g;
+    int32_t count;
+    uint32_t flags;
+};
+
 struct StepArgs {
     float b1, a1, b2, a2, eps, lr_scale, first, second;
     uint64_t step, seed;
@@ -51,6 +58,9 @@ struct CarryArgs {
     int64_t n_in, n_out;
 };
 
+// Elements of a NormItem at most.
+inline int64_t norm_chunk(int64_t elements) { return elements < (int64_t)1 << 25 ? 4096 : 16384; }
+inline int64_t norm_items(int64_t n, int64_t chunk) { return (n + chunk - 1) / chunk; }
 inline int64_t optim_items(int64_t n) { return (n + kOptimChunk - 1) / kOptimChunk; }
 inline uint32_t optim_flags(const gs_adamw_tensor &t) {
     uint32_t f = 0;
@@ -66,11 +76,13 @@ inline uint32_t optim_flags(const gs_adamw_tensor &t) {
 }
 
 size_t optim_part_bytes();
-hipError_t launch_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, OptimItem *items, hipStream_t s);
-hipError_t launch_grad_norm(const OptimItem *items, int64_t n_items, double *part, const NormArgs &a,
+hipError_t launch_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, int64_t elements, OptimItem *items,
+                             NormItem *norms, hipStream_t s);
+// once: keep nothing in the caches
+hipError_t launch_grad_norm(const NormItem *items, int64_t n_items, bool once, double *part, const NormArgs &a,
                             gs_adamw_control *control, hipStream_t s);
-hipError_t launch_adamw(const OptimItem *items, int64_t n_items, const StepArgs &a, const gs_adamw_control *control,
-                        hipStream_t s);
+hipError_t launch_adamw(const OptimItem *items, int64_t n_items, bool once, const StepArgs &a,
+                        const gs_adamw_control *control, hipStream_t s);
 hipError_t launch_adamw_carry(const gs_adamw_rows *arrays, int count, int64_t n_in, const int32_t *source,
                               int64_t n_out, hipStream_t s);
 

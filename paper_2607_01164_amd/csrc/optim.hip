@@ -19,67 +19,112 @@ typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u2v __attribute__((ext_vector_type(2)));
 
 constexpr int kFill = 24;         // tensors whose pieces one launch of k_fill_items writes
+constexpr uint32_t kXcdItems = 32;     // neighbouring items that one XCD takes
 constexpr int64_t kMaxGrid = 1 << 23;  // workgroups of a launch at most: 2^31 threads
-constexpr int kNormBlocks = 1024; // workgroups of the norm at most: one partial sum each
+constexpr int kNormBlocks = 2048;      // workgroups of the norm at most: one partial sum each
 
 struct FillArgs {
     OptimTensor t[kFill];
-    uint32_t first[kFill + 1];  // first item of each, counted from the launch's first
-    int count;
+    uint32_t first[kFill + 1];       // first item of each, counted from the launch's first
+    uint32_t first_norm[kFill + 1];  // the same of its NormItems
+    int count, norm_chunk;
 };
 
 // ---- items ----------------------------------------------------------------
 
-__global__ __launch_bounds__(kBlock) void k_fill_items(FillArgs a, OptimItem *items) {
+__global__ __launch_bounds__(kBlock) void k_fill_items(FillArgs a, OptimItem *items, NormItem *norms) {
     const uint32_t i = blockIdx.x * kBlock + threadIdx.x;
-    if (i >= a.first[a.count]) return;
-    int k = 0;
-    while (i >= a.first[k + 1]) ++k;
-    const OptimTensor t = a.t[k];
-    const int64_t base = (int64_t)(i - a.first[k]) * kOptimChunk;
-    const int64_t left = t.n - base;
-    OptimItem it;
-    const int ps = t.flags & kParamBf16 ? 2 : 4, gs = t.flags & kGradBf16 ? 2 : 4, ms = t.flags & kMoments8 ? 1 : 4;
-    it.p = t.p ? (char *)t.p + base * ps : nullptr;
-    it.g = (const char *)t.g + base * gs;
-    it.m = t.m ? (char *)t.m + base * ms : nullptr;
-    it.v = t.v ? (char *)t.v + base * ms : nullptr;
-    it.ms = t.ms ? t.ms + base / 32 : nullptr;
-    it.vs = t.vs ? t.vs + base / 32 : nullptr;
-    it.base = base;
-    it.count = (int32_t)(left < kOptimChunk ? left : kOptimChunk);
-    it.place = t.place;
-    it.lr = t.lr;
-    it.wd = t.wd;
-    it.flags = t.flags;
-    it.pad = 0;
-    items[i] = it;
+    if (i < a.first[a.count]) {
+        int k = 0;
+        while (i >= a.first[k + 1]) ++k;
+        const OptimTensor t = a.t[k];
+        const int64_t base = (int64_t)(i - a.first[k]) * kOptimChunk;
+        const int64_t left = t.n - base;
+        OptimItem it;
+        const int ps = t.flags & kParamBf16 ? 2 : 4, gs = t.flags & kGradBf16 ? 2 : 4;
+        const int ms = t.flags & kMoments8 ? 1 : 4;
+        it.p = (char *)t.p + base * ps;
+        it.g = (const char *)t.g + base * gs;
+        it.m = (char *)t.m + base * ms;
+        it.v = (char *)t.v + base * ms;
+        it.ms = t.ms ? t.ms + base / 32 : nullptr;
+        it.vs = t.vs ? t.vs + base / 32 : nullptr;
+        it.base = base;
+        it.count = (int32_t)(left < kOptimChunk ? left : kOptimChunk);
+        it.place = t.place;
+        it.lr = t.lr;
+        it.wd = t.wd;
+        it.flags = t.flags;
+        it.pad = 0;
+        items[i] = it;
+    }
+    if (i < a.first_norm[a.count]) {
+        int k = 0;
+        while (i >= a.first_norm[k + 1]) ++k;
+        const OptimTensor t = a.t[k];
+        const int64_t base = (int64_t)(i - a.first_norm[k]) * a.norm_chunk;
+        const int64_t left = t.n - base;
+        NormItem it;
+        it.g = (const char *)t.g + base * (t.flags & kGradBf16 ? 2 : 4);
+        it.count = (int32_t)(left < a.norm_chunk ? left : a.norm_chunk);
+        it.flags = t.flags;
+        norms[i] = it;
+    }
 }
 
+// Through words and shifts: an item that is read as one object stays in
+// memory, which the compiler then moves to LDS.
 __device__ __forceinline__ OptimItem load_item(const OptimItem *items, uint32_t i) {
     static_assert(sizeof(OptimItem) == 80, "read as five quarters");
-    union {
-        i4v q[5];
-        OptimItem it;
-    } u;
     ConstI4 *p = (ConstI4 *)(items + i);
-#pragma unroll
-    for (int k = 0; k < 5; ++k) u.q[k] = p[k];
-    return u.it;
+    const i4v a = p[0], b = p[1], c = p[2], d = p[3], e = p[4];
+    const auto address = [](int lo, int hi) { return (uint64_t)(uint32_t)hi << 32 | (uint32_t)lo; };
+    OptimItem it;
+    it.p = (void *)address(a.x, a.y);
+    it.g = (const void *)address(a.z, a.w);
+    it.m = (void *)address(b.x, b.y);
+    it.v = (void *)address(b.z, b.w);
+    it.ms = (uint8_t *)address(c.x, c.y);
+    it.vs = (uint8_t *)address(c.z, c.w);
+    it.base = (int64_t)address(d.x, d.y);
+    it.count = d.z;
+    it.place = (uint32_t)d.w;
+    it.lr = __builtin_bit_cast(float, (int)e.x);
+    it.wd = __builtin_bit_cast(float, (int)e.y);
+    it.flags = (uint32_t)e.z;
+    return it;
+}
+
+__device__ __forceinline__ NormItem load_norm_item(const NormItem *items, uint32_t i) {
+    static_assert(sizeof(NormItem) == 16, "read at once");
+    return __builtin_bit_cast(NormItem, *(ConstI4 *)(items + i));
 }
 
 // ---- element types ----------------------------------------------------------
 
 __device__ __forceinline__ float bf16_to_f32(uint32_t b) { return __builtin_bit_cast(float, b << 16); }
 
-// Four consecutive elements, of which k are there, as float32 bits. Vector
-// loads where the arrays allow them, single ones elsewhere.
-template <bool BF16>
-__device__ __forceinline__ void load4(const void *base, int i, int k, bool vec, float x[4]) {
+// Loads and stores that keep nothing in the caches (ONCE), or ordinary ones.
+template <bool ONCE, typename T>
+__device__ __forceinline__ T get(Glob<const T> *p) {
+    return ONCE ? __builtin_nontemporal_load(p) : *p;
+}
+template <bool ONCE, typename T>
+__device__ __forceinline__ void put(Glob<T> *p, T x) {
+    if (ONCE)
+        __builtin_nontemporal_store(x, p);
+    else
+        *p = x;
+}
+
+// Four consecutive elements as float32. FAST: all there, on a vector's
+// boundary. Otherwise the first k, one by one, and zeros.
+template <bool BF16, bool FAST, bool ONCE>
+__device__ __forceinline__ void load4(const void *base, int i, int k, float x[4]) {
     if (BF16) {
         Glob<const uint16_t> *p = (Glob<const uint16_t> *)base + i;
-        if (vec && k == 4) {
-            const u2v q = *(Glob<const u2v> *)p;
+        if (FAST) {
+            const u2v q = get<ONCE>((Glob<const u2v> *)p);
             x[0] = bf16_to_f32(q.x & 0xFFFFu);
             x[1] = bf16_to_f32(q.x >> 16);
             x[2] = bf16_to_f32(q.y & 0xFFFFu);
@@ -90,8 +135,8 @@ __device__ __forceinline__ void load4(const void *base, int i, int k, bool vec, 
         }
     } else {
         Glob<const float> *p = (Glob<const float> *)base + i;
-        if (vec && k == 4) {
-            const f4v q = *(Glob<const f4v> *)p;
+        if (FAST) {
+            const f4v q = get<ONCE>((Glob<const f4v> *)p);
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[j] = q[j];
         } else {
@@ -101,10 +146,11 @@ __device__ __forceinline__ void load4(const void *base, int i, int k, bool vec, 
     }
 }
 
-__device__ __forceinline__ void store4_f32(void *base, int i, int k, bool vec, const float x[4]) {
+template <bool FAST, bool ONCE>
+__device__ __forceinline__ void store4_f32(void *base, int i, int k, const float x[4]) {
     Glob<float> *p = (Glob<float> *)base + i;
-    if (vec && k == 4) {
-        *(Glob<f4v> *)p = f4v{x[0], x[1], x[2], x[3]};
+    if (FAST) {
+        put<ONCE>((Glob<f4v> *)p, f4v{x[0], x[1], x[2], x[3]});
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -112,9 +158,22 @@ __device__ __forceinline__ void store4_f32(void *base, int i, int k, bool vec, c
     }
 }
 
-__device__ __forceinline__ uint32_t load4_bytes(const void *base, int i, int k, bool vec) {
+template <bool FAST, bool ONCE>
+__device__ __forceinline__ void store4_bf16(void *base, int i, int k, const uint32_t x[4]) {
+    Glob<uint16_t> *p = (Glob<uint16_t> *)base + i;
+    if (FAST) {
+        put<ONCE>((Glob<u2v> *)p, u2v{x[0] | x[1] << 16, x[2] | x[3] << 16});
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < k) p[j] = (uint16_t)x[j];
+    }
+}
+
+template <bool FAST, bool ONCE>
+__device__ __forceinline__ uint32_t load4_bytes(const void *base, int i, int k) {
     Glob<const uint8_t> *p = (Glob<const uint8_t> *)base + i;
-    if (vec && k == 4) return *(Glob<const uint32_t> *)p;
+    if (FAST) return get<ONCE>((Glob<const uint32_t> *)p);
     uint32_t x = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -122,10 +181,11 @@ __device__ __forceinline__ uint32_t load4_bytes(const void *base, int i, int k, 
     return x;
 }
 
-__device__ __forceinline__ void store4_bytes(void *base, int i, int k, bool vec, uint32_t x) {
+template <bool FAST, bool ONCE>
+__device__ __forceinline__ void store4_bytes(void *base, int i, int k, uint32_t x) {
     Glob<uint8_t> *p = (Glob<uint8_t> *)base + i;
-    if (vec && k == 4) {
-        *(Glob<uint32_t> *)p = x;
+    if (FAST) {
+        put<ONCE>((Glob<uint32_t> *)p, x);
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -158,161 +218,216 @@ __device__ __forceinline__ float scale_of(uint32_t byte) {
 }
 
 __device__ __forceinline__ void decode4(uint32_t codes, float scale, float x[4]) {
-    typedef float f2v __attribute__((ext_vector_type(2)));
-    const f2v a = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false);
-    const f2v b = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
-    x[0] = a.x * scale;
-    x[1] = a.y * scale;
-    x[2] = b.x * scale;
-    x[3] = b.y * scale;
+    const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, scale, false);
+    const auto b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, scale, true);
+    x[0] = a[0];
+    x[1] = a[1];
+    x[2] = b[0];
+    x[3] = b[1];
 }
 
-// The largest finite |x| of a block, as float32 bits: 8 lanes of 4 elements.
-__device__ __forceinline__ uint32_t block_top(const float x[4]) {
-    uint32_t top = 0;
+// Maximum over the 8 lanes that hold a block of 32.
+__device__ __forceinline__ uint32_t block_max(const uint32_t x[4]) {
+    uint32_t top = umax_(umax_(x[0], x[1]), umax_(x[2], x[3]));
+    top = umax_(top, dpp_u<0xB1>(top));         // lane ^ 1
+    top = umax_(top, dpp_u<0x4E>(top));         // lane ^ 2
+    return umax_(top, dpp_u<0x141>(top));       // 7 - lane, within 8
+}
+
+// The scale byte of a block: the smallest 2^e >= 2^-126 with |x| <= 448 2^e =
+// 1.75 2^(e + 8) for its finite values (8 lanes of 4 elements). Sizes are
+// compared as float32 bits; what is not finite, and rare, is taken out where
+// it is met. A mantissa above 1.75 carries into the exponent.
+__device__ __forceinline__ uint32_t block_scale(const float x[4]) {
+    uint32_t b[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = __builtin_bit_cast(uint32_t, x[j]) & 0x7FFFFFFFu;
+    uint32_t top = block_max(b);
+    if (top >= 0x7F800000u) {  // all 8 lanes or none
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b[j] = b[j] < 0x7F800000u ? b[j] : 0u;
+        top = block_max(b);
+    }
+    const int byte = (int)((top + 0x1FFFFFu) >> 23) - 8;
+    return (uint32_t)(byte > 1 ? byte : 1);
+}
+
+// Four numbers to E4M3 codes under a scale. The hardware's stochastic
+// rounding adds the upper 20 bits of the seed to the 20 bits below the last
+// place kept (denormals too), which with the seed k 2^16 + 2^15 is the
+// definition's rounding by (k + 1/2) / 2^16. What is not finite becomes NaN.
+template <bool HIGH>
+__device__ __forceinline__ uint32_t encode4_random(const float x[4], float scale, const uint32_t bits[4]) {
+    uint32_t seed[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) seed[j] = HIGH ? (bits[j] & 0xFFFF0000u) | 0x8000u : bits[j] << 16 | 0x8000u;
+    int c = __builtin_amdgcn_cvt_scalef32_sr_fp8_f32(0, x[0], seed[0], scale, 0);
+    c = __builtin_amdgcn_cvt_scalef32_sr_fp8_f32(c, x[1], seed[1], scale, 1);
+    c = __builtin_amdgcn_cvt_scalef32_sr_fp8_f32(c, x[2], seed[2], scale, 2);
+    return (uint32_t)__builtin_amdgcn_cvt_scalef32_sr_fp8_f32(c, x[3], seed[3], scale, 3);
+}
+
+// The same to the nearest, ties to even.
+__device__ __forceinline__ uint32_t encode4_nearest(const float x[4], float scale) {
+    typedef short s2v __attribute__((ext_vector_type(2)));
+    s2v c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(s2v{0, 0}, x[0], x[1], scale, false);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, x[2], x[3], scale, true);
+    return __builtin_bit_cast(uint32_t, c);
+}
+
+// s with every positive value at the grid's smallest, 2^-9 of the scale, or
+// above (NaN stays).
+__device__ __forceinline__ void keep_positive(float s[4], float scale) {
+    const float least = scale * 0x1p-9f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const uint32_t b = __builtin_bit_cast(uint32_t, x[j]) & 0x7FFFFFFFu;
-        top = umax_(top, b < 0x7F800000u ? b : 0u);
+        const float floor = s[j] == 0.0f ? 0.0f : least;
+        s[j] = s[j] < floor ? floor : s[j];
     }
-    top = umax_(top, dpp_u<0xB1>(top));   // lane ^ 1
-    top = umax_(top, dpp_u<0x4E>(top));   // lane ^ 2
-    top = umax_(top, dpp_u<0x141>(top));  // 7 - lane, within 8
-    return top;
 }
-
-// Scale byte of a block with this top: the smallest 2^e >= 2^-126 with
-// top <= 448 2^e = 1.75 2^(e + 8). A mantissa above 1.75 carries.
-__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
-    const int s = (int)((top + 0x1FFFFFu) >> 23) - 8;
-    return (uint32_t)(s > 1 ? s : 1);
-}
-
-// |x| to E4M3 under a scale. x 2^-e 2^-120 puts E4M3's exponent range on
-// float32's lowest exponents, denormals on denormals, so the code is the top
-// of the float32 bits with 20 bits below it, and `r` of those is added to
-// round (2^20 r is the odds of the next code). What is not finite gives 0x7F,
-// E4M3's NaN.
-__device__ __forceinline__ uint32_t encode1(float x, float inv, uint32_t r) {
-    const float y = __builtin_fabsf(x) * inv * 0x1p-120f;
-    const uint32_t c = (__builtin_bit_cast(uint32_t, y) + r) >> 20;
-    return c < 0x7Fu ? c : 0x7Fu;
-}
-
-__device__ __forceinline__ float inverse_scale(uint32_t byte) {
-    return __builtin_bit_cast(float, (254u - byte) << 23);
-}
-
-__device__ __forceinline__ uint32_t nearest_bits(float x, float inv) {
-    const uint32_t b = __builtin_bit_cast(uint32_t, __builtin_fabsf(x) * inv * 0x1p-120f);
-    return 0x7FFFFu + ((b >> 20) & 1u);
-}
-
-__device__ __forceinline__ uint32_t sign_bit8(float x) { return (__builtin_bit_cast(uint32_t, x) >> 24) & 0x80u; }
 
 // ---- AdamW ------------------------------------------------------------------
 
 struct StepConst {
     float b1, a1, b2, a2;  // beta and 1 - beta
     float eps, clip, rate, second, decay;
-    uint32_t key;
+    uint64_t t, seed;
 };
 
 // One element, its moments in float32; s = sqrt(v) is returned for the 8-bit
-// form.
+// form. The root and the reciprocal are the hardware's, good to an ulp: the
+// correctly rounded sequences would be half of the arithmetic, and p's own
+// rounding is far above them. The root takes denormals for 0, so they are
+// scaled first.
 __device__ __forceinline__ float adamw1(const StepConst &c, float g, float &p, float &m, float &v) {
     g = g * c.clip;
-    m = m * c.b1 + g * c.a1;
-    v = v * c.b2 + g * c.a2 * g;
-    const float s = sqrtf(v);
-    p = p - (c.rate * (m / (s * c.second + c.eps)) + c.decay * p);
+    m = fmaf_(m, c.b1, g * c.a1);
+    v = fmaf_(v, c.b2, g * c.a2 * g);
+    const bool tiny = v < 0x1p-126f;
+    float s = __builtin_amdgcn_sqrtf(tiny ? v * 0x1p64f : v);
+    s = tiny ? s * 0x1p-32f : s;
+    const float u = m * __builtin_amdgcn_rcpf(fmaf_(s, c.second, c.eps));
+    p = p - fmaf_(c.rate, u, c.decay * p);
     return s;
 }
 
-template <bool PB, bool GB, bool M8>
-__device__ __forceinline__ void step_item(const OptimItem &it, const StepConst &c) {
-    const bool vec = it.flags & kVectors;
-    for (int i = 4 * (int)threadIdx.x; i < it.count + 31; i += 4 * kBlock) {  // whole blocks of lanes
-        const int left = it.count - i;
-        const int k = left < 4 ? (left > 0 ? left : 0) : 4;
-        float p[4], g[4], m[4], v[4], s[4];
-        uint32_t bits[4];
-        load4<PB>(it.p, i, k, vec, p);
-        load4<GB>(it.g, i, k, vec, g);
-        if (M8) {
-            const uint32_t cm = load4_bytes(it.m, i, k, vec), cv = load4_bytes(it.v, i, k, vec);
-            const float sm = k > 0 ? scale_of(((Glob<const uint8_t> *)it.ms)[i >> 5]) : 0.0f;
-            const float sv = k > 0 ? scale_of(((Glob<const uint8_t> *)it.vs)[i >> 5]) : 0.0f;
-            decode4(cm, sm, m);
-            decode4(cv, sv, v);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = v[j] * v[j];
-        } else {
-            load4<false>(it.m, i, k, vec, m);
-            load4<false>(it.v, i, k, vec, v);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            s[j] = adamw1(c, g[j], p[j], m[j], v[j]);
-            if (M8 || PB) bits[j] = mix32(((uint32_t)it.base + (uint32_t)(i + j)) ^ c.key);
-        }
-        if (PB) {
-            uint32_t q[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) q[j] = to_bf16_random(p[j], (bits[j] * 0x9e3779b1u) >> 16);
-            Glob<uint16_t> *out = (Glob<uint16_t> *)it.p + i;
-            if (vec && k == 4) {
-                *(Glob<u2v> *)out = u2v{q[0] | q[1] << 16, q[2] | q[3] << 16};
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j < k) out[j] = (uint16_t)q[j];
-            }
-        } else {
-            store4_f32(it.p, i, k, vec, p);
-        }
-        if (M8) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (j >= k) m[j] = s[j] = 0.0f;  // no part in the block's scale
-            const uint32_t bm = scale_byte(block_top(m)), bs = scale_byte(block_top(s));
-            const float im = inverse_scale(bm), is = inverse_scale(bs);
-            uint32_t cm = 0, cs = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t a = encode1(m[j], im, (bits[j] & 0xFFFFu) * 16u + 8u);
-                const uint32_t b = encode1(s[j], is, (bits[j] >> 16) * 16u + 8u);
-                cm |= (a | sign_bit8(m[j])) << (8 * j);
-                cs |= (s[j] > 0.0f ? umax_(b, 1u) : b) << (8 * j);
-            }
-            if (k > 0) {
-                store4_bytes(it.m, i, k, vec, cm);
-                store4_bytes(it.v, i, k, vec, cs);
-                if ((threadIdx.x & 7) == 0) {
-                    ((Glob<uint8_t> *)it.ms)[i >> 5] = (uint8_t)bm;
-                    ((Glob<uint8_t> *)it.vs)[i >> 5] = (uint8_t)bs;
-                }
-            }
-        } else {
-            store4_f32(it.m, i, k, vec, m);
-            store4_f32(it.v, i, k, vec, v);
-        }
+// The part of an element's random bits that an item has in common.
+__device__ __forceinline__ uint32_t random_key(const OptimItem &it, const StepConst &c) {
+    uint32_t key = mix32(it.place + 0x9e3779b9u);
+    key = mix32(key ^ (uint32_t)c.t);
+    key = mix32(key ^ (uint32_t)(c.t >> 32));
+    key = mix32(key ^ (uint32_t)c.seed);
+    key = mix32(key ^ (uint32_t)(c.seed >> 32));
+    return mix32(key ^ (uint32_t)((uint64_t)it.base >> 32));
+}
+
+// A thread's four elements of a pass: in memory, m and v are four values or
+// four codes with the bytes of their block's scales.
+template <bool M8>
+struct Quad {
+    float p[4], g[4], m[4], v[4];
+    uint32_t cm, cv, sm, sv;
+};
+
+template <bool PB, bool GB, bool M8, bool FAST, bool ONCE>
+__device__ __forceinline__ void load_quad(const OptimItem &it, int i, int k, Quad<M8> &q) {
+    load4<PB, FAST, ONCE>(it.p, i, k, q.p);
+    load4<GB, FAST, ONCE>(it.g, i, k, q.g);
+    if (M8) {
+        q.cm = load4_bytes<FAST, ONCE>(it.m, i, k);
+        q.cv = load4_bytes<FAST, ONCE>(it.v, i, k);
+        q.sm = FAST || k > 0 ? ((Glob<const uint8_t> *)it.ms)[i >> 5] : 0u;
+        q.sv = FAST || k > 0 ? ((Glob<const uint8_t> *)it.vs)[i >> 5] : 0u;
+    } else {
+        load4<false, FAST, ONCE>(it.m, i, k, q.m);
+        load4<false, FAST, ONCE>(it.v, i, k, q.v);
     }
 }
 
+template <bool PB, bool M8, bool FAST, bool ONCE>
+__device__ __forceinline__ void step_quad(const OptimItem &it, const StepConst &c, int i, int k, Quad<M8> &q) {
+    float s[4];
+    uint32_t bits[4];
+    const uint32_t key = M8 || PB ? random_key(it, c) : 0u;
+    if (M8) {
+        decode4(q.cm, scale_of(q.sm), q.m);
+        decode4(q.cv, scale_of(q.sv), q.v);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q.v[j] = q.v[j] * q.v[j];
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        s[j] = adamw1(c, q.g[j], q.p[j], q.m[j], q.v[j]);
+        // i and the item's first element are multiples of 4
+        if (M8 || PB) bits[j] = mix32((((uint32_t)it.base + (uint32_t)i) ^ key) ^ (uint32_t)j);
+    }
+    if (PB) {
+        uint32_t b[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b[j] = to_bf16_random(q.p[j], (bits[j] * 0x9e3779b1u) >> 16);
+        store4_bf16<FAST, ONCE>(it.p, i, k, b);
+    } else {
+        store4_f32<FAST, ONCE>(it.p, i, k, q.p);
+    }
+    if (M8) {
+        if (!FAST) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j >= k) q.m[j] = s[j] = 0.0f;  // no part in the block's scale
+        }
+        const uint32_t bm = block_scale(q.m), bs = block_scale(s);
+        const float scm = scale_of(bm), scs = scale_of(bs);
+        keep_positive(s, scs);
+        const uint32_t cm = encode4_random<false>(q.m, scm, bits), cs = encode4_random<true>(s, scs, bits);
+        store4_bytes<FAST, ONCE>(it.m, i, k, cm);
+        store4_bytes<FAST, ONCE>(it.v, i, k, cs);
+        if ((threadIdx.x & 7) == 0 && (FAST || k > 0)) {
+            ((Glob<uint8_t> *)it.ms)[i >> 5] = (uint8_t)bm;
+            ((Glob<uint8_t> *)it.vs)[i >> 5] = (uint8_t)bs;
+        }
+    } else {
+        store4_f32<FAST, ONCE>(it.m, i, k, q.m);
+        store4_f32<FAST, ONCE>(it.v, i, k, q.v);
+    }
+}
+
+// An item is one pass of the workgroup. In a shorter last one the lanes past
+// the end stay: those of its last block take part in the block's maximum.
+template <bool PB, bool GB, bool M8, bool ONCE>
+__device__ __forceinline__ void step_item(const OptimItem &it, const StepConst &c) {
+    static_assert(kOptimChunk == 4 * kBlock, "an item is four elements a thread");
+    const int i = 4 * (int)threadIdx.x;
+    Quad<M8> q;
+    if (it.count == kOptimChunk && it.flags & kVectors) {
+        load_quad<PB, GB, M8, true, ONCE>(it, i, 4, q);
+        step_quad<PB, M8, true, ONCE>(it, c, i, 4, q);
+    } else {
+        const int left = it.count - i;
+        const int k = left < 4 ? (left > 0 ? left : 0) : 4;
+        load_quad<PB, GB, M8, false, false>(it, i, k, q);
+        step_quad<PB, M8, false, false>(it, c, i, k, q);
+    }
+}
+
+template <bool CONTROL, bool ONCE>
 __global__ __launch_bounds__(kBlock) void k_adamw(const OptimItem *items, StepArgs a, const gs_adamw_control *control) {
-    const OptimItem it = load_item(items, blockIdx.x);
+    OptimItem it = load_item(items, xcd_group<kXcdItems>(blockIdx.x, gridDim.x));
     StepConst c;
-    uint64_t t = a.step;
     float first = a.first;
     c.second = a.second;
     c.clip = 1.0f;
-    if (control) {
-        if (!control->apply) return;
-        t = (uint64_t)control->step;
-        first = control->first;
-        c.second = control->second;
-        c.clip = control->clip;
+    c.t = a.step;
+    c.seed = a.seed;
+    if (CONTROL) {
+        typedef __attribute__((address_space(4))) const gs_adamw_control ConstControl;
+        ConstControl *now = (ConstControl *)control;
+        // A skipped step has nothing to do; a return here would make the
+        // item's loads wait for the control's.
+        if (!now->apply) it.count = 0;
+        c.t = (uint64_t)now->step;
+        first = now->first;
+        c.second = now->second;
+        c.clip = now->clip;
     }
     c.b1 = a.b1;
     c.a1 = a.a1;
@@ -322,28 +437,39 @@ __global__ __launch_bounds__(kBlock) void k_adamw(const OptimItem *items, StepAr
     const float lr = it.lr * a.lr_scale;
     c.rate = lr * first;
     c.decay = lr * it.wd;
-    uint32_t key = mix32(it.place + 0x9e3779b9u);
-    key = mix32(key ^ (uint32_t)t);
-    key = mix32(key ^ (uint32_t)(t >> 32));
-    key = mix32(key ^ (uint32_t)a.seed);
-    key = mix32(key ^ (uint32_t)(a.seed >> 32));
-    c.key = mix32(key ^ (uint32_t)((uint64_t)it.base >> 32));
     switch (it.flags & (kParamBf16 | kGradBf16 | kMoments8)) {
-        case 0: step_item<false, false, false>(it, c); break;
-        case kGradBf16: step_item<false, true, false>(it, c); break;
-        case kParamBf16 | kGradBf16: step_item<true, true, false>(it, c); break;
-        case kMoments8: step_item<false, false, true>(it, c); break;
-        case kMoments8 | kGradBf16: step_item<false, true, true>(it, c); break;
-        case kMoments8 | kParamBf16 | kGradBf16: step_item<true, true, true>(it, c); break;
+        case 0: step_item<false, false, false, ONCE>(it, c); break;
+        case kGradBf16: step_item<false, true, false, ONCE>(it, c); break;
+        case kParamBf16 | kGradBf16: step_item<true, true, false, ONCE>(it, c); break;
+        case kMoments8: step_item<false, false, true, ONCE>(it, c); break;
+        case kMoments8 | kGradBf16: step_item<false, true, true, ONCE>(it, c); break;
+        case kMoments8 | kParamBf16 | kGradBf16: step_item<true, true, true, ONCE>(it, c); break;
         default: break;
     }
 }
 
 // ---- gradient norm ------------------------------------------------------------
 
+template <int CTRL>
+__device__ __forceinline__ double dpp_d(double x) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    return __builtin_bit_cast(double, (uint64_t)dpp_u<CTRL>((uint32_t)(b >> 32)) << 32 | dpp_u<CTRL>((uint32_t)b));
+}
+
+__device__ __forceinline__ double readlane_d(double x, int lane) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(b >> 32), lane);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)b, lane);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+// Sum over the workgroup, in every thread, in a fixed order.
 __device__ __forceinline__ double block_sum(double x, double *lds) {
-#pragma unroll
-    for (int o = kWave / 2; o > 0; o >>= 1) x += __shfl_xor(x, o, kWave);
+    x += dpp_d<0xB1>(x);
+    x += dpp_d<0x4E>(x);
+    x += dpp_d<0x124>(x);
+    x += dpp_d<0x128>(x);
+    x = (readlane_d(x, 0) + readlane_d(x, 16)) + (readlane_d(x, 32) + readlane_d(x, 48));
     if ((threadIdx.x & (kWave - 1)) == 0) lds[threadIdx.x / kWave] = x;
     __syncthreads();
     double r = 0.0;
@@ -352,29 +478,70 @@ __device__ __forceinline__ double block_sum(double x, double *lds) {
     return r;
 }
 
-template <bool BF16>
-__device__ __forceinline__ double item_squares(const OptimItem &it) {
-    double sum = 0.0;
-    for (int i = 4 * (int)threadIdx.x; i < it.count; i += 4 * kBlock) {
-        const int left = it.count - i;
-        float g[4];
-        load4<BF16>(it.g, i, left < 4 ? left : 4, it.flags & kVectors, g);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) sum = __builtin_fma((double)g[j], (double)g[j], sum);
-    }
-    return sum;
+// beta^t by squaring: its error, t 2^-53 of a number that falls as beta^t,
+// is far below float32's.
+__device__ __forceinline__ double power(double beta, uint64_t t) {
+    double r = 1.0;
+    for (; t; t >>= 1, beta *= beta)
+        if (t & 1) r *= beta;
+    return r;
 }
 
-__global__ __launch_bounds__(kBlock) void k_grad_norm(const OptimItem *items, uint32_t n_items, double *part,
-                                                      NormArgs a, gs_adamw_control *control) {
-    __shared__ double lds[2][kWavesPerBlock];
-    __shared__ uint32_t last;
-    double sum = 0.0;
-    for (uint32_t i = blockIdx.x; i < n_items; i += gridDim.x) {
-        const OptimItem it = load_item(items, i);
-        sum += it.flags & kGradBf16 ? item_squares<true>(it) : item_squares<false>(it);
+template <bool BF16, bool ONCE>
+__device__ __forceinline__ void add_squares(const void *g, int i, double sum[4]) {
+    const u4v q = get<ONCE>((Glob<const u4v> *)((const char *)g + (size_t)i * (BF16 ? 2 : 4)));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t w = q[j];
+        if (BF16) {
+            const double lo = (double)bf16_to_f32(w & 0xFFFFu);
+            const double hi = (double)__builtin_bit_cast(float, w & 0xFFFF0000u);
+            sum[j] = __builtin_fma(lo, lo, sum[j]);
+            sum[j] = __builtin_fma(hi, hi, sum[j]);
+        } else {
+            const double x = (double)__builtin_bit_cast(float, w);
+            sum[j] = __builtin_fma(x, x, sum[j]);
+        }
     }
-    sum = block_sum(sum, lds[0]);
+}
+
+template <bool BF16, bool ONCE>
+__device__ __forceinline__ void item_squares(const NormItem &it, double sum[4]) {
+    constexpr int kEach = BF16 ? 8 : 4, kPass = kEach * kBlock;
+    int i = kEach * (int)threadIdx.x;
+    if ((uintptr_t)it.g % 16 == 0) {
+#pragma unroll 4
+        for (const int end = it.count - kEach; i <= end; i += kPass) add_squares<BF16, ONCE>(it.g, i, sum);
+    }
+    for (; i < it.count; i += kPass) {
+        for (int j = i; j < i + kEach && j < it.count; ++j) {
+            const double x = BF16 ? (double)bf16_to_f32(((Glob<const uint16_t> *)it.g)[j])
+                                  : (double)((Glob<const float> *)it.g)[j];
+            sum[0] = __builtin_fma(x, x, sum[0]);
+        }
+    }
+}
+
+template <bool ONCE>
+__global__ __launch_bounds__(kBlock) void k_grad_norm(const NormItem *items, uint32_t n_items, double *part,
+                                                      NormArgs a, gs_adamw_control *control) {
+    __shared__ double lds[2][kWavesPerBlock], powers[2];
+    __shared__ uint32_t last;
+    double s4[4] = {0.0, 0.0, 0.0, 0.0};
+    for (uint32_t i = blockIdx.x; i < n_items; i += gridDim.x) {
+        const NormItem it = load_norm_item(items, i);
+        if (it.flags & kGradBf16)
+            item_squares<true, ONCE>(it, s4);
+        else
+            item_squares<false, ONCE>(it, s4);
+    }
+    // While the first wave's sum is on its way, the second one raises the
+    // betas to the coming step.
+    if (threadIdx.x == kWave || threadIdx.x == kWave + 1) {
+        const int j = (int)threadIdx.x - kWave;
+        powers[j] = power(j ? a.beta2 : a.beta1, (uint64_t)control->step + 1);
+    }
+    double sum = block_sum((s4[0] + s4[1]) + (s4[2] + s4[3]), lds[0]);
     if (threadIdx.x == 0) {
         __hip_atomic_store(&part[blockIdx.x], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         last = __hip_atomic_fetch_add(&control->arrived, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) ==
@@ -397,11 +564,10 @@ __global__ __launch_bounds__(kBlock) void k_grad_norm(const OptimItem *items, ui
         control->skipped += 1;
         return;
     }
-    const int64_t t = control->step + 1;
-    control->step = t;
+    control->step += 1;
     control->clip = norm > a.max_norm ? (float)(a.max_norm / norm) : 1.0f;
-    control->first = (float)(1.0 / (1.0 - pow(a.beta1, (double)t)));
-    control->second = (float)(1.0 / sqrt(1.0 - pow(a.beta2, (double)t)));
+    control->first = (float)(1.0 / (1.0 - powers[0]));
+    control->second = (float)(1.0 / sqrt(1.0 - powers[1]));
 }
 
 // ---- moments through a densification ------------------------------------------
@@ -435,27 +601,21 @@ __device__ __forceinline__ void carry_rows(const gs_adamw_rows &a, int64_t n_in,
     const int64_t left = total - e0;
     const int k = left < 4 ? (left > 0 ? (int)left : 0) : 4;
     if (M8) {
-        const uint32_t bm = scale_byte(block_top(m)), bs = scale_byte(block_top(v));
-        const float im = inverse_scale(bm), is = inverse_scale(bs);
-        uint32_t cm = 0, cs = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t p = encode1(m[j], im, nearest_bits(m[j], im));
-            const uint32_t q = encode1(v[j], is, nearest_bits(v[j], is));
-            cm |= (p | sign_bit8(m[j])) << (8 * j);
-            cs |= (v[j] > 0.0f ? umax_(q, 1u) : q) << (8 * j);
-        }
+        const uint32_t bm = block_scale(m), bs = block_scale(v);
+        const float scm = scale_of(bm), scs = scale_of(bs);
+        keep_positive(v, scs);
+        const uint32_t cm = encode4_nearest(m, scm), cs = encode4_nearest(v, scs);
         if (k > 0) {
-            store4_bytes((uint8_t *)a.m_out + e0, 0, k, false, cm);
-            store4_bytes((uint8_t *)a.v_out + e0, 0, k, false, cs);
+            store4_bytes<false, false>((uint8_t *)a.m_out + e0, 0, k, cm);
+            store4_bytes<false, false>((uint8_t *)a.v_out + e0, 0, k, cs);
             if ((threadIdx.x & 7) == 0) {
                 ((Glob<uint8_t> *)a.m_scale_out)[e0 >> 5] = (uint8_t)bm;
                 ((Glob<uint8_t> *)a.v_scale_out)[e0 >> 5] = (uint8_t)bs;
             }
         }
     } else {
-        store4_f32((float *)a.m_out + e0, 0, k, false, m);
-        store4_f32((float *)a.v_out + e0, 0, k, false, v);
+        store4_f32<false, false>((float *)a.m_out + e0, 0, k, m);
+        store4_f32<false, false>((float *)a.v_out + e0, 0, k, v);
     }
 }
 
@@ -478,20 +638,23 @@ __global__ __launch_bounds__(kBlock) void k_carry(CarryArgs a, const int32_t *so
 
 size_t optim_part_bytes() { return kNormBlocks * sizeof(double); }
 
-hipError_t launch_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, OptimItem *items, hipStream_t s) {
+hipError_t launch_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, int64_t elements, OptimItem *items,
+                             NormItem *norms, hipStream_t s) {
     FillArgs a;
-    uint64_t done = 0;
+    a.norm_chunk = (int)norm_chunk(elements);
+    uint64_t done = 0, done_norm = 0;
     int64_t i = 0;
     while (i < count) {
         a.count = 0;
-        uint64_t here = 0;
+        uint64_t here = 0, here_norm = 0;
         // A tensor's pieces stay in one launch; a launch takes tensors while
         // their pieces fit 31 bits.
         while (i < count && a.count < kFill) {
             const gs_adamw_tensor &t = tensors[i];
-            const uint64_t pieces = (uint64_t)optim_items(t.n);
+            const uint64_t pieces = t.param ? (uint64_t)optim_items(t.n) : 0;
+            const uint64_t norm_pieces = (uint64_t)norm_items(t.n, a.norm_chunk);
             if (a.count && here + pieces > 0x7FFFFFFFu) break;
-            if (pieces) {
+            if (norm_pieces) {
                 OptimTensor &o = a.t[a.count];
                 o.p = t.param;
                 o.g = t.grad;
@@ -504,39 +667,47 @@ hipError_t launch_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, Opti
                 o.flags = optim_flags(t);
                 o.lr = t.lr;
                 o.wd = t.weight_decay;
-                a.first[a.count++] = (uint32_t)here;
+                a.first[a.count] = (uint32_t)here;
+                a.first_norm[a.count++] = (uint32_t)here_norm;
                 here += pieces;
+                here_norm += norm_pieces;
             }
             ++i;
         }
         if (!a.count) break;
         a.first[a.count] = (uint32_t)here;
+        a.first_norm[a.count] = (uint32_t)here_norm;
+        const uint64_t most = here > here_norm ? here : here_norm;
         prof_begin("adamw_plan", s);
-        hipLaunchKernelGGL(k_fill_items, dim3((uint32_t)((here + kBlock - 1) / kBlock)), dim3(kBlock), 0, s, a,
-                           items + done);
+        hipLaunchKernelGGL(k_fill_items, dim3((uint32_t)((most + kBlock - 1) / kBlock)), dim3(kBlock), 0, s, a,
+                           items + done, norms + done_norm);
         prof_end("adamw_plan", s);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
         done += here;
+        done_norm += here_norm;
     }
     return hipSuccess;
 }
 
-hipError_t launch_grad_norm(const OptimItem *items, int64_t n_items, double *part, const NormArgs &a,
+hipError_t launch_grad_norm(const NormItem *items, int64_t n_items, bool once, double *part, const NormArgs &a,
                             gs_adamw_control *control, hipStream_t s) {
     const uint32_t blocks = (uint32_t)(n_items < 1 ? 1 : n_items < kNormBlocks ? n_items : kNormBlocks);
     prof_begin("grad_norm", s);
-    hipLaunchKernelGGL(k_grad_norm, dim3(blocks), dim3(kBlock), 0, s, items, (uint32_t)n_items, part, a, control);
+    const auto kernel = once ? k_grad_norm<true> : k_grad_norm<false>;
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kBlock), 0, s, items, (uint32_t)n_items, part, a, control);
     prof_end("grad_norm", s);
     return hipGetLastError();
 }
 
-hipError_t launch_adamw(const OptimItem *items, int64_t n_items, const StepArgs &a, const gs_adamw_control *control,
-                        hipStream_t s) {
+hipError_t launch_adamw(const OptimItem *items, int64_t n_items, bool once, const StepArgs &a,
+                        const gs_adamw_control *control, hipStream_t s) {
     for (int64_t i = 0; i < n_items; i += kMaxGrid) {
         const int64_t here = n_items - i < kMaxGrid ? n_items - i : kMaxGrid;
         prof_begin("adamw", s);
-        hipLaunchKernelGGL(k_adamw, dim3((uint32_t)here), dim3(kBlock), 0, s, items + i, a, control);
+        const auto kernel = control ? (once ? k_adamw<true, true> : k_adamw<true, false>)
+                                    : (once ? k_adamw<false, true> : k_adamw<false, false>);
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)here), dim3(kBlock), 0, s, items + i, a, control);
         prof_end("adamw", s);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;

@@ -100,7 +100,8 @@ class GsAdamwTensor(ctypes.Structure):
 
 class GsAdamwPlan(ctypes.Structure):
     _fields_ = [("work", ctypes.c_void_p), ("work_bytes", ctypes.c_size_t), ("n_items", ctypes.c_int64),
-                ("n_elements", ctypes.c_int64), ("count", ctypes.c_int32), ("updatable", ctypes.c_int32)]
+                ("n_norm_items", ctypes.c_int64), ("step_bytes", ctypes.c_int64), ("norm_bytes", ctypes.c_int64),
+                ("count", ctypes.c_int32), ("updatable", ctypes.c_int32)]
 
 
 class GsAdamwParams(ctypes.Structure):
@@ -802,7 +803,7 @@ class AdamPlan:
         if need == ctypes.c_size_t(-1).value:
             raise GsError(GS_ERR_INVALID_ARGUMENT, "malformed list of tensors")
         self.work = _alloc_bytes(need, device)
-        self.c = GsAdamwPlan(self.work.data_ptr(), int(self.work.numel()), -1, 0, 0, 0)
+        self.c = GsAdamwPlan(self.work.data_ptr(), int(self.work.numel()), -1, -1, 0, 0, 0, 0)
         _check(L.gs_plan_adamw(rows, len(self.tensors), ctypes.byref(self.c), _stream(stream)))
 
 

@@ -90,7 +90,7 @@ def tensor(**k):
 
 
 def plan(work=FAKE, work_bytes=1 << 20, n_items=4, updatable=1):
-    return gsq.GsAdamwPlan(work, work_bytes, n_items, 100, 1, updatable)
+    return gsq.GsAdamwPlan(work, work_bytes, n_items, 1, 100, 100, 1, updatable)
 
 
 def params(beta1=0.9, beta2=0.999, eps=1e-8, lr_scale=1.0, max_norm=1.0):
