@@ -101,8 +101,7 @@ typedef struct gs_adamw_control {
     float first;     /* 1 / (1 - beta1^t) */
     float second;    /* 1 / sqrt(1 - beta2^t) */
     uint32_t apply;  /* whether the last call opened a step */
-    uint32_t arrived; /* used within gs_grad_norm, 0 outside */
-    uint32_t reserved[6];
+    uint32_t reserved[7];
 } gs_adamw_control;
 
 /* Settings of a step. 0 <= beta < 1, eps >= 0, lr_scale >= 0 (a schedule's

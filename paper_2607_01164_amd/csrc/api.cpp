@@ -543,13 +543,14 @@ bool adamw_sizes(const gs_adamw_tensor *tensors, int64_t count, AdamwSizes *z) {
 struct AdamwPlanLayout {
     OptimItem *items;
     NormItem *norms;
-    double *part;
+    NormWork work;
     size_t bytes;
 };
 AdamwPlanLayout adamw_plan_layout(void *work, int64_t items, int64_t norms) {
     Carver c(work);
     AdamwPlanLayout l;
-    l.part = c.take<double>(optim_part_bytes() / sizeof(double));
+    l.work.part = c.take<double>(kNormBlocks);
+    l.work.count = c.take<uint32_t>(kNormCounters * kNormCounter);
     l.norms = c.take<NormItem>((size_t)norms);
     l.items = c.take<OptimItem>((size_t)items);
     l.bytes = c.off;
@@ -1111,7 +1112,7 @@ gs_status gs_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, gs_adamw_
     if (!plan->work || plan->work_bytes < l.bytes || !aligned(plan->work))
         return fail(GS_ERR_WORKSPACE, "gs_plan_adamw: plan needs %zu bytes, 256-byte aligned (got %zu)", l.bytes,
                     plan->work_bytes);
-    GS_TRY(launch_plan_adamw(tensors, count, z.elements, l.items, l.norms, stream), "gs_plan_adamw");
+    GS_TRY(launch_plan_adamw(tensors, count, z.elements, l.items, l.norms, l.work, stream), "gs_plan_adamw");
     plan->n_items = z.items;
     plan->n_norm_items = z.norm_items;
     plan->step_bytes = z.step_bytes;
@@ -1129,7 +1130,7 @@ gs_status gs_grad_norm(const gs_adamw_plan *plan, const gs_adamw_params *params,
     if (!control || (uintptr_t)control % 8)
         return fail(GS_ERR_INVALID_ARGUMENT, "gs_grad_norm: control is null or not 8-byte aligned");
     const AdamwPlanLayout l = adamw_plan_layout(plan->work, plan->n_items, plan->n_norm_items);
-    GS_TRY(launch_grad_norm(l.norms, plan->n_norm_items, plan->norm_bytes >= kOnceBytes, l.part,
+    GS_TRY(launch_grad_norm(l.norms, plan->n_norm_items, plan->norm_bytes >= kOnceBytes, l.work,
                             NormArgs{params->beta1, params->beta2, params->max_norm}, control, stream),
            "gs_grad_norm");
     return GS_OK;

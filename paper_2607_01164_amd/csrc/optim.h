@@ -44,6 +44,18 @@ struct alignas(16) NormItem {
     uint32_t flags;
 };
 
+// The norm's workspace: a partial sum for each workgroup, and counters of
+// those that are done, each in a line of its own: the root's, then one for
+// each group of workgroups.
+constexpr int kNormBlocks = 2048;  // workgroups at most
+constexpr uint32_t kNormGroup = 32;
+constexpr int kNormCounters = 1 + kNormBlocks / (int)kNormGroup;
+constexpr int kNormCounter = 32;  // words from one counter to the next
+struct NormWork {
+    double *part;
+    uint32_t *count;
+};
+
 struct StepArgs {
     float b1, a1, b2, a2, eps, lr_scale, first, second;
     uint64_t step, seed;
@@ -75,12 +87,11 @@ inline uint32_t optim_flags(const gs_adamw_tensor &t) {
     return f;
 }
 
-size_t optim_part_bytes();
 hipError_t launch_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, int64_t elements, OptimItem *items,
-                             NormItem *norms, hipStream_t s);
+                             NormItem *norms, const NormWork &work, hipStream_t s);
 // once: keep nothing in the caches
-hipError_t launch_grad_norm(const NormItem *items, int64_t n_items, bool once, double *part, const NormArgs &a,
-                            gs_adamw_control *control, hipStream_t s);
+hipError_t launch_grad_norm(const NormItem *items, int64_t n_items, bool once, const NormWork &work,
+                            const NormArgs &a, gs_adamw_control *control, hipStream_t s);
 hipError_t launch_adamw(const OptimItem *items, int64_t n_items, bool once, const StepArgs &a,
                         const gs_adamw_control *control, hipStream_t s);
 hipError_t launch_adamw_carry(const gs_adamw_rows *arrays, int count, int64_t n_in, const int32_t *source,

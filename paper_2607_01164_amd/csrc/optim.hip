@@ -21,7 +21,6 @@ typedef uint32_t u2v __attribute__((ext_vector_type(2)));
 constexpr int kFill = 24;         // tensors whose pieces one launch of k_fill_items writes
 constexpr uint32_t kXcdItems = 32;     // neighbouring items that one XCD takes
 constexpr int64_t kMaxGrid = 1 << 23;  // workgroups of a launch at most: 2^31 threads
-constexpr int kNormBlocks = 2048;      // workgroups of the norm at most: one partial sum each
 
 struct FillArgs {
     OptimTensor t[kFill];
@@ -522,8 +521,30 @@ __device__ __forceinline__ void item_squares(const NormItem &it, double sum[4]) 
     }
 }
 
+// Leaves a workgroup's sum and returns whether it is the last one to do so.
+// Only operations that are carried out at the device's point of coherence:
+// the exchange has its answer before the count is touched, so whoever reads
+// the full count finds every sum. (A release in its place writes back the
+// XCD's whole L2 for each workgroup, 170 ns one after the other.) Counts from
+// all XCDs to one word follow each other, so workgroups count in groups and
+// the last of each group in the root. Counters are 0 between launches.
+__device__ __forceinline__ bool leave_sum(const NormWork &work, double sum) {
+    const uint64_t old = __hip_atomic_exchange((uint64_t *)&work.part[blockIdx.x],
+                                               __builtin_bit_cast(uint64_t, sum), __ATOMIC_RELAXED,
+                                               __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("" ::"v"(old) : "memory");  // the answer is here
+    const uint32_t group = blockIdx.x / kNormGroup, groups = (gridDim.x + kNormGroup - 1) / kNormGroup;
+    const uint32_t here = group + 1 < groups ? kNormGroup : gridDim.x - group * kNormGroup;
+    uint32_t *mine = work.count + (group + 1) * kNormCounter;
+    if (__hip_atomic_fetch_add(mine, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != here - 1) return false;
+    __hip_atomic_store(mine, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (__hip_atomic_fetch_add(work.count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != groups - 1) return false;
+    __hip_atomic_store(work.count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return true;
+}
+
 template <bool ONCE>
-__global__ __launch_bounds__(kBlock) void k_grad_norm(const NormItem *items, uint32_t n_items, double *part,
+__global__ __launch_bounds__(kBlock) void k_grad_norm(const NormItem *items, uint32_t n_items, NormWork work,
                                                       NormArgs a, gs_adamw_control *control) {
     __shared__ double lds[2][kWavesPerBlock], powers[2];
     __shared__ uint32_t last;
@@ -542,21 +563,17 @@ __global__ __launch_bounds__(kBlock) void k_grad_norm(const NormItem *items, uin
         powers[j] = power(j ? a.beta2 : a.beta1, (uint64_t)control->step + 1);
     }
     double sum = block_sum((s4[0] + s4[1]) + (s4[2] + s4[3]), lds[0]);
-    if (threadIdx.x == 0) {
-        __hip_atomic_store(&part[blockIdx.x], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        last = __hip_atomic_fetch_add(&control->arrived, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) ==
-               gridDim.x - 1;
-    }
+    if (threadIdx.x == 0) last = leave_sum(work, sum);
     __syncthreads();
     if (!last) return;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
     // The last workgroup to arrive adds the partial sums, in their order.
     sum = 0.0;
     for (uint32_t i = threadIdx.x; i < gridDim.x; i += kBlock)
-        sum += __hip_atomic_load(&part[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        sum += __hip_atomic_load(&work.part[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     sum = block_sum(sum, lds[1]);
     if (threadIdx.x != 0) return;
     const double norm = sqrt(sum);
-    control->arrived = 0;
     control->norm = (float)norm;
     const bool finite = sum < __builtin_inf();
     control->apply = finite;
@@ -636,10 +653,10 @@ __global__ __launch_bounds__(kBlock) void k_carry(CarryArgs a, const int32_t *so
 
 // ---- host -----------------------------------------------------------------------
 
-size_t optim_part_bytes() { return kNormBlocks * sizeof(double); }
-
 hipError_t launch_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, int64_t elements, OptimItem *items,
-                             NormItem *norms, hipStream_t s) {
+                             NormItem *norms, const NormWork &work, hipStream_t s) {
+    const hipError_t e0 = fill_u32(work.count, 0u, kNormCounters * kNormCounter, s);
+    if (e0 != hipSuccess) return e0;
     FillArgs a;
     a.norm_chunk = (int)norm_chunk(elements);
     uint64_t done = 0, done_norm = 0;
@@ -690,12 +707,12 @@ hipError_t launch_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, int6
     return hipSuccess;
 }
 
-hipError_t launch_grad_norm(const NormItem *items, int64_t n_items, bool once, double *part, const NormArgs &a,
+hipError_t launch_grad_norm(const NormItem *items, int64_t n_items, bool once, const NormWork &work, const NormArgs &a,
                             gs_adamw_control *control, hipStream_t s) {
     const uint32_t blocks = (uint32_t)(n_items < 1 ? 1 : n_items < kNormBlocks ? n_items : kNormBlocks);
     prof_begin("grad_norm", s);
     const auto kernel = once ? k_grad_norm<true> : k_grad_norm<false>;
-    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kBlock), 0, s, items, (uint32_t)n_items, part, a, control);
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kBlock), 0, s, items, (uint32_t)n_items, work, a, control);
     prof_end("grad_norm", s);
     return hipGetLastError();
 }
