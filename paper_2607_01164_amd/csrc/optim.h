@@ -8,7 +8,7 @@
 namespace gs {
 
 constexpr int64_t kOptimChunk = 1024;  // elements of an item at most: a multiple of 32 that divides 2^32
-constexpr int64_t kCarryChunk = 1024;  // output elements of a workgroup of the carry
+constexpr uint32_t kCarryMost = 4096;  // elements of a workgroup's rows in the carry at most
 
 // Flags of a tensor and its items.
 constexpr uint32_t kParamBf16 = 1, kGradBf16 = 2, kMoments8 = 4;
@@ -63,10 +63,30 @@ struct StepArgs {
 struct NormArgs {
     double beta1, beta2, max_norm;
 };
+struct CarryArray {
+    const void *m, *v;
+    const uint8_t *m_scale, *v_scale;
+    void *m_out, *v_out;
+    uint8_t *m_scale_out, *v_scale_out;
+    // rows: of a workgroup, a multiple of 32. over, over_parts: x / d = x over
+    // >> 20 with over = 2^20 / d, up, for d = width and the (width + 3) / 4
+    // parts of a row (x below 2^14 times over's excess, below d <= 64, stays
+    // below 2^20).
+    uint32_t width, rows, over, over_parts;
+    uint32_t moments8, vectors;
+};
+// 8-bit rows: 4 parts of a row a thread, which are 3072 elements for rows of
+// three (one part a thread took twice as long); 32-bit rows: one pass of 4
+// elements a thread.
+inline uint32_t carry_rows(uint32_t width, bool moments8) {
+    const uint32_t most = moments8 ? (width < 4 ? 1024 * width : kCarryMost) : 1024;
+    const uint32_t rows = most / width / 32 * 32;
+    return rows ? rows : 32;
+}
 struct CarryArgs {
-    gs_adamw_rows rows[GS_ADAMW_ROWS_MAX];
-    uint32_t first[GS_ADAMW_ROWS_MAX + 1];  // first workgroup of each array
-    uint32_t block0;                        // the launch's first workgroup
+    CarryArray rows[GS_ADAMW_ROWS_MAX];
+    uint32_t first[GS_ADAMW_ROWS_MAX];  // first workgroup of each array, 2^32 - 1 past the last
+    uint32_t block0;                    // the launch's first workgroup
     int64_t n_in, n_out;
 };
 

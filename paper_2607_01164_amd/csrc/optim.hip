@@ -211,10 +211,9 @@ __device__ __forceinline__ uint32_t to_bf16_random(float x, uint32_t r16) {
 
 // ---- MXFP8 ------------------------------------------------------------------
 
-// 2^e of a scale byte (byte 0 is 2^-127, a float32 denormal).
-__device__ __forceinline__ float scale_of(uint32_t byte) {
-    return __builtin_bit_cast(float, umax_(byte << 23, 0x400000u));
-}
+// 2^e of a scale byte as the conversions take it: they use the exponent's 8
+// bits alone, whatever the others are, and read 0 as 2^-127.
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
 
 __device__ __forceinline__ void decode4(uint32_t codes, float scale, float x[4]) {
     const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, scale, false);
@@ -589,64 +588,201 @@ __global__ __launch_bounds__(kBlock) void k_grad_norm(const NormItem *items, uin
 
 // ---- moments through a densification ------------------------------------------
 
-template <bool M8>
-__device__ __forceinline__ void carry_rows(const gs_adamw_rows &a, int64_t n_in, Glob<const int32_t> *source,
-                                           int64_t total, int64_t base) {
-    const int64_t row0 = base / a.width;
-    const uint32_t col0 = (uint32_t)(base - row0 * a.width);
-    const int64_t e0 = base + 4 * (int)threadIdx.x;
-    float m[4], v[4];
+// 32-bit moments: neighbouring lanes take neighbouring elements, since rows
+// of 1, 3 or 4 elements that keep their order lie side by side but on no
+// vector's boundary. Every lane gets an address inside the arrays, so that no
+// load waits on a branch: elements past the end take the last one's, new rows
+// row 0's (there is one: n_in > 0). The scheduler may not put the first use
+// of a source before the last of their loads: it did, and each load waited
+// alone.
+__device__ __forceinline__ void carry_f32(const CarryArray &a, uint32_t n_in, Glob<const int32_t> *source, int64_t base,
+                                          int count) {
+    constexpr int kEach = 4;
+    for (int i = (int)threadIdx.x; i < count; i += kEach * kBlock) {
+        float m[kEach], v[kEach];
+        if (n_in) {
+            uint32_t col[kEach], src[kEach];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        m[j] = v[j] = 0.0f;
-        if (e0 + j >= total) continue;
-        const uint32_t x = col0 + 4 * threadIdx.x + j, q = x / (uint32_t)a.width;
-        const int64_t src = source[row0 + q];
-        if (src < 0 || src >= n_in) continue;
-        const int64_t at = src * a.width + (x - q * (uint32_t)a.width);
-        if (M8) {
-            float t[4];
-            decode4(((Glob<const uint8_t> *)a.m)[at], scale_of(((Glob<const uint8_t> *)a.m_scale)[at >> 5]), t);
-            m[j] = t[0];
-            decode4(((Glob<const uint8_t> *)a.v)[at], scale_of(((Glob<const uint8_t> *)a.v_scale)[at >> 5]), t);
-            v[j] = t[0];
+            for (int j = 0; j < kEach; ++j) {
+                const uint32_t e = i + j * kBlock < count ? i + j * kBlock : count - 1;
+                const uint32_t q = __umul24(e, a.over) >> 20;  // e / width
+                col[j] = e - __umul24(q, a.width);
+                src[j] = (uint32_t)source[q];  // negative: past n_in
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                const uint64_t at = (uint64_t)(src[j] < n_in ? src[j] : 0u) * a.width + col[j];
+                m[j] = ((Glob<const float> *)a.m)[at];
+                v[j] = ((Glob<const float> *)a.v)[at];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                m[j] = src[j] < n_in ? m[j] : 0.0f;
+                v[j] = src[j] < n_in ? v[j] : 0.0f;
+            }
         } else {
-            m[j] = ((Glob<const float> *)a.m)[at];
-            v[j] = ((Glob<const float> *)a.v)[at];
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) m[j] = v[j] = 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int e = i + j * kBlock;
+            if (e < count) {
+                ((Glob<float> *)a.m_out)[base + e] = m[j];
+                ((Glob<float> *)a.v_out)[base + e] = v[j];
+            }
         }
     }
-    const int64_t left = total - e0;
-    const int k = left < 4 ? (left > 0 ? (int)left : 0) : 4;
-    if (M8) {
+}
+
+// Four bytes of an array of n from byte `at` on, as far as they are there.
+// ANY: the array may be shorter than four.
+template <bool ANY, typename U>
+__device__ __forceinline__ uint32_t four_bytes(const void *base, U at, U n) {
+    typedef uint32_t word __attribute__((aligned(1)));
+    Glob<const uint8_t> *p = (Glob<const uint8_t> *)base;
+    if (!ANY || n >= 4) {
+        const U b = at < n - 4 ? at : n - 4;
+        return *(Glob<const word> *)(p + b) >> (8 * (uint32_t)(at - b));
+    }
+    uint32_t x = 0;
+    for (int j = 0; j < 3; ++j)
+        if (at + j < n) x |= (uint32_t)p[at + j] << (8 * j);
+    return x;
+}
+
+// The scale bytes of block i (the low one) and of the next, of n.
+template <bool ANY, typename U>
+__device__ __forceinline__ uint32_t two_scales(const uint8_t *base, U i, U n) {
+    typedef uint16_t half __attribute__((aligned(1)));
+    Glob<const uint8_t> *p = (Glob<const uint8_t> *)base;
+    if (ANY && n < 2) return p[0];
+    const U b = i < n - 2 ? i : n - 2;
+    return (uint32_t)(*(Glob<const half> *)(p + b)) >> (8 * (uint32_t)(i - b));
+}
+
+// Rows of 8-bit moments into LDS, a word for each element: m's code and scale
+// byte, then v's; zeros for new Gaussians. A thread takes up to four elements
+// of a row at a time, with one unaligned word of codes and one pair of scales
+// a moment, and four such parts at once: single bytes would be four loads an
+// element, which keeps the address units busy, and one part at a time leaves
+// too little in flight. WHOLE: a row is one part.
+template <bool WHOLE, bool ANY, typename U>
+__device__ __forceinline__ void rows_to_lds(const CarryArray &a, uint32_t n_in, Glob<const int32_t> *source,
+                                            uint32_t rows, uint32_t *lds) {
+    constexpr int kEach = 4;
+    const U n = (U)n_in * a.width, scales = (n + 31) >> 5;
+    const uint32_t parts = WHOLE ? 1u : (a.width + 3) >> 2, all = rows * parts;
+    for (uint32_t p0 = threadIdx.x; p0 < all; p0 += kEach * kBlock) {
+        uint32_t row[kEach], col[kEach], src[kEach], cm[kEach], cv[kEach], sm[kEach], sv[kEach], place[kEach];
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const uint32_t p = p0 + j * kBlock < all ? p0 + j * kBlock : all - 1;  // the last one several times
+            row[j] = WHOLE ? p : __umul24(p, a.over_parts) >> 20;
+            col[j] = WHOLE ? 0u : 4 * (p - __umul24(row[j], parts));
+            src[j] = (uint32_t)source[row[j]];  // negative: past n_in
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const U at = (U)(src[j] < n_in ? src[j] : 0u) * a.width + col[j];
+            place[j] = (uint32_t)at & 31u;
+            cm[j] = four_bytes<ANY>(a.m, at, n);
+            cv[j] = four_bytes<ANY>(a.v, at, n);
+            sm[j] = two_scales<ANY>(a.m_scale, (U)(at >> 5), scales);
+            sv[j] = two_scales<ANY>(a.v_scale, (U)(at >> 5), scales);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const bool live = src[j] < n_in;
+            // bytes 1 and 3 of a word: the scales of this block, of the next
+            const uint32_t first = __builtin_amdgcn_perm(sv[j], sm[j], 0x040C000Cu);
+            const uint32_t next = __builtin_amdgcn_perm(sv[j], sm[j], 0x050C010Cu);
+            uint32_t *out = lds + __umul24(row[j], a.width) + col[j];
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                if (i >= (WHOLE ? a.width : a.width - col[j])) break;
+                // bytes 0 and 2: byte i of cm and of cv
+                const uint32_t codes = __builtin_amdgcn_perm(cv[j], cm[j], 0x0C040C00u + i * 0x00010001u);
+                const uint32_t word = codes | (place[j] + i > 31u ? next : first);
+                out[i] = live ? word : 0u;
+            }
+        }
+    }
+}
+
+// 8-bit moments: whole rows, a multiple of 32 of them, go through LDS and are
+// taken from there as the step takes its elements, four a lane and a block in
+// 8 lanes.
+__device__ __forceinline__ void carry_mxfp8(const CarryArray &a, uint32_t n_in, Glob<const int32_t> *source,
+                                            uint32_t rows, int64_t base, uint32_t *lds) {
+    const int count = (int)(rows * a.width);
+    if (n_in == 0) {
+        for (int i = (int)threadIdx.x; i < count; i += kBlock) lds[i] = 0u;
+    } else if (n_in < 64 || (uint64_t)n_in * a.width >= 0xFFFFFFFFu) {
+        rows_to_lds<false, true, uint64_t>(a, n_in, source, rows, lds);
+    } else if (a.width <= 4) {
+        rows_to_lds<true, false, uint32_t>(a, n_in, source, rows, lds);
+    } else {
+        rows_to_lds<false, false, uint32_t>(a, n_in, source, rows, lds);
+    }
+    __syncthreads();
+    uint8_t *m_out = (uint8_t *)a.m_out + base, *v_out = (uint8_t *)a.v_out + base;
+    for (int i = 4 * (int)threadIdx.x; i < count + 31; i += 4 * kBlock) {  // whole blocks of lanes, as in the step
+        const int left = count - i;
+        const int k = left < 4 ? (left > 0 ? left : 0) : 4;
+        uint32_t w[4];
+        if (k == 4) {
+            const u4v q = *(const u4v *)(lds + i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = q[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = j < k ? lds[i + j] : 0u;
+        }
+        float m[4], v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            // scales in bits 30 .. 23
+            m[j] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[j], __builtin_bit_cast(float, w[j] << 15), false)[0];
+            v[j] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[j], __builtin_bit_cast(float, w[j] >> 1), true)[0];
+        }
         const uint32_t bm = block_scale(m), bs = block_scale(v);
         const float scm = scale_of(bm), scs = scale_of(bs);
         keep_positive(v, scs);
-        const uint32_t cm = encode4_nearest(m, scm), cs = encode4_nearest(v, scs);
-        if (k > 0) {
-            store4_bytes<false, false>((uint8_t *)a.m_out + e0, 0, k, cm);
-            store4_bytes<false, false>((uint8_t *)a.v_out + e0, 0, k, cs);
-            if ((threadIdx.x & 7) == 0) {
-                ((Glob<uint8_t> *)a.m_scale_out)[e0 >> 5] = (uint8_t)bm;
-                ((Glob<uint8_t> *)a.v_scale_out)[e0 >> 5] = (uint8_t)bs;
-            }
+        const uint32_t om = encode4_nearest(m, scm), os = encode4_nearest(v, scs);
+        if (k == 4 && a.vectors) {
+            store4_bytes<true, false>(m_out, i, 4, om);
+            store4_bytes<true, false>(v_out, i, 4, os);
+        } else {
+            store4_bytes<false, false>(m_out, i, k, om);
+            store4_bytes<false, false>(v_out, i, k, os);
         }
-    } else {
-        store4_f32<false, false>((float *)a.m_out + e0, 0, k, m);
-        store4_f32<false, false>((float *)a.v_out + e0, 0, k, v);
+        if ((threadIdx.x & 7) == 0 && k > 0) {
+            ((Glob<uint8_t> *)a.m_scale_out)[(base + i) >> 5] = (uint8_t)bm;
+            ((Glob<uint8_t> *)a.v_scale_out)[(base + i) >> 5] = (uint8_t)bs;
+        }
     }
 }
 
 __global__ __launch_bounds__(kBlock) void k_carry(CarryArgs a, const int32_t *source) {
-    const uint32_t block = a.block0 + blockIdx.x;
+    __shared__ alignas(16) uint32_t lds[kCarryMost];
+    const uint32_t block = a.block0 + xcd_group<kXcdItems>(blockIdx.x, gridDim.x);
     int k = 0;
-    while (block >= a.first[k + 1]) ++k;
-    const gs_adamw_rows r = a.rows[k];
-    const int64_t base = (int64_t)(block - a.first[k]) * kCarryChunk;
-    const int64_t total = a.n_out * r.width;
-    if (r.moments == GS_MOMENTS_MXFP8)
-        carry_rows<true>(r, a.n_in, (Glob<const int32_t> *)source, total, base);
+#pragma unroll
+    for (int j = 1; j < GS_ADAMW_ROWS_MAX; ++j) k = block >= a.first[j] ? j : k;
+    const CarryArray r = a.rows[k];
+    const int64_t row0 = (int64_t)(block - a.first[k]) * r.rows, left = a.n_out - row0;
+    const uint32_t rows = left < r.rows ? (uint32_t)left : r.rows;
+    const int64_t base = row0 * r.width;
+    Glob<const int32_t> *from = (Glob<const int32_t> *)source + row0;
+    if (r.moments8)
+        carry_mxfp8(r, (uint32_t)a.n_in, from, rows, base, lds);
     else
-        carry_rows<false>(r, a.n_in, (Glob<const int32_t> *)source, total, base);
+        carry_f32(r, (uint32_t)a.n_in, from, base, (int)(rows * r.width));
 }
 
 }  // namespace
@@ -738,12 +874,28 @@ hipError_t launch_adamw_carry(const gs_adamw_rows *arrays, int count, int64_t n_
     a.n_in = n_in;
     a.n_out = n_out;
     uint32_t blocks = 0;
-    for (int k = 0; k < count; ++k) {
-        a.rows[k] = arrays[k];
-        a.first[k] = blocks;
-        blocks += (uint32_t)((n_out * arrays[k].width + kCarryChunk - 1) / kCarryChunk);
+    for (int k = 0; k < GS_ADAMW_ROWS_MAX; ++k) {
+        a.first[k] = k < count ? blocks : 0xFFFFFFFFu;
+        CarryArray &o = a.rows[k];
+        o = CarryArray();
+        if (k >= count) continue;
+        const gs_adamw_rows &r = arrays[k];
+        o.m = r.m;
+        o.v = r.v;
+        o.m_scale = r.m_scale;
+        o.v_scale = r.v_scale;
+        o.m_out = r.m_out;
+        o.v_out = r.v_out;
+        o.m_scale_out = r.m_scale_out;
+        o.v_scale_out = r.v_scale_out;
+        o.width = (uint32_t)r.width;
+        o.over = ((1u << 20) + o.width - 1) / o.width;
+        o.over_parts = ((1u << 20) + (o.width + 3) / 4 - 1) / ((o.width + 3) / 4);
+        o.rows = carry_rows(o.width, r.moments == GS_MOMENTS_MXFP8);
+        o.moments8 = r.moments == GS_MOMENTS_MXFP8;
+        o.vectors = !(((uintptr_t)r.m_out | (uintptr_t)r.v_out) & 3);
+        blocks += (uint32_t)((n_out + o.rows - 1) / o.rows);
     }
-    a.first[count] = blocks;
     for (uint32_t b = 0; b < blocks; b += (uint32_t)kMaxGrid) {
         const uint32_t here = blocks - b < (uint32_t)kMaxGrid ? blocks - b : (uint32_t)kMaxGrid;
         a.block0 = b;
