@@ -537,6 +537,7 @@ __device__ __forceinline__ bool leave_sum(const NormWork &work, double sum) {
     uint32_t *mine = work.count + (group + 1) * kNormCounter;
     if (__hip_atomic_fetch_add(mine, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != here - 1) return false;
     __hip_atomic_store(mine, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (groups == 1) return true;
     if (__hip_atomic_fetch_add(work.count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != groups - 1) return false;
     __hip_atomic_store(work.count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     return true;
@@ -545,7 +546,9 @@ __device__ __forceinline__ bool leave_sum(const NormWork &work, double sum) {
 template <bool ONCE>
 __global__ __launch_bounds__(kBlock) void k_grad_norm(const NormItem *items, uint32_t n_items, NormWork work,
                                                       NormArgs a, gs_adamw_control *control) {
-    __shared__ double lds[2][kWavesPerBlock], powers[2];
+    __shared__ double lds[2][kWavesPerBlock];
+    __shared__ uint64_t coming;
+    __shared__ float corrections[2];
     __shared__ uint32_t last;
     double s4[4] = {0.0, 0.0, 0.0, 0.0};
     for (uint32_t i = blockIdx.x; i < n_items; i += gridDim.x) {
@@ -555,12 +558,14 @@ __global__ __launch_bounds__(kBlock) void k_grad_norm(const NormItem *items, uin
         else
             item_squares<false, ONCE>(it, s4);
     }
-    // While the first wave's sum is on its way, the second one raises the
-    // betas to the coming step.
-    if (threadIdx.x == kWave || threadIdx.x == kWave + 1) {
-        const int j = (int)threadIdx.x - kWave;
-        powers[j] = power(j ? a.beta2 : a.beta1, (uint64_t)control->step + 1);
+    // Off the way of the sums, the last wave forms what the coming step needs
+    // if it is opened.
+    if (threadIdx.x == kBlock - 1) {
+        coming = (uint64_t)control->step + 1;
+        corrections[0] = (float)(1.0 / (1.0 - power(a.beta1, coming)));
     }
+    if (threadIdx.x == kBlock - 2)
+        corrections[1] = (float)(1.0 / sqrt(1.0 - power(a.beta2, (uint64_t)control->step + 1)));
     double sum = block_sum((s4[0] + s4[1]) + (s4[2] + s4[3]), lds[0]);
     if (threadIdx.x == 0) last = leave_sum(work, sum);
     __syncthreads();
@@ -580,10 +585,10 @@ __global__ __launch_bounds__(kBlock) void k_grad_norm(const NormItem *items, uin
         control->skipped += 1;
         return;
     }
-    control->step += 1;
+    control->step = (int64_t)coming;
     control->clip = norm > a.max_norm ? (float)(a.max_norm / norm) : 1.0f;
-    control->first = (float)(1.0 / (1.0 - powers[0]));
-    control->second = (float)(1.0 / sqrt(1.0 - powers[1]));
+    control->first = corrections[0];
+    control->second = corrections[1];
 }
 
 // ---- moments through a densification ------------------------------------------
