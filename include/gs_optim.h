@@ -63,9 +63,8 @@ enum { GS_MOMENTS_F32 = 0, GS_MOMENTS_MXFP8 = 1 };
  * float32 or bfloat16 gradients, or bfloat16 with bfloat16 gradients; the
  * types and moments may differ between the tensors of a list. m and v are
  * float32 arrays [n], or byte arrays [n] with scales [(n + 31) / 32] for
- * MXFP8 moments. Any element alignment; arrays on 16-byte boundaries (8 for
- * bfloat16, 4 for bytes) are faster. param may be null for a tensor that
- * only counts for gs_grad_norm. Arrays do not overlap. */
+ * MXFP8 moments. Arrays may start at any element. param may be null for a
+ * tensor that only counts for gs_grad_norm. Arrays do not overlap. */
 typedef struct gs_adamw_tensor {
     void *param;
     const void *grad;
@@ -104,7 +103,8 @@ typedef struct gs_adamw_control {
     uint32_t reserved[7];
 } gs_adamw_control;
 
-/* Settings of a step. 0 <= beta < 1, eps >= 0, lr_scale >= 0 (a schedule's
+/* Settings of a step. 0 <= beta < 1, eps >= 2^-126 (an element that never
+ * had a gradient is divided by it), lr_scale >= 0 (a schedule's
  * factor on every tensor's learning rate), max_norm > 0 (infinity: no
  * clipping), all but max_norm finite. */
 typedef struct gs_adamw_params {

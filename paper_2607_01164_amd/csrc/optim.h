@@ -12,7 +12,6 @@ constexpr uint32_t kCarryMost = 4096;  // elements of a workgroup's rows in the 
 
 // Flags of a tensor and its items.
 constexpr uint32_t kParamBf16 = 1, kGradBf16 = 2, kMoments8 = 4;
-constexpr uint32_t kVectors = 8;  // every array allows loads of four elements
 
 struct OptimTensor {
     void *p;
@@ -73,7 +72,7 @@ struct CarryArray {
     // parts of a row (x below 2^14 times over's excess, below d <= 64, stays
     // below 2^20).
     uint32_t width, rows, over, over_parts;
-    uint32_t moments8, vectors;
+    uint32_t moments8, pad;
 };
 // 8-bit rows: 4 parts of a row a thread, which are 3072 elements for rows of
 // three (one part a thread took twice as long); 32-bit rows: one pass of 4
@@ -96,14 +95,9 @@ inline int64_t norm_items(int64_t n, int64_t chunk) { return (n + chunk - 1) / c
 inline int64_t optim_items(int64_t n) { return (n + kOptimChunk - 1) / kOptimChunk; }
 inline uint32_t optim_flags(const gs_adamw_tensor &t) {
     uint32_t f = 0;
-    const bool pb = t.param_type == GS_TYPE_BF16, gb = t.grad_type == GS_TYPE_BF16;
-    const bool m8 = t.moments == GS_MOMENTS_MXFP8;
-    if (pb) f |= kParamBf16;
-    if (gb) f |= kGradBf16;
-    if (m8) f |= kMoments8;
-    const uintptr_t pm = pb ? 7 : 15, gm = gb ? 7 : 15, mm = m8 ? 3 : 15;
-    if (!((uintptr_t)t.param & pm) && !((uintptr_t)t.grad & gm) && !(((uintptr_t)t.m | (uintptr_t)t.v) & mm))
-        f |= kVectors;
+    if (t.param_type == GS_TYPE_BF16) f |= kParamBf16;
+    if (t.grad_type == GS_TYPE_BF16) f |= kGradBf16;
+    if (t.moments == GS_MOMENTS_MXFP8) f |= kMoments8;
     return f;
 }
 

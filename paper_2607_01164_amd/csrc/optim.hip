@@ -17,6 +17,13 @@ template <typename T>
 using Glob = __attribute__((address_space(1))) T;  // global, not generic, addresses
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u2v __attribute__((ext_vector_type(2)));
+// Vectors at any address that their elements may have: global loads and
+// stores need no more.
+typedef f4v f4a __attribute__((aligned(4)));
+typedef u4v u4a __attribute__((aligned(2)));
+typedef u2v u2a __attribute__((aligned(2)));
+typedef uint32_t u1a __attribute__((aligned(1)));
+typedef uint16_t h1a __attribute__((aligned(1)));
 
 constexpr int kFill = 24;         // tensors whose pieces one launch of k_fill_items writes
 constexpr uint32_t kXcdItems = 32;     // neighbouring items that one XCD takes
@@ -104,26 +111,35 @@ __device__ __forceinline__ NormItem load_norm_item(const NormItem *items, uint32
 __device__ __forceinline__ float bf16_to_f32(uint32_t b) { return __builtin_bit_cast(float, b << 16); }
 
 // Loads and stores that keep nothing in the caches (ONCE), or ordinary ones.
-template <bool ONCE, typename T>
-__device__ __forceinline__ T get(Glob<const T> *p) {
-    return ONCE ? __builtin_nontemporal_load(p) : *p;
-}
-template <bool ONCE, typename T>
-__device__ __forceinline__ void put(Glob<T> *p, T x) {
-    if (ONCE)
-        __builtin_nontemporal_store(x, p);
-    else
-        *p = x;
-}
+// (A template over the vector would drop its alignment.)
+#define GS_OPTIM_ACCESS(NAME, VALUE, UNALIGNED)                                         \
+    template <bool ONCE>                                                                \
+    __device__ __forceinline__ VALUE get_##NAME(const void *base, size_t byte) {        \
+        Glob<const UNALIGNED> *p = (Glob<const UNALIGNED> *)((const char *)base + byte); \
+        return ONCE ? __builtin_nontemporal_load(p) : *p;                               \
+    }                                                                                   \
+    template <bool ONCE>                                                                \
+    __device__ __forceinline__ void put_##NAME(void *base, size_t byte, VALUE x) {      \
+        Glob<UNALIGNED> *p = (Glob<UNALIGNED> *)((char *)base + byte);                  \
+        if (ONCE)                                                                       \
+            __builtin_nontemporal_store(x, p);                                          \
+        else                                                                            \
+            *p = x;                                                                     \
+    }
+GS_OPTIM_ACCESS(f4, f4v, f4a)
+GS_OPTIM_ACCESS(u4, u4v, u4a)
+GS_OPTIM_ACCESS(u2, u2v, u2a)
+GS_OPTIM_ACCESS(u1, uint32_t, u1a)
+#undef GS_OPTIM_ACCESS
 
-// Four consecutive elements as float32. FAST: all there, on a vector's
-// boundary. Otherwise the first k, one by one, and zeros.
+// Four consecutive elements as float32. FAST: all there. Otherwise the first
+// k, one by one, and zeros.
 template <bool BF16, bool FAST, bool ONCE>
 __device__ __forceinline__ void load4(const void *base, int i, int k, float x[4]) {
     if (BF16) {
         Glob<const uint16_t> *p = (Glob<const uint16_t> *)base + i;
         if (FAST) {
-            const u2v q = get<ONCE>((Glob<const u2v> *)p);
+            const u2v q = get_u2<ONCE>(base, 2 * (size_t)i);
             x[0] = bf16_to_f32(q.x & 0xFFFFu);
             x[1] = bf16_to_f32(q.x >> 16);
             x[2] = bf16_to_f32(q.y & 0xFFFFu);
@@ -135,7 +151,7 @@ __device__ __forceinline__ void load4(const void *base, int i, int k, float x[4]
     } else {
         Glob<const float> *p = (Glob<const float> *)base + i;
         if (FAST) {
-            const f4v q = get<ONCE>((Glob<const f4v> *)p);
+            const f4v q = get_f4<ONCE>(base, 4 * (size_t)i);
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[j] = q[j];
         } else {
@@ -149,7 +165,7 @@ template <bool FAST, bool ONCE>
 __device__ __forceinline__ void store4_f32(void *base, int i, int k, const float x[4]) {
     Glob<float> *p = (Glob<float> *)base + i;
     if (FAST) {
-        put<ONCE>((Glob<f4v> *)p, f4v{x[0], x[1], x[2], x[3]});
+        put_f4<ONCE>(base, 4 * (size_t)i, f4v{x[0], x[1], x[2], x[3]});
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -161,7 +177,7 @@ template <bool FAST, bool ONCE>
 __device__ __forceinline__ void store4_bf16(void *base, int i, int k, const uint32_t x[4]) {
     Glob<uint16_t> *p = (Glob<uint16_t> *)base + i;
     if (FAST) {
-        put<ONCE>((Glob<u2v> *)p, u2v{x[0] | x[1] << 16, x[2] | x[3] << 16});
+        put_u2<ONCE>(base, 2 * (size_t)i, u2v{x[0] | x[1] << 16, x[2] | x[3] << 16});
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -172,7 +188,7 @@ __device__ __forceinline__ void store4_bf16(void *base, int i, int k, const uint
 template <bool FAST, bool ONCE>
 __device__ __forceinline__ uint32_t load4_bytes(const void *base, int i, int k) {
     Glob<const uint8_t> *p = (Glob<const uint8_t> *)base + i;
-    if (FAST) return get<ONCE>((Glob<const uint32_t> *)p);
+    if (FAST) return get_u1<ONCE>(base, (size_t)i);
     uint32_t x = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -184,7 +200,7 @@ template <bool FAST, bool ONCE>
 __device__ __forceinline__ void store4_bytes(void *base, int i, int k, uint32_t x) {
     Glob<uint8_t> *p = (Glob<uint8_t> *)base + i;
     if (FAST) {
-        put<ONCE>((Glob<uint32_t> *)p, x);
+        put_u1<ONCE>(base, (size_t)i, x);
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -396,7 +412,7 @@ __device__ __forceinline__ void step_item(const OptimItem &it, const StepConst &
     static_assert(kOptimChunk == 4 * kBlock, "an item is four elements a thread");
     const int i = 4 * (int)threadIdx.x;
     Quad<M8> q;
-    if (it.count == kOptimChunk && it.flags & kVectors) {
+    if (it.count == kOptimChunk) {
         load_quad<PB, GB, M8, true, ONCE>(it, i, 4, q);
         step_quad<PB, M8, true, ONCE>(it, c, i, 4, q);
     } else {
@@ -487,7 +503,7 @@ __device__ __forceinline__ double power(double beta, uint64_t t) {
 
 template <bool BF16, bool ONCE>
 __device__ __forceinline__ void add_squares(const void *g, int i, double sum[4]) {
-    const u4v q = get<ONCE>((Glob<const u4v> *)((const char *)g + (size_t)i * (BF16 ? 2 : 4)));
+    const u4v q = get_u4<ONCE>(g, (size_t)i * (BF16 ? 2 : 4));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const uint32_t w = q[j];
@@ -507,16 +523,13 @@ template <bool BF16, bool ONCE>
 __device__ __forceinline__ void item_squares(const NormItem &it, double sum[4]) {
     constexpr int kEach = BF16 ? 8 : 4, kPass = kEach * kBlock;
     int i = kEach * (int)threadIdx.x;
-    if ((uintptr_t)it.g % 16 == 0) {
 #pragma unroll 4
-        for (const int end = it.count - kEach; i <= end; i += kPass) add_squares<BF16, ONCE>(it.g, i, sum);
-    }
-    for (; i < it.count; i += kPass) {
-        for (int j = i; j < i + kEach && j < it.count; ++j) {
-            const double x = BF16 ? (double)bf16_to_f32(((Glob<const uint16_t> *)it.g)[j])
-                                  : (double)((Glob<const float> *)it.g)[j];
-            sum[0] = __builtin_fma(x, x, sum[0]);
-        }
+    for (const int end = it.count - kEach; i <= end; i += kPass) add_squares<BF16, ONCE>(it.g, i, sum);
+    for (; i < it.count; ++i) {  // the last elements, of one thread
+        const double x = BF16 ? (double)bf16_to_f32(((Glob<const uint16_t> *)it.g)[i])
+                              : (double)((Glob<const float> *)it.g)[i];
+        sum[0] = __builtin_fma(x, x, sum[0]);
+        if (i % kEach == kEach - 1) break;
     }
 }
 
@@ -646,11 +659,10 @@ __device__ __forceinline__ void carry_f32(const CarryArray &a, uint32_t n_in, Gl
 // ANY: the array may be shorter than four.
 template <bool ANY, typename U>
 __device__ __forceinline__ uint32_t four_bytes(const void *base, U at, U n) {
-    typedef uint32_t word __attribute__((aligned(1)));
     Glob<const uint8_t> *p = (Glob<const uint8_t> *)base;
     if (!ANY || n >= 4) {
         const U b = at < n - 4 ? at : n - 4;
-        return *(Glob<const word> *)(p + b) >> (8 * (uint32_t)(at - b));
+        return *(Glob<const u1a> *)(p + b) >> (8 * (uint32_t)(at - b));
     }
     uint32_t x = 0;
     for (int j = 0; j < 3; ++j)
@@ -661,11 +673,10 @@ __device__ __forceinline__ uint32_t four_bytes(const void *base, U at, U n) {
 // The scale bytes of block i (the low one) and of the next, of n.
 template <bool ANY, typename U>
 __device__ __forceinline__ uint32_t two_scales(const uint8_t *base, U i, U n) {
-    typedef uint16_t half __attribute__((aligned(1)));
     Glob<const uint8_t> *p = (Glob<const uint8_t> *)base;
     if (ANY && n < 2) return p[0];
     const U b = i < n - 2 ? i : n - 2;
-    return (uint32_t)(*(Glob<const half> *)(p + b)) >> (8 * (uint32_t)(i - b));
+    return (uint32_t)(*(Glob<const h1a> *)(p + b)) >> (8 * (uint32_t)(i - b));
 }
 
 // Rows of 8-bit moments into LDS, a word for each element: m's code and scale
@@ -759,7 +770,7 @@ __device__ __forceinline__ void carry_mxfp8(const CarryArray &a, uint32_t n_in, 
         const float scm = scale_of(bm), scs = scale_of(bs);
         keep_positive(v, scs);
         const uint32_t om = encode4_nearest(m, scm), os = encode4_nearest(v, scs);
-        if (k == 4 && a.vectors) {
+        if (k == 4) {
             store4_bytes<true, false>(m_out, i, 4, om);
             store4_bytes<true, false>(v_out, i, 4, os);
         } else {
@@ -898,7 +909,6 @@ hipError_t launch_adamw_carry(const gs_adamw_rows *arrays, int count, int64_t n_
         o.over_parts = ((1u << 20) + (o.width + 3) / 4 - 1) / ((o.width + 3) / 4);
         o.rows = carry_rows(o.width, r.moments == GS_MOMENTS_MXFP8);
         o.moments8 = r.moments == GS_MOMENTS_MXFP8;
-        o.vectors = !(((uintptr_t)r.m_out | (uintptr_t)r.v_out) & 3);
         blocks += (uint32_t)((n_out + o.rows - 1) / o.rows);
     }
     for (uint32_t b = 0; b < blocks; b += (uint32_t)kMaxGrid) {

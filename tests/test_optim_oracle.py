@@ -132,7 +132,7 @@ def test_plan_refuses_workspaces():
     assert L.gs_plan_adamw(None, 1, ctypes.byref(plan()), None) == gs.GS_ERR_INVALID_ARGUMENT
 
 
-@pytest.mark.parametrize("case", ["null_plan", "null_params", "unmade", "short", "beta1", "beta2", "nan_beta", "eps",
+@pytest.mark.parametrize("case", ["null_plan", "null_params", "unmade", "short", "beta1", "beta2", "nan_beta", "eps", "no_eps",
                                   "lr_scale", "step", "control", "no_param"])
 def test_step_refuses(case):
     L = gs.load_library()
@@ -149,6 +149,8 @@ def test_step_refuses(case):
         s = params(beta1=float("nan"))
     elif case == "eps":
         s = params(eps=-1e-8)
+    elif case == "no_eps":
+        s = params(eps=0.0)
     elif case == "lr_scale":
         s = params(lr_scale=float("inf"))
     elif case == "step":
