@@ -655,28 +655,25 @@ __device__ __forceinline__ void carry_f32(const CarryArray &a, uint32_t n_in, Gl
     }
 }
 
-// Four bytes of an array of n from byte `at` on, as far as they are there.
-// ANY: the array may be shorter than four.
-template <bool ANY, typename U>
+// Four bytes of an array of n from byte `at` on, and the scale bytes of block
+// i (the low one) and of the next, of n, as far as they are there.
+template <typename U>
 __device__ __forceinline__ uint32_t four_bytes(const void *base, U at, U n) {
-    Glob<const uint8_t> *p = (Glob<const uint8_t> *)base;
-    if (!ANY || n >= 4) {
+    if (n >= 4) {
         const U b = at < n - 4 ? at : n - 4;
-        return *(Glob<const u1a> *)(p + b) >> (8 * (uint32_t)(at - b));
+        return get_u1<false>(base, b) >> (8 * (uint32_t)(at - b));
     }
+    Glob<const uint8_t> *p = (Glob<const uint8_t> *)base;
     uint32_t x = 0;
     for (int j = 0; j < 3; ++j)
         if (at + j < n) x |= (uint32_t)p[at + j] << (8 * j);
     return x;
 }
-
-// The scale bytes of block i (the low one) and of the next, of n.
-template <bool ANY, typename U>
+template <typename U>
 __device__ __forceinline__ uint32_t two_scales(const uint8_t *base, U i, U n) {
-    Glob<const uint8_t> *p = (Glob<const uint8_t> *)base;
-    if (ANY && n < 2) return p[0];
+    if (n < 2) return *(Glob<const uint8_t> *)base;
     const U b = i < n - 2 ? i : n - 2;
-    return (uint32_t)(*(Glob<const h1a> *)(p + b)) >> (8 * (uint32_t)(i - b));
+    return (uint32_t) * (Glob<const h1a> *)(base + b) >> (8 * (uint32_t)(i - b));
 }
 
 // Rows of 8-bit moments into LDS, a word for each element: m's code and scale
@@ -684,15 +681,21 @@ __device__ __forceinline__ uint32_t two_scales(const uint8_t *base, U i, U n) {
 // of a row at a time, with one unaligned word of codes and one pair of scales
 // a moment, and four such parts at once: single bytes would be four loads an
 // element, which keeps the address units busy, and one part at a time leaves
-// too little in flight. WHOLE: a row is one part.
-template <bool WHOLE, bool ANY, typename U>
+// too little in flight. Reads stay inside the arrays: the few parts from
+// which they would not (of the last block, or any of a short array) are read
+// with a look at the end. WHOLE: a row is one part; U: 32 bits where the
+// input's elements fit.
+template <bool WHOLE, typename U>
 __device__ __forceinline__ void rows_to_lds(const CarryArray &a, uint32_t n_in, Glob<const int32_t> *source,
                                             uint32_t rows, uint32_t *lds) {
     constexpr int kEach = 4;
     const U n = (U)n_in * a.width, scales = (n + 31) >> 5;
+    const U inner = scales > 1 ? (scales - 1) * 32 - 3 : 0;  // parts below it have both words whole
     const uint32_t parts = WHOLE ? 1u : (a.width + 3) >> 2, all = rows * parts;
     for (uint32_t p0 = threadIdx.x; p0 < all; p0 += kEach * kBlock) {
         uint32_t row[kEach], col[kEach], src[kEach], cm[kEach], cv[kEach], sm[kEach], sv[kEach], place[kEach];
+        U at[kEach];
+        bool outer = false;
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
             const uint32_t p = p0 + j * kBlock < all ? p0 + j * kBlock : all - 1;  // the last one several times
@@ -703,17 +706,31 @@ __device__ __forceinline__ void rows_to_lds(const CarryArray &a, uint32_t n_in, 
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            const U at = (U)(src[j] < n_in ? src[j] : 0u) * a.width + col[j];
-            place[j] = (uint32_t)at & 31u;
-            cm[j] = four_bytes<ANY>(a.m, at, n);
-            cv[j] = four_bytes<ANY>(a.v, at, n);
-            sm[j] = two_scales<ANY>(a.m_scale, (U)(at >> 5), scales);
-            sv[j] = two_scales<ANY>(a.v_scale, (U)(at >> 5), scales);
+            at[j] = (U)(src[j] < n_in ? src[j] : 0u) * a.width + col[j];
+            place[j] = (uint32_t)at[j] & 31u;
+            outer |= at[j] >= inner;
         }
-        __builtin_amdgcn_sched_barrier(0);
+        if (__any(outer)) {
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                cm[j] = four_bytes<U>(a.m, at[j], n);
+                cv[j] = four_bytes<U>(a.v, at[j], n);
+                sm[j] = two_scales<U>(a.m_scale, at[j] >> 5, scales);
+                sv[j] = two_scales<U>(a.v_scale, at[j] >> 5, scales);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                cm[j] = get_u1<false>(a.m, at[j]);
+                cv[j] = get_u1<false>(a.v, at[j]);
+                sm[j] = *(Glob<const h1a> *)(a.m_scale + (at[j] >> 5));
+                sv[j] = *(Glob<const h1a> *)(a.v_scale + (at[j] >> 5));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            const bool live = src[j] < n_in;
+            if (src[j] >= n_in) cm[j] = cv[j] = 0u;
             // bytes 1 and 3 of a word: the scales of this block, of the next
             const uint32_t first = __builtin_amdgcn_perm(sv[j], sm[j], 0x040C000Cu);
             const uint32_t next = __builtin_amdgcn_perm(sv[j], sm[j], 0x050C010Cu);
@@ -723,11 +740,29 @@ __device__ __forceinline__ void rows_to_lds(const CarryArray &a, uint32_t n_in, 
                 if (i >= (WHOLE ? a.width : a.width - col[j])) break;
                 // bytes 0 and 2: byte i of cm and of cv
                 const uint32_t codes = __builtin_amdgcn_perm(cv[j], cm[j], 0x0C040C00u + i * 0x00010001u);
-                const uint32_t word = codes | (place[j] + i > 31u ? next : first);
-                out[i] = live ? word : 0u;
+                out[i] = codes | (place[j] + i > 31u ? next : first);
             }
         }
     }
+}
+
+// Four elements' words from LDS to codes under new scales.
+__device__ __forceinline__ void requantise(const uint32_t w[4], uint32_t &cm, uint32_t &cv, uint32_t &sm, uint32_t &sv) {
+    float m[4], v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        // scales in bits 30 .. 23
+        m[j] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[j], __builtin_bit_cast(float, w[j] << 15), false)[0];
+        v[j] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[j], __builtin_bit_cast(float, w[j] >> 1), true)[0];
+    }
+    sm = block_scale(m);
+    sv = block_scale(v);
+    cm = encode4_nearest(m, scale_of(sm));
+    cv = encode4_nearest(v, scale_of(sv));
+    // A positive s stays positive: 1 in every byte that was not 0 and is now.
+    const uint32_t was = __builtin_amdgcn_perm(__builtin_amdgcn_perm(w[3], w[2], 0x0C0C0602u),
+                                               __builtin_amdgcn_perm(w[1], w[0], 0x0C0C0602u), 0x05040100u);
+    cv |= ((was + 0x7F7F7F7Fu) & ~(cv + 0x7F7F7F7Fu)) >> 7 & 0x01010101u;  // codes of s are below 0x80
 }
 
 // 8-bit moments: whole rows, a multiple of 32 of them, go through LDS and are
@@ -738,48 +773,42 @@ __device__ __forceinline__ void carry_mxfp8(const CarryArray &a, uint32_t n_in, 
     const int count = (int)(rows * a.width);
     if (n_in == 0) {
         for (int i = (int)threadIdx.x; i < count; i += kBlock) lds[i] = 0u;
-    } else if (n_in < 64 || (uint64_t)n_in * a.width >= 0xFFFFFFFFu) {
-        rows_to_lds<false, true, uint64_t>(a, n_in, source, rows, lds);
+    } else if ((uint64_t)n_in * a.width >= 0xFFFFFFFFu) {
+        rows_to_lds<false, uint64_t>(a, n_in, source, rows, lds);
     } else if (a.width <= 4) {
-        rows_to_lds<true, false, uint32_t>(a, n_in, source, rows, lds);
+        rows_to_lds<true, uint32_t>(a, n_in, source, rows, lds);
     } else {
-        rows_to_lds<false, false, uint32_t>(a, n_in, source, rows, lds);
+        rows_to_lds<false, uint32_t>(a, n_in, source, rows, lds);
     }
     __syncthreads();
     uint8_t *m_out = (uint8_t *)a.m_out + base, *v_out = (uint8_t *)a.v_out + base;
-    for (int i = 4 * (int)threadIdx.x; i < count + 31; i += 4 * kBlock) {  // whole blocks of lanes, as in the step
+    uint8_t *m_scale = a.m_scale_out + (base >> 5), *v_scale = a.v_scale_out + (base >> 5);
+    const bool writes = (threadIdx.x & 7) == 0;
+    int i = 4 * (int)threadIdx.x;
+    for (; i < (count & ~31); i += 4 * kBlock) {
+        const u4v q = *(const u4v *)(lds + i);
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+        uint32_t cm, cv, sm, sv;
+        requantise(w, cm, cv, sm, sv);
+        put_u1<false>(m_out, i, cm);
+        put_u1<false>(v_out, i, cv);
+        if (writes) {
+            ((Glob<uint8_t> *)m_scale)[i >> 5] = (uint8_t)sm;
+            ((Glob<uint8_t> *)v_scale)[i >> 5] = (uint8_t)sv;
+        }
+    }
+    if (i < count + 31) {  // the last block, if it is a shorter one: all its lanes, as in the step
         const int left = count - i;
         const int k = left < 4 ? (left > 0 ? left : 0) : 4;
-        uint32_t w[4];
-        if (k == 4) {
-            const u4v q = *(const u4v *)(lds + i);
+        uint32_t w[4], cm, cv, sm, sv;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = q[j];
-        } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = j < k ? lds[i + j] : 0u;
-        }
-        float m[4], v[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            // scales in bits 30 .. 23
-            m[j] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[j], __builtin_bit_cast(float, w[j] << 15), false)[0];
-            v[j] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[j], __builtin_bit_cast(float, w[j] >> 1), true)[0];
-        }
-        const uint32_t bm = block_scale(m), bs = block_scale(v);
-        const float scm = scale_of(bm), scs = scale_of(bs);
-        keep_positive(v, scs);
-        const uint32_t om = encode4_nearest(m, scm), os = encode4_nearest(v, scs);
-        if (k == 4) {
-            store4_bytes<true, false>(m_out, i, 4, om);
-            store4_bytes<true, false>(v_out, i, 4, os);
-        } else {
-            store4_bytes<false, false>(m_out, i, k, om);
-            store4_bytes<false, false>(v_out, i, k, os);
-        }
-        if ((threadIdx.x & 7) == 0 && k > 0) {
-            ((Glob<uint8_t> *)a.m_scale_out)[(base + i) >> 5] = (uint8_t)bm;
-            ((Glob<uint8_t> *)a.v_scale_out)[(base + i) >> 5] = (uint8_t)bs;
+        for (int j = 0; j < 4; ++j) w[j] = j < k ? lds[i + j] : 0u;
+        requantise(w, cm, cv, sm, sv);
+        store4_bytes<false, false>(m_out, i, k, cm);
+        store4_bytes<false, false>(v_out, i, k, cv);
+        if (writes && k > 0) {
+            ((Glob<uint8_t> *)m_scale)[i >> 5] = (uint8_t)sm;
+            ((Glob<uint8_t> *)v_scale)[i >> 5] = (uint8_t)sv;
         }
     }
 }
