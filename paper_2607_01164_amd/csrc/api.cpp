@@ -519,7 +519,7 @@ void *scratch_address(hipError_t *err) {
 
 // Pieces and sizes of a list of tensors; false if it is malformed.
 struct AdamwSizes {
-    int64_t items = 0, norm_items = 0, elements = 0, step_bytes = 0, norm_bytes = 0;
+    int64_t items = 0, norms = 0, step_bytes = 0, norm_bytes = 0;
 };
 bool adamw_sizes(const gs_adamw_tensor *tensors, int64_t count, AdamwSizes *z) {
     if (count < 0 || count > ((int64_t)1 << 20) || (count > 0 && !tensors)) return false;
@@ -528,16 +528,15 @@ bool adamw_sizes(const gs_adamw_tensor *tensors, int64_t count, AdamwSizes *z) {
         if (t.n < 0 || t.n >= ((int64_t)1 << 40)) return false;
         const int64_t ps = t.param_type == GS_TYPE_BF16 ? 2 : 4, gs = t.grad_type == GS_TYPE_BF16 ? 2 : 4;
         const int64_t ms = t.moments == GS_MOMENTS_MXFP8 ? 1 : 4;
-        z->elements += t.n;
+        z->norms += norm_items(t.n);
         z->norm_bytes += t.n * gs;
         if (t.param) {
             z->items += optim_items(t.n);
             z->step_bytes += t.n * (2 * ps + gs + 4 * ms);
         }
-        if (z->items >= ((int64_t)1 << 31)) return false;
+        if (z->items >= ((int64_t)1 << 31) || z->norms >= ((int64_t)1 << 31)) return false;
     }
-    for (int64_t i = 0; i < count; ++i) z->norm_items += norm_items(tensors[i].n, norm_chunk(z->elements));
-    return z->norm_items < ((int64_t)1 << 31);
+    return true;
 }
 
 struct AdamwPlanLayout {
@@ -1075,7 +1074,7 @@ gs_status gs_densify(const gs_params *in, int64_t n_in, const float *weight, con
 size_t gs_adamw_plan_bytes(const gs_adamw_tensor *tensors, int64_t count) {
     AdamwSizes z;
     if (!adamw_sizes(tensors, count, &z)) return (size_t)-1;
-    return adamw_plan_layout(nullptr, z.items, z.norm_items).bytes;
+    return adamw_plan_layout(nullptr, z.items, z.norms).bytes;
 }
 
 gs_status gs_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, gs_adamw_plan *plan, hipStream_t stream) {
@@ -1108,13 +1107,13 @@ gs_status gs_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, gs_adamw_
             return bad("moments are null or not aligned to their type");
         if (m8 && (!t.m_scale || !t.v_scale)) return bad("the scales of MXFP8 moments are null");
     }
-    const AdamwPlanLayout l = adamw_plan_layout(plan->work, z.items, z.norm_items);
+    const AdamwPlanLayout l = adamw_plan_layout(plan->work, z.items, z.norms);
     if (!plan->work || plan->work_bytes < l.bytes || !aligned(plan->work))
         return fail(GS_ERR_WORKSPACE, "gs_plan_adamw: plan needs %zu bytes, 256-byte aligned (got %zu)", l.bytes,
                     plan->work_bytes);
-    GS_TRY(launch_plan_adamw(tensors, count, z.elements, l.items, l.norms, l.work, stream), "gs_plan_adamw");
+    GS_TRY(launch_plan_adamw(tensors, count, l.items, l.norms, l.work, stream), "gs_plan_adamw");
     plan->n_items = z.items;
-    plan->n_norm_items = z.norm_items;
+    plan->n_norm_items = z.norms;
     plan->step_bytes = z.step_bytes;
     plan->norm_bytes = z.norm_bytes;
     plan->count = (int32_t)count;

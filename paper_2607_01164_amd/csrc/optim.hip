@@ -33,7 +33,7 @@ struct FillArgs {
     OptimTensor t[kFill];
     uint32_t first[kFill + 1];       // first item of each, counted from the launch's first
     uint32_t first_norm[kFill + 1];  // the same of its NormItems
-    int count, norm_chunk;
+    int count;
 };
 
 // ---- items ----------------------------------------------------------------
@@ -68,11 +68,11 @@ __global__ __launch_bounds__(kBlock) void k_fill_items(FillArgs a, OptimItem *it
         int k = 0;
         while (i >= a.first_norm[k + 1]) ++k;
         const OptimTensor t = a.t[k];
-        const int64_t base = (int64_t)(i - a.first_norm[k]) * a.norm_chunk;
+        const int64_t base = (int64_t)(i - a.first_norm[k]) * kNormChunk;
         const int64_t left = t.n - base;
         NormItem it;
         it.g = (const char *)t.g + base * (t.flags & kGradBf16 ? 2 : 4);
-        it.count = (int32_t)(left < a.norm_chunk ? left : a.norm_chunk);
+        it.count = (int32_t)(left < kNormChunk ? left : kNormChunk);
         it.flags = t.flags;
         norms[i] = it;
     }
@@ -834,12 +834,11 @@ __global__ __launch_bounds__(kBlock) void k_carry(CarryArgs a, const int32_t *so
 
 // ---- host -----------------------------------------------------------------------
 
-hipError_t launch_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, int64_t elements, OptimItem *items,
-                             NormItem *norms, const NormWork &work, hipStream_t s) {
+hipError_t launch_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, OptimItem *items, NormItem *norms,
+                             const NormWork &work, hipStream_t s) {
     const hipError_t e0 = fill_u32(work.count, 0u, kNormCounters * kNormCounter, s);
     if (e0 != hipSuccess) return e0;
     FillArgs a;
-    a.norm_chunk = (int)norm_chunk(elements);
     uint64_t done = 0, done_norm = 0;
     int64_t i = 0;
     while (i < count) {
@@ -850,7 +849,7 @@ hipError_t launch_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, int6
         while (i < count && a.count < kFill) {
             const gs_adamw_tensor &t = tensors[i];
             const uint64_t pieces = t.param ? (uint64_t)optim_items(t.n) : 0;
-            const uint64_t norm_pieces = (uint64_t)norm_items(t.n, a.norm_chunk);
+            const uint64_t norm_pieces = (uint64_t)norm_items(t.n);
             if (a.count && here + pieces > 0x7FFFFFFFu) break;
             if (norm_pieces) {
                 OptimTensor &o = a.t[a.count];

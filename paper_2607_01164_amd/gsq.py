@@ -756,32 +756,37 @@ class AdamTensor:
         return AdamTensor(param, grad, z(n), z(n), z(moment_scales(n)), z(moment_scales(n)), lr, weight_decay)
 
     def c(self) -> GsAdamwTensor:
-        types = {torch.float32: GS_TYPE_F32, torch.bfloat16: GS_TYPE_BF16}
-        n = self.grad.numel()
-        for t, nm in ((self.param, "param"), (self.grad, "grad")):
-            if t is not None and (not t.is_cuda or not t.is_contiguous() or t.dtype not in types or t.numel() != n):
-                raise ValueError(f"{nm} must be a contiguous float32 or bfloat16 device tensor of the gradient's size")
-        moments = GS_MOMENTS_F32
-        if self.param is not None:
-            moments = _moments_of(self.m, self.v, self.m_scale, self.v_scale, n, "")
-        return GsAdamwTensor(_ptr(self.param), self.grad.data_ptr(), _ptr(self.m), _ptr(self.v), _ptr(self.m_scale),
-                             _ptr(self.v_scale), n, types[self.grad.dtype if self.param is None else self.param.dtype],
-                             types[self.grad.dtype], moments, float(self.lr), float(self.weight_decay))
+        p, g = self.param, self.grad
+        n, gt = g.numel(), _ADAM_TYPES.get(g.dtype)
+        if gt is None or not g.is_cuda or not g.is_contiguous():
+            raise ValueError("grad must be a contiguous float32 or bfloat16 device tensor")
+        if p is None:
+            return GsAdamwTensor(None, g.data_ptr(), None, None, None, None, n, gt, gt, GS_MOMENTS_F32,
+                                 self.lr, self.weight_decay)
+        pt = _ADAM_TYPES.get(p.dtype)
+        if pt is None or not p.is_cuda or not p.is_contiguous() or p.numel() != n:
+            raise ValueError("param must be a contiguous float32 or bfloat16 device tensor of the gradient's size")
+        moments = _moments_of(self.m, self.v, self.m_scale, self.v_scale, n, "")
+        return GsAdamwTensor(p.data_ptr(), g.data_ptr(), self.m.data_ptr(), self.v.data_ptr(), _ptr(self.m_scale),
+                             _ptr(self.v_scale), n, pt, gt, moments, self.lr, self.weight_decay)
+
+
+_ADAM_TYPES = {torch.float32: GS_TYPE_F32, torch.bfloat16: GS_TYPE_BF16}
 
 
 def _moments_of(m, v, m_scale, v_scale, n: int, label: str) -> int:
     """Checks the moments of n elements and returns their form."""
-    if m is None or v is None or m.dtype != v.dtype or m.dtype not in (torch.float32, torch.uint8):
+    if m is None or v is None or m.dtype is not v.dtype or m.dtype not in (torch.float32, torch.uint8):
         raise ValueError(f"m{label} and v{label} must both be float32 or both uint8")
-    for t, nm in ((m, "m"), (v, "v")):
-        if not t.is_cuda or not t.is_contiguous() or t.numel() < n:
-            raise ValueError(f"{nm}{label} must be a contiguous device tensor of {n} elements")
-    if m.dtype == torch.float32:
+    if not (m.is_cuda and v.is_cuda and m.is_contiguous() and v.is_contiguous() and m.numel() >= n and
+            v.numel() >= n):
+        raise ValueError(f"m{label} and v{label} must be contiguous device tensors of {n} elements")
+    if m.dtype is torch.float32:
         return GS_MOMENTS_F32
+    k = moment_scales(n)
     for t, nm in ((m_scale, "m_scale"), (v_scale, "v_scale")):
-        if t is None or not t.is_cuda or t.dtype != torch.uint8 or not t.is_contiguous() or \
-                t.numel() < moment_scales(n):
-            raise ValueError(f"{nm}{label} must be a contiguous uint8 device tensor of {moment_scales(n)} elements")
+        if t is None or not t.is_cuda or t.dtype is not torch.uint8 or not t.is_contiguous() or t.numel() < k:
+            raise ValueError(f"{nm}{label} must be a contiguous uint8 device tensor of {k} elements")
     return GS_MOMENTS_MXFP8
 
 
