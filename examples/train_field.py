@@ -129,6 +129,10 @@ class Trainer:
 
     def step(self):
         """One iteration; nothing of it but the index's pair count is waited for."""
+        self.gradients()
+        self.update()
+
+    def gradients(self):
         gs.gs_activate(self.raw, SCALE_CAP, self.gauss.scale, self.gauss.value, self.gauss.weight)
         self.build_index()
         self.offsets.uniform_(0.0, 1.0, generator=self.gen)
@@ -140,6 +144,8 @@ class Trainer:
         gs.gs_sample_backward(self.gauss, self.index, self.query, self.plan, self.value, self.influence,
                               self.grad_value, self.grad_influence, self.grads, work)
         gs.gs_activate_backward(self.raw, SCALE_CAP, self.grads, self.raw_grads)
+
+    def update(self):
         gs.gs_grad_norm(self.adam, self.control, max_norm=self.max_norm)
         gs.gs_adamw(self.adam, control=self.control, eps=1e-15, seed=self.seed)
 
