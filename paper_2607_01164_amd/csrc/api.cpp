@@ -576,7 +576,7 @@ extern "C" {
 
 const char *gs_last_error(void) { return g_err.c_str(); }
 
-int gs_version(void) { return 100; }
+int gs_version(void) { return 110; }
 
 void gs_profile_enable(int on) { g_prof_on = on != 0; }
 

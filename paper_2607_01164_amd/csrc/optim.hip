@@ -529,7 +529,6 @@ __device__ __forceinline__ void item_squares(const NormItem &it, double sum[4]) 
         const double x = BF16 ? (double)bf16_to_f32(((Glob<const uint16_t> *)it.g)[i])
                               : (double)((Glob<const float> *)it.g)[i];
         sum[0] = __builtin_fma(x, x, sum[0]);
-        if (i % kEach == kEach - 1) break;
     }
 }
 

@@ -437,6 +437,67 @@ def test_elements_past_32_bits():
     assert not p[:1 << 20].any() and not t.m[(1 << 31):(1 << 31) + 4096].any()
 
 
+@pytest.mark.parametrize("types", TYPES, ids=["-".join(t) for t in TYPES])
+@pytest.mark.parametrize("form", FORMS)
+def test_lists_past_the_cache(form, types):
+    """A list whose step touches more than 256 MB, which goes past the caches:
+    its pieces at the start, at the end and across tensors follow the
+    definition, and the norm is the sum's."""
+    import torch
+    n = 31_000_003 if form == "mxfp8" else 14_000_003
+    t, u = make(n, types, form, 21), make(4099, types, form, 22)
+    plan_bytes = sum(x.numel() * x.element_size() * (1 if x is t.grad else 2) for x in (t.param, t.grad, t.m, t.v))
+    assert plan_bytes > 256 << 20
+    ends = [(0, 5000), (n // 2 // 32 * 32, 5000), ((n - 3000) // 32 * 32, n)]
+    import paper_2607_01164_amd as gs
+
+    def window(a, b):
+        b = min(a + b, n)
+        w = lambda x: None if x is None else x[a // 32:(b + 31) // 32]  # noqa: E731
+        return gs.AdamTensor(t.param[a:b], t.grad[a:b], t.m[a:b], t.v[a:b], w(t.m_scale), w(t.v_scale), t.lr,
+                             t.weight_decay)
+
+    views = [window(a, b) for a, b in ends]
+    before, tail = [snapshot(v) for v in views], snapshot(u)
+    control = gs.alloc_adam_control("cuda")
+    plan = gs.AdamPlan([t, u])
+    gs.gs_grad_norm(plan, control)
+    gs.gs_adamw(plan, beta1=B1, beta2=B2, eps=EPS, control=control, seed=13)
+    want = math.sqrt(float(t.grad.double().square().sum() + u.grad.double().square().sum()))
+    assert abs(gs.read_adam_control(control)["norm"] / want - 1) < 2 * oo.U
+    for v, b, (a, _) in zip(views, before, ends):
+        check(v, b, 0, 1, seed=13, first=a, label=f"{form} {types} from {a}")
+    check(u, tail, 1, 1, seed=13, label=f"{form} {types} second tensor")
+
+
+def test_binding_refuses_on_the_device():
+    import torch
+    import paper_2607_01164_amd as gs
+    x = torch.zeros(64, 2, device="cuda")
+    h = torch.zeros(64, dtype=torch.float16, device="cuda")
+    m = torch.zeros(64, dtype=torch.uint8, device="cuda")
+    good = dict(param=x[:, 0].contiguous(), grad=x[:, 0].contiguous(), m=x[:, 0].contiguous(), v=x[:, 0].contiguous())
+    gs.AdamTensor(**good).c()
+    for bad in (dict(grad=x[:, 0]), dict(param=x[:, 0]), dict(m=x[:, 0]), dict(grad=h), dict(param=h), dict(m=m),
+                dict(m=m, v=m), dict(m=m, v=m, m_scale=m[:2], v_scale=m[:1]), dict(m=x[0], v=x[0]), dict(param=x),
+                dict(m=None), dict(m=m, v=m, m_scale=m[:4:2], v_scale=m[:2])):
+        with pytest.raises(ValueError):
+            gs.AdamTensor(**{**good, **bad}).c()
+    with pytest.raises(gs.GsError):
+        gs.AdamPlan([gs.AdamTensor(**{**good, "param": good["param"].bfloat16()})])  # bfloat16 with float32 gradients
+    with pytest.raises(gs.GsError):
+        gs.gs_adamw(gs.AdamPlan([gs.AdamTensor(None, good["grad"])]), step=1)  # nothing to update
+    with pytest.raises(ValueError):
+        gs.gs_grad_norm(gs.AdamPlan([gs.AdamTensor(**good)]), m[:63])
+    with pytest.raises(ValueError):
+        gs.AdamCarry([gs.AdamRows(3, m, m, x, x, m[:2], m[:2])])
+    carry = gs.AdamCarry([gs.AdamRows(4, m, m, m.clone(), m.clone(), m[:2], m[:2], m[:2].clone(), m[:2].clone())])
+    with pytest.raises(ValueError):
+        gs.gs_adamw_carry(carry, 16, torch.zeros(17, dtype=torch.int32, device="cuda"), 17)
+    with pytest.raises(ValueError):
+        gs.gs_adamw_carry(carry, 16, torch.zeros(16, dtype=torch.int64, device="cuda"), 16)
+
+
 # ---- the rounding as a whole ------------------------------------------------
 
 def test_averages_move_although_a_step_is_below_the_grid():
