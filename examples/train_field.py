@@ -44,7 +44,7 @@ class Moments:
         self.form, self.arrays = form, []
         for _, w, _ in ARRAYS:
             dt = torch.float32 if form == gs.GS_MOMENTS_F32 else torch.uint8
-            a = {"m": torch.zeros(rows * w, dtype=dt, device=device), "v": torch.zeros(rows * w, dtype=dt, device=device)}
+            a = {k: torch.zeros(rows * w, dtype=dt, device=device) for k in ("m", "v")}
             if form == gs.GS_MOMENTS_MXFP8:
                 for k in ("m_scale", "v_scale"):
                     a[k] = torch.zeros(gs.moment_scales(rows * w), dtype=torch.uint8, device=device)
@@ -73,7 +73,7 @@ class Trainer:
         rows = capacity or 2 * n
         self.sets = [gs.ParamSet.empty(rows, device) for _ in range(2)]
         self.moments = [Moments(rows, moments, device) for _ in range(2)]
-        self.carries = [carry_between(self.moments[0], self.moments[1]), carry_between(self.moments[1], self.moments[0])]
+        self.carries = [carry_between(self.moments[i], self.moments[1 - i]) for i in range(2)]
         self.now = 0  # which of the two sets is trained
         self.control = gs.alloc_adam_control(device)
         cells = max(4, min(32, dims // 4))
@@ -195,7 +195,8 @@ def main():
     ap.add_argument("--densify-every", type=int, default=100)
     a = ap.parse_args()
     t = Trainer(a.gaussians, a.dims, gs.GS_MOMENTS_MXFP8 if a.moments == 8 else gs.GS_MOMENTS_F32)
-    train(t, a.steps, a.densify_every, lambda k, n, x: print(f"step {k:5d}  {n:8d} Gaussians  loss {x:.5f}", flush=True))
+    train(t, a.steps, a.densify_every,
+          lambda k, n, x: print(f"step {k:5d}  {n:8d} Gaussians  loss {x:.5f}", flush=True))
     c = gs.read_adam_control(t.control)
     print(f"{c['step']} steps, {c['skipped']} skipped, last gradient norm {c['norm']:.3g}, PSNR {t.psnr():.2f} dB")
 

@@ -27,8 +27,8 @@
  * from the unrounded m and v; then m and s are rounded to the block's grid,
  * up with probability equal to the share of the way ((k + 1/2) / 2^16 with
  * 16 random bits k). Rounding to the nearest would not do: with 1 - beta2 =
- * 0.001 an average moves by a 50th of the grid's spacing per step, and would
- * never leave its place. A positive s never becomes 0 (it becomes the
+ * 0.001 a falling s moves by a hundredth of the grid's spacing a step, and
+ * would never leave its place. A positive s never becomes 0 (it becomes the
  * smallest value of its block's grid), so that a remembered m is not divided
  * by a forgotten v. Values that are not finite are kept as NaN. All-zero
  * bytes are the state of a new tensor.

@@ -77,9 +77,9 @@ struct CarryArray {
     uint32_t width, rows, over, over_parts;
     uint32_t moments8, pad;
 };
-// 8-bit rows: 4 parts of a row a thread, which are 3072 elements for rows of
-// three (one part a thread took twice as long); 32-bit rows: one pass of 4
-// elements a thread.
+// 8-bit rows: 4 parts of a row a thread (for 2 M Gaussians 45 us; 50 with 2
+// parts, and with 8, which leave fewer workgroups resident); 32-bit rows: one
+// pass of 4 elements a thread.
 inline uint32_t carry_rows(uint32_t width, bool moments8) {
     const uint32_t most = moments8 ? (width < 4 ? 1024 * width : kCarryMost) : 1024;
     const uint32_t rows = most / width / 32 * 32;

@@ -35,8 +35,8 @@ EXPORTED = ("gs_query_size", "gs_index_work_bytes", "gs_build_index", "gs_plan_b
             "gs_profile_select", "gs_profile_reset", "gs_profile_read", "gs_activate", "gs_activate_backward",
             "gs_loss_work_bytes", "gs_loss", "gs_densify_work_bytes", "gs_densify",
             "gs_sample_gaussian_major_work_bytes", "gs_sample_gaussian_major", "gs_backward_pair_count",
-            "gs_sample_pair_counts", "gs_sample_backward_noalloc", "gs_plan_queries", "gs_sample_planned", "gs_adamw_plan_bytes",
-            "gs_plan_adamw", "gs_grad_norm", "gs_adamw", "gs_adamw_carry")
+            "gs_sample_pair_counts", "gs_sample_backward_noalloc", "gs_plan_queries", "gs_sample_planned",
+            "gs_adamw_plan_bytes", "gs_plan_adamw", "gs_grad_norm", "gs_adamw", "gs_adamw_carry")
 
 GS_TYPE_F32 = 0
 GS_TYPE_BF16 = 1

@@ -61,8 +61,8 @@ def make(n, types, form, seed, lr=0.01, wd=0.1, offset=0, spread=3.0):
     p = dev(r.normal(size=n).astype(np.float32), dtype(types[0]))
     g = dev(g.astype(np.float32), dtype(types[1]))
     if form == "f32":
-        return gs.AdamTensor(p, g, dev(m.astype(np.float32), torch.float32), dev((s * s).astype(np.float32), torch.float32),
-                             lr=lr, weight_decay=wd)
+        f = lambda a: dev(a.astype(np.float32), torch.float32)  # noqa: E731
+        return gs.AdamTensor(p, g, f(m), f(s * s), lr=lr, weight_decay=wd)
     k = gs.moment_scales(n)
     codes = lambda x, e: oo.magnitude_code(  # noqa: E731
         np.abs(oo.e4m3(torch.from_numpy((np.abs(x) * np.exp2(-np.repeat(e, 32)[:n])).astype(np.float32))
@@ -71,8 +71,8 @@ def make(n, types, form, seed, lr=0.01, wd=0.1, offset=0, spread=3.0):
     qm = codes(m, em).astype(np.uint8) | ((m < 0) * 128).astype(np.uint8)
     qs = codes(s, es).astype(np.uint8)
     # torch.empty(n + offset) of bytes: the codes are off their allocation too
-    return gs.AdamTensor(p, g, dev(qm, torch.uint8), dev(qs, torch.uint8), dev_bytes(em + 127, k), dev_bytes(es + 127, k),
-                         lr=lr, weight_decay=wd)
+    return gs.AdamTensor(p, g, dev(qm, torch.uint8), dev(qs, torch.uint8), dev_bytes(em + 127, k),
+                         dev_bytes(es + 127, k), lr=lr, weight_decay=wd)
 
 
 def dev_bytes(a, k):
@@ -87,7 +87,8 @@ def snapshot(t):
     return out
 
 
-def check(t, before, place, step, seed=0, clip=1.0, lr_scale=1.0, beta1=B1, beta2=B2, eps=EPS, first=0, sharp=True, label=""):
+def check(t, before, place, step, seed=0, clip=1.0, lr_scale=1.0, beta1=B1, beta2=B2, eps=EPS, first=0, sharp=True,
+          label=""):
     """The tensor after a step against the oracle's step from `before`.
     first: the index of the first element looked at."""
     import torch
@@ -105,7 +106,8 @@ def check(t, before, place, step, seed=0, clip=1.0, lr_scale=1.0, beta1=B1, beta
         bad = ~((np.abs(got - p) <= dp) | (np.isnan(p) & np.isnan(got)) | (got == p))
         assert not bad.any(), f"{label} param: {bad.sum()} off, {got[bad][:3]} for {p[bad][:3]} within {dp[bad][:3]}"
     if t.m_scale is None:
-        for nm, x, y, d in (("m", host(t.m), m, dm), ("v", host(t.v), v, 7 * oo.U * v * (2 if clip != 1.0 else 1) + 3 * oo.TINY)):
+        dv = 7 * oo.U * v * (2 if clip != 1.0 else 1) + 3 * oo.TINY
+        for nm, x, y, d in (("m", host(t.m), m, dm), ("v", host(t.v), v, dv)):
             bad = ~((np.abs(x - y) <= d) | (np.isnan(x) & np.isnan(y)) | (x == y) | (np.isinf(x) & (y > 3.4e38)))
             assert not bad.any(), f"{label} {nm}: {bad.sum()} off, {x[bad][:3]} for {y[bad][:3]}"
     else:
@@ -285,8 +287,8 @@ def test_norm(sizes, gtype):
     import torch
     import paper_2607_01164_amd as gs
     r = np.random.default_rng(sum(sizes))
-    gsl = [torch.from_numpy((r.normal(size=n) * np.exp(r.normal(size=n) * 2)).astype(np.float32)).to(dtype(gtype)).cuda()
-           for n in sizes]
+    draws = [(r.normal(size=n) * np.exp(r.normal(size=n) * 2)).astype(np.float32) for n in sizes]
+    gsl = [torch.from_numpy(x).to(dtype(gtype)).cuda() for x in draws]
     plan = gs.AdamPlan([gs.AdamTensor(None, g) for g in gsl])
     want = math.sqrt(math.fsum(float(x) for g in gsl for x in np.square(host(g))))
     for max_norm in (float("inf"), want * 2, want / 3):
