@@ -631,3 +631,45 @@ def test_carry_of_a_set_in_one_launch():
         assert np.all(host(out["m"])[:100 * w] == 0) and np.all(host(out["v"])[:100 * w] == 0)
     with pytest.raises(ValueError):
         gs.gs_adamw_carry(carry, n_in + 1, src, 10)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_carry_from_past_32_bits(form):
+    """Inputs of more than 2^32 elements: rows near their end and near their
+    start, by addresses of 64 bits."""
+    import torch
+    import paper_2607_01164_amd as gs
+    free, _ = torch.cuda.mem_get_info()
+    if free < 60 << 30:
+        pytest.skip("needs 60 GiB")
+    width, n_in, tail = 4, 1_100_000_000, 4000
+    log(f"case: carry from {n_in} rows of {width}, {form}")
+    n, last = n_in * width, tail * width
+    src = make(last, ("f32", "f32"), form, 31)
+    dt = torch.float32 if form == "f32" else torch.uint8
+    a = {k: torch.zeros(n, dtype=dt, device="cuda") for k in ("m", "v")}
+    a["m"][n - last:], a["v"][n - last:] = src.m, src.v
+    if form == "mxfp8":
+        for k, x in (("m_scale", src.m_scale), ("v_scale", src.v_scale)):
+            a[k] = torch.zeros(gs.moment_scales(n), dtype=torch.uint8, device="cuda")
+            a[k][-gs.moment_scales(last):] = x
+    r = np.random.default_rng(8)
+    source = np.concatenate([n_in - tail + np.sort(r.permutation(tail)[:3000]), [0, 1, 2 ** 30 - 1, 2 ** 30, -1, n_in],
+                             n_in - 1 - np.arange(50)])
+    out = {k: torch.full((len(source) * width,), 9, dtype=dt, device="cuda") for k in ("m", "v")}
+    if form == "mxfp8":
+        for k in ("m_scale", "v_scale"):
+            out[k] = torch.full((gs.moment_scales(len(source) * width),), 9, dtype=dt, device="cuda")
+    rows = gs.AdamRows(width, a["m"], a["v"], out["m"], out["v"], a.get("m_scale"), a.get("v_scale"),
+                       out.get("m_scale"), out.get("v_scale"))
+    gs.gs_adamw_carry(gs.AdamCarry([rows]), n_in, torch.from_numpy(source.astype(np.int32)).cuda(), len(source))
+    b = snapshot(src)
+    local = source - (n_in - tail)
+    live = (local >= 0) & (source < n_in)
+    for k in ("m", "v"):
+        x = np.sqrt(b[k]) if form == "mxfp8" and k == "v" else b[k]
+        want = np.where(live[:, None], x.reshape(tail, width)[np.where(live, local, 0)], 0.0).reshape(-1)
+        if form == "f32":
+            np.testing.assert_array_equal(host(out[k]), want)
+        else:
+            oo.check_mxfp8(host(out[k]), host(out[k + "_scale"]), want, 0.0 * want, positive=k == "v", label=k)
