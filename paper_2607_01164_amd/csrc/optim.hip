@@ -139,12 +139,12 @@ GS_OPTIM_ACCESS(u1, uint32_t, u1a)
 #undef GS_OPTIM_ACCESS
 
 // Four consecutive elements as float32. FAST: all there. Otherwise the first
-// k, one by one, and zeros.
+// k, and zeros (one by one where k < 4).
 template <bool BF16, bool FAST, bool ONCE>
 __device__ __forceinline__ void load4(const void *base, int i, int k, float x[4]) {
     if (BF16) {
         Glob<const uint16_t> *p = (Glob<const uint16_t> *)base + i;
-        if (FAST) {
+        if (FAST || k == 4) {
             const u2v q = get_u2<ONCE>(base, 2 * (size_t)i);
             x[0] = bf16_to_f32(q.x & 0xFFFFu);
             x[1] = bf16_to_f32(q.x >> 16);
@@ -156,7 +156,7 @@ __device__ __forceinline__ void load4(const void *base, int i, int k, float x[4]
         }
     } else {
         Glob<const float> *p = (Glob<const float> *)base + i;
-        if (FAST) {
+        if (FAST || k == 4) {
             const f4v q = get_f4<ONCE>(base, 4 * (size_t)i);
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[j] = q[j];
@@ -170,7 +170,7 @@ __device__ __forceinline__ void load4(const void *base, int i, int k, float x[4]
 template <bool FAST, bool ONCE>
 __device__ __forceinline__ void store4_f32(void *base, int i, int k, const float x[4]) {
     Glob<float> *p = (Glob<float> *)base + i;
-    if (FAST) {
+    if (FAST || k == 4) {
         put_f4<ONCE>(base, 4 * (size_t)i, f4v{x[0], x[1], x[2], x[3]});
     } else {
 #pragma unroll
@@ -182,7 +182,7 @@ __device__ __forceinline__ void store4_f32(void *base, int i, int k, const float
 template <bool FAST, bool ONCE>
 __device__ __forceinline__ void store4_bf16(void *base, int i, int k, const uint32_t x[4]) {
     Glob<uint16_t> *p = (Glob<uint16_t> *)base + i;
-    if (FAST) {
+    if (FAST || k == 4) {
         put_u2<ONCE>(base, 2 * (size_t)i, u2v{x[0] | x[1] << 16, x[2] | x[3] << 16});
     } else {
 #pragma unroll
@@ -194,7 +194,7 @@ __device__ __forceinline__ void store4_bf16(void *base, int i, int k, const uint
 template <bool FAST, bool ONCE>
 __device__ __forceinline__ uint32_t load4_bytes(const void *base, int i, int k) {
     Glob<const uint8_t> *p = (Glob<const uint8_t> *)base + i;
-    if (FAST) return get_u1<ONCE>(base, (size_t)i);
+    if (FAST || k == 4) return get_u1<ONCE>(base, (size_t)i);
     uint32_t x = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
@@ -205,7 +205,7 @@ __device__ __forceinline__ uint32_t load4_bytes(const void *base, int i, int k) 
 template <bool FAST, bool ONCE>
 __device__ __forceinline__ void store4_bytes(void *base, int i, int k, uint32_t x) {
     Glob<uint8_t> *p = (Glob<uint8_t> *)base + i;
-    if (FAST) {
+    if (FAST || k == 4) {
         put_u1<ONCE>(base, (size_t)i, x);
     } else {
 #pragma unroll
@@ -412,7 +412,9 @@ __device__ __forceinline__ void step_quad(const OptimItem &it, const StepConst &
 }
 
 // An item is one pass of the workgroup. In a shorter last one the lanes past
-// the end stay: those of its last block take part in the block's maximum.
+// the end stay: those of its last block take part in the block's maximum. Its
+// lanes of four elements take vectors as well: 8000 tensors of 2047 elements
+// 81 us, 119 one by one (float32; 100 elements each 12.6, 10.7).
 template <bool PB, bool GB, bool M8, bool ONCE>
 __device__ __forceinline__ void step_item(const OptimItem &it, const StepConst &c) {
     static_assert(kOptimChunk == 4 * kBlock, "an item is four elements a thread");
