@@ -762,13 +762,13 @@ class AdamTensor:
             raise ValueError("grad must be a contiguous float32 or bfloat16 device tensor")
         if p is None:
             return GsAdamwTensor(None, g.data_ptr(), None, None, None, None, n, gt, gt, GS_MOMENTS_F32,
-                                 self.lr, self.weight_decay)
+                                 float(self.lr), float(self.weight_decay))
         pt = _ADAM_TYPES.get(p.dtype)
         if pt is None or not p.is_cuda or not p.is_contiguous() or p.numel() != n:
             raise ValueError("param must be a contiguous float32 or bfloat16 device tensor of the gradient's size")
         moments = _moments_of(self.m, self.v, self.m_scale, self.v_scale, n, "")
         return GsAdamwTensor(p.data_ptr(), g.data_ptr(), self.m.data_ptr(), self.v.data_ptr(), _ptr(self.m_scale),
-                             _ptr(self.v_scale), n, pt, gt, moments, self.lr, self.weight_decay)
+                             _ptr(self.v_scale), n, pt, gt, moments, float(self.lr), float(self.weight_decay))
 
 
 _ADAM_TYPES = {torch.float32: GS_TYPE_F32, torch.bfloat16: GS_TYPE_BF16}
