@@ -92,6 +92,16 @@ struct CarryArgs {
     int64_t n_in, n_out;
 };
 
+// Scales of n > 0 elements, for every n of the type (n + 31 need not fit it).
+template <typename U>
+constexpr U scale_count(U n) {
+    return ((n - 1) >> 5) + 1;
+}
+static_assert(scale_count(1u) == 1 && scale_count(32u) == 1 && scale_count(33u) == 2, "blocks of 32");
+static_assert(scale_count(0xFFFFFFE0u) == 0x7FFFFFFu && scale_count(0xFFFFFFE1u) == 0x8000000u &&
+                  scale_count(0xFFFFFFFFu) == 0x8000000u,
+              "up to the end of 32 bits");
+
 inline int64_t norm_items(int64_t n) { return (n + kNormChunk - 1) / kNormChunk; }
 inline int64_t optim_items(int64_t n) { return (n + kOptimChunk - 1) / kOptimChunk; }
 inline uint32_t optim_flags(const gs_adamw_tensor &t) {

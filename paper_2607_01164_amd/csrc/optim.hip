@@ -722,7 +722,7 @@ template <bool WHOLE, typename U>
 __device__ __forceinline__ void rows_to_lds(const CarryArray &a, uint32_t n_in, Glob<const int32_t> *source,
                                             uint32_t rows, uint32_t *lds) {
     constexpr int kEach = 4;
-    const U n = (U)n_in * a.width, scales = (n + 31) >> 5;
+    const U n = (U)n_in * a.width, scales = scale_count(n);
     const U inner = scales > 1 ? (scales - 1) * 32 - 3 : 0;  // parts below it have both words whole
     const uint32_t parts = WHOLE ? 1u : (a.width + 3) >> 2, all = rows * parts;
     for (uint32_t p0 = threadIdx.x; p0 < all; p0 += kEach * kBlock) {
