@@ -794,9 +794,12 @@ __device__ __forceinline__ void requantise(const uint32_t w[4], uint32_t &cm, ui
     cm = encode4_nearest(m, scale_of(sm));
     cv = encode4_nearest(v, scale_of(sv));
     // A positive s stays positive: 1 in every byte that was not 0 and is now.
+    // Signs are left out (NaN may have one), so that no byte carries into the
+    // next.
     const uint32_t was = __builtin_amdgcn_perm(__builtin_amdgcn_perm(w[3], w[2], 0x0C0C0602u),
                                                __builtin_amdgcn_perm(w[1], w[0], 0x0C0C0602u), 0x05040100u);
-    cv |= ((was + 0x7F7F7F7Fu) & ~(cv + 0x7F7F7F7Fu)) >> 7 & 0x01010101u;  // codes of s are below 0x80
+    const auto not_zero = [](uint32_t x) { return (x & 0x7F7F7F7Fu) + 0x7F7F7F7Fu; };  // in bit 7 of each byte
+    cv |= (not_zero(was) & ~not_zero(cv)) >> 7 & 0x01010101u;
 }
 
 // 8-bit moments: whole rows, a multiple of 32 of them, go through LDS and are

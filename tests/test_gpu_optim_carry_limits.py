@@ -1,5 +1,6 @@
 """Moments in 8 bits through a densification, at the ends of what the call
-takes: inputs of about 2^32 elements."""
+takes: inputs of about 2^32 elements, and codes that are NaN with either sign
+beside zeros and beside values that a new scale makes small."""
 import numpy as np
 import pytest
 
@@ -70,3 +71,55 @@ def test_inputs_of_about_2_to_32_elements(width, n_in):
         x = oo.e4m3(host(a[k][at])) * oo.scale_value(host(a[k + "_scale"][at // 32]))
         want = np.where(np.repeat(live, width), x, 0.0)
         oo.check_mxfp8(out[k], out[k + "_scale"], want, 0.0 * want, positive=k == "v", label=f"{width} x {n_in} {k}")
+
+
+@pytest.mark.parametrize("width", [1, 3, 4, 7])
+@pytest.mark.parametrize("nan", [0x7F, 0xFF])
+def test_nan_beside_zeros_and_small_values(nan, width):
+    """A NaN in any place of its word, either sign, in m and v: zeros beside it
+    stay zeros, and values of sqrt(v) that the new block's scale takes below
+    half its smallest number stay positive."""
+    import torch
+    r = np.random.default_rng(width)
+    n_in = 512
+    n = n_in * width
+    kinds = r.integers(0, 4, n)
+    small = np.repeat(np.arange((n + 31) // 32) % 2 == 1, 32)[:n]  # every other block has a far smaller scale
+    codes = np.where(kinds == 0, 0, np.where(kinds == 1, nan, np.where(small, r.integers(1, 8, n),
+                                                                       r.integers(0x70, 0x7F, n))))
+    scales = np.where(np.arange((n + 31) // 32) % 2 == 1, 100, 130)
+    dev = lambda x: torch.from_numpy(x.astype(np.uint8)).cuda()  # noqa: E731
+    a = {"m": dev(codes), "v": dev(codes), "m_scale": dev(scales), "v_scale": dev(scales)}
+    source = np.concatenate([r.permutation(n_in), -1 - np.arange(9), r.permutation(n_in)])
+    out = carry(width, a, n_in, source)
+    x = np.concatenate([oo.values(codes, scales).reshape(n_in, width), np.zeros((1, width))])
+    want = x[np.where(source >= 0, source, n_in)].reshape(-1)
+    assert ((want > 0) & (want < 2.0 ** -20)).sum() > 100
+    for k in "mv":
+        oo.check_mxfp8(out[k], out[k + "_scale"], want, np.zeros_like(want), positive=k == "v",
+                       label=f"{k}, NaN {nan:#x}, width {width}")
+
+
+def test_a_gradient_that_is_not_a_number_then_a_carry():
+    """NaN gradients of either sign, a step, and the moments' carry: the same
+    elements are NaN, every other keeps its kind."""
+    import torch
+    import paper_2607_01164_amd as gs
+    n = 4096
+    r = np.random.default_rng(2)
+    g = np.where(r.random(n) < 0.5, 0.0, np.exp(r.normal(size=n) * 6 - 10)).astype(np.float32)
+    bits = g.view(np.uint32)
+    bits[::5] = 0x7FC00000
+    bits[2::5] = 0xFFC00000
+    t = gs.AdamTensor.new(torch.zeros(n, device="cuda"), torch.from_numpy(g).cuda(), 0.01,
+                          moments=gs.GS_MOMENTS_MXFP8)
+    gs.gs_adamw(gs.AdamPlan([t]), step=1)
+    a = {"m": t.m, "v": t.v, "m_scale": t.m_scale, "v_scale": t.v_scale}
+    source = np.concatenate([r.permutation(n), [-1]])
+    out = carry(1, a, n, source)
+    index = np.where(source >= 0, source, 0)
+    nan = np.isnan(g[index]) & (source >= 0)
+    for k in "mv":
+        x = np.where(source >= 0, oo.values(host(a[k]), host(a[k + "_scale"]))[index], 0.0)
+        assert np.array_equal(np.isnan(x), nan)
+        oo.check_mxfp8(out[k], out[k + "_scale"], x, 0.0 * np.nan_to_num(x), positive=k == "v", label=k)
