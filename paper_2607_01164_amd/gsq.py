@@ -225,6 +225,17 @@ def _stream(stream=None) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _torch_stream(stream, device) -> torch.cuda.Stream:
+    """torch's object for a stream argument: a stream of torch's, its number,
+    or None for the current stream."""
+    if stream is None:
+        return torch.cuda.current_stream(device)
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    h = _stream(stream)
+    return torch.cuda.ExternalStream(h, device=device) if h else torch.cuda.default_stream(device)
+
+
 def _dev_f32(t: torch.Tensor, name: str, shape_tail=()) -> torch.Tensor:
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
@@ -800,7 +811,13 @@ def moment_values(m: torch.Tensor, m_scale: torch.Tensor) -> torch.Tensor:
 class AdamPlan:
     """A list of tensors laid out on the device for gs_grad_norm and
     gs_adamw. It holds the tensors' addresses, learning rates and decays:
-    make a new one when these change."""
+    make a new one when these change. It is laid out on `stream`, on which its
+    workspace is allocated too; a call on another stream has to come after
+    that, as after every other call of the plan. A plan may be dropped while
+    its calls still run: its workspace, and the memory of tensors that are the
+    current stream's when the plan is made, is not used again before they have
+    ended, on whichever streams they were made. A captured graph does not hold
+    its plan: keep it as long as the graph."""
 
     def __init__(self, tensors: Sequence[AdamTensor], device=None, stream=None):
         L = load_library()
@@ -814,9 +831,35 @@ class AdamPlan:
         need = L.gs_adamw_plan_bytes(rows, len(self.tensors))
         if need == ctypes.c_size_t(-1).value:
             raise GsError(GS_ERR_INVALID_ARGUMENT, "malformed list of tensors")
-        self.work = _alloc_bytes(need, device)
+        h, current = _stream(stream), _stream()
+        self._kept = {h, current}  # streams that the plan's memory is kept for
+        if h == current:
+            self.work = _alloc_bytes(need, device)
+        else:  # from that stream's memory, which earlier work of the current one cannot still be using
+            s = _torch_stream(stream, device)
+            with torch.cuda.stream(s):
+                self.work = _alloc_bytes(need, device)
+            self.work.record_stream(_torch_stream(None, device))
+            self._keep_tensors(s)
         self.c = GsAdamwPlan(self.work.data_ptr(), int(self.work.numel()), -1, -1, 0, 0, 0, 0)
-        _check(L.gs_plan_adamw(rows, len(self.tensors), ctypes.byref(self.c), _stream(stream)))
+        _check(L.gs_plan_adamw(rows, len(self.tensors), ctypes.byref(self.c), h))
+
+    def _keep_tensors(self, s) -> None:
+        for t in self.tensors:
+            for x in (t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale):
+                if x is not None:
+                    x.record_stream(s)
+
+    def on(self, stream=None) -> int:
+        """The number of the stream that a call of the plan is made on; the
+        plan's memory is not used again before that stream's work is done."""
+        h = _stream(stream)
+        if h not in self._kept:
+            s = _torch_stream(stream, self.work.device)
+            self.work.record_stream(s)
+            self._keep_tensors(s)
+            self._kept.add(h)
+        return h
 
 
 def alloc_adam_control(device) -> torch.Tensor:
@@ -851,7 +894,7 @@ def gs_grad_norm(plan: AdamPlan, control: torch.Tensor, max_norm: float = float(
     norm is not finite."""
     p = GsAdamwParams(beta1, beta2, 0.0, 1.0, max_norm, 0)
     _check(load_library().gs_grad_norm(ctypes.byref(plan.c), ctypes.byref(p), _control_ptr(control),
-                                       _stream(stream)))
+                                       plan.on(stream)))
 
 
 def gs_adamw(plan: AdamPlan, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, lr_scale: float = 1.0,
@@ -862,7 +905,7 @@ def gs_adamw(plan: AdamPlan, beta1: float = 0.9, beta2: float = 0.999, eps: floa
         raise ValueError("give either step or control")
     p = GsAdamwParams(beta1, beta2, eps, lr_scale, 1.0, seed)
     _check(load_library().gs_adamw(ctypes.byref(plan.c), ctypes.byref(p), 0 if step is None else step,
-                                   None if control is None else _control_ptr(control), _stream(stream)))
+                                   None if control is None else _control_ptr(control), plan.on(stream)))
 
 
 @dataclass
