@@ -64,7 +64,8 @@ enum { GS_MOMENTS_F32 = 0, GS_MOMENTS_MXFP8 = 1 };
  * types and moments may differ between the tensors of a list. m and v are
  * float32 arrays [n], or byte arrays [n] with scales [(n + 31) / 32] for
  * MXFP8 moments. Arrays may start at any element. param may be null for a
- * tensor that only counts for gs_grad_norm. Arrays do not overlap. */
+ * tensor that only counts for gs_grad_norm (of parameters that are held as
+ * they are, say): gs_adamw passes it by. Arrays do not overlap. */
 typedef struct gs_adamw_tensor {
     void *param;
     const void *grad;
@@ -87,7 +88,7 @@ typedef struct gs_adamw_plan {
     int64_t step_bytes;   /* what a step reads and writes */
     int64_t norm_bytes;   /* what the norm reads */
     int32_t count;        /* tensors */
-    int32_t updatable;    /* whether every tensor with elements has a parameter */
+    int32_t updatable;    /* whether a tensor with elements has a parameter, or none has elements */
 } gs_adamw_plan;
 
 /* What a training run keeps on the device between steps: 64 bytes, 8-byte
@@ -142,7 +143,8 @@ gs_status gs_grad_norm(const gs_adamw_plan *plan, const gs_adamw_params *params,
                        hipStream_t stream);
 
 /*
- * One step of all tensors of the plan. With a control (device memory), t,
+ * One step of all tensors of the plan that have a parameter (a plan whose
+ * tensors all have none is refused). With a control (device memory), t,
  * the clip factor and whether to do anything are what the last gs_grad_norm
  * left there, and step is ignored; with a null control t = step >= 1 and
  * the gradients are taken as they are. A gradient that is not finite makes

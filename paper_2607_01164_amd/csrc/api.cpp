@@ -1083,7 +1083,6 @@ gs_status gs_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, gs_adamw_
     AdamwSizes z;
     if (!adamw_sizes(tensors, count, &z))
         return fail(GS_ERR_INVALID_ARGUMENT, "gs_plan_adamw: null list, or a count or size out of range");
-    bool updatable = true;
     for (int64_t i = 0; i < count; ++i) {
         const gs_adamw_tensor &t = tensors[i];
         const bool pb = t.param_type == GS_TYPE_BF16, gb = t.grad_type == GS_TYPE_BF16;
@@ -1098,10 +1097,7 @@ gs_status gs_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, gs_adamw_
             return bad("lr and weight_decay must be finite and >= 0");
         if (t.n == 0) continue;
         if (!t.grad || (uintptr_t)t.grad % (gb ? 2 : 4)) return bad("grad is null or not aligned to its type");
-        if (!t.param) {
-            updatable = false;
-            continue;
-        }
+        if (!t.param) continue;
         if ((uintptr_t)t.param % (pb ? 2 : 4)) return bad("param is not aligned to its type");
         if (!t.m || !t.v || (!m8 && (((uintptr_t)t.m | (uintptr_t)t.v) % 4)))
             return bad("moments are null or not aligned to their type");
@@ -1117,7 +1113,7 @@ gs_status gs_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, gs_adamw_
     plan->step_bytes = z.step_bytes;
     plan->norm_bytes = z.norm_bytes;
     plan->count = (int32_t)count;
-    plan->updatable = updatable;
+    plan->updatable = z.items > 0 || z.norms == 0;
     return GS_OK;
 }
 
@@ -1139,7 +1135,7 @@ gs_status gs_adamw(const gs_adamw_plan *plan, const gs_adamw_params *params, int
                    const gs_adamw_control *control, hipStream_t stream) {
     gs_status st = check_adamw("gs_adamw", plan, params);
     if (st != GS_OK) return st;
-    if (!plan->updatable) return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw: a tensor of the plan has no parameter");
+    if (!plan->updatable) return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw: no tensor of the plan has a parameter");
     if (!(std::isfinite(params->eps) && params->eps >= 0x1p-126))
         return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw: eps must be finite and >= 2^-126");
     if (!(std::isfinite(params->lr_scale) && params->lr_scale >= 0.0))

@@ -741,7 +741,7 @@ def moment_scales(n: int) -> int:
 @dataclass
 class AdamTensor:
     """A tensor of an optimiser's list (include/gs_optim.h): param and grad
-    float32 or bfloat16 (param None: it only counts for the norm), moments m
+    float32 or bfloat16 (param None: it counts for the norm alone), moments m
     and v float32, or uint8 with scales m_scale and v_scale (MXFP8; v then
     holds sqrt(v)). All contiguous, on one device."""
     param: Optional[torch.Tensor]
@@ -899,8 +899,8 @@ def gs_grad_norm(plan: AdamPlan, control: torch.Tensor, max_norm: float = float(
 
 def gs_adamw(plan: AdamPlan, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, lr_scale: float = 1.0,
              step: Optional[int] = None, control: Optional[torch.Tensor] = None, seed: int = 0, stream=None) -> None:
-    """One AdamW step of all tensors of a list: step number `step` (1, 2,
-    ...), or the step that gs_grad_norm opened in `control`."""
+    """One AdamW step of all tensors of a list that have a parameter: step
+    number `step` (1, 2, ...), or the step that gs_grad_norm opened in `control`."""
     if (step is None) == (control is None):
         raise ValueError("give either step or control")
     p = GsAdamwParams(beta1, beta2, eps, lr_scale, 1.0, seed)
