@@ -107,7 +107,7 @@ typedef struct gs_adamw_control {
 /* Settings of a step. 0 <= beta < 1, eps >= 2^-126 (an element that never
  * had a gradient is divided by it), lr_scale >= 0 (a schedule's
  * factor on every tensor's learning rate), max_norm > 0 (infinity: no
- * clipping), all but max_norm finite. */
+ * clipping); eps and lr_scale finite as float32 numbers. */
 typedef struct gs_adamw_params {
     double beta1, beta2;
     double eps;

@@ -1136,10 +1136,10 @@ gs_status gs_adamw(const gs_adamw_plan *plan, const gs_adamw_params *params, int
     gs_status st = check_adamw("gs_adamw", plan, params);
     if (st != GS_OK) return st;
     if (!plan->updatable) return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw: no tensor of the plan has a parameter");
-    if (!(std::isfinite(params->eps) && params->eps >= 0x1p-126))
-        return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw: eps must be finite and >= 2^-126");
-    if (!(std::isfinite(params->lr_scale) && params->lr_scale >= 0.0))
-        return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw: lr_scale must be finite and >= 0");
+    if (!(std::isfinite((float)params->eps) && params->eps >= 0x1p-126))
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw: eps must be >= 2^-126 and finite in float32");
+    if (!(std::isfinite((float)params->lr_scale) && params->lr_scale >= 0.0))
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw: lr_scale must be >= 0 and finite in float32");
     if (control ? (uintptr_t)control % 8 != 0 : step < 1)
         return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw: without a control step must be >= 1 (a control is 8-byte "
                                              "aligned)");
