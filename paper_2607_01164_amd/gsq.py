@@ -768,16 +768,16 @@ class AdamTensor:
 
     def c(self) -> GsAdamwTensor:
         p, g = self.param, self.grad
-        n, gt = g.numel(), _ADAM_TYPES.get(g.dtype)
-        if gt is None or not g.is_cuda or not g.is_contiguous():
+        n, gt, dev = g.numel(), _ADAM_TYPES.get(g.dtype), g.get_device()
+        if gt is None or dev < 0 or not g.is_contiguous():
             raise ValueError("grad must be a contiguous float32 or bfloat16 device tensor")
         if p is None:
             return GsAdamwTensor(None, g.data_ptr(), None, None, None, None, n, gt, gt, GS_MOMENTS_F32,
                                  float(self.lr), float(self.weight_decay))
         pt = _ADAM_TYPES.get(p.dtype)
-        if pt is None or not p.is_cuda or not p.is_contiguous() or p.numel() != n:
-            raise ValueError("param must be a contiguous float32 or bfloat16 device tensor of the gradient's size")
-        moments = _moments_of(self.m, self.v, self.m_scale, self.v_scale, n, "")
+        if pt is None or p.get_device() != dev or not p.is_contiguous() or p.numel() != n:
+            raise ValueError("param must be a contiguous float32 or bfloat16 tensor of the gradient's size and device")
+        moments = _moments_of(self.m, self.v, self.m_scale, self.v_scale, n, dev, "")
         return GsAdamwTensor(p.data_ptr(), g.data_ptr(), self.m.data_ptr(), self.v.data_ptr(), _ptr(self.m_scale),
                              _ptr(self.v_scale), n, pt, gt, moments, float(self.lr), float(self.weight_decay))
 
@@ -785,19 +785,19 @@ class AdamTensor:
 _ADAM_TYPES = {torch.float32: GS_TYPE_F32, torch.bfloat16: GS_TYPE_BF16}
 
 
-def _moments_of(m, v, m_scale, v_scale, n: int, label: str) -> int:
-    """Checks the moments of n elements and returns their form."""
+def _moments_of(m, v, m_scale, v_scale, n: int, dev: int, label: str) -> int:
+    """Checks the moments of n elements on a device and returns their form."""
     if m is None or v is None or m.dtype is not v.dtype or m.dtype not in (torch.float32, torch.uint8):
         raise ValueError(f"m{label} and v{label} must both be float32 or both uint8")
-    if not (m.is_cuda and v.is_cuda and m.is_contiguous() and v.is_contiguous() and m.numel() >= n and
-            v.numel() >= n):
-        raise ValueError(f"m{label} and v{label} must be contiguous device tensors of {n} elements")
+    if not (m.get_device() == v.get_device() == dev and dev >= 0 and m.is_contiguous() and v.is_contiguous() and
+            m.numel() >= n and v.numel() >= n):
+        raise ValueError(f"m{label} and v{label} must be contiguous tensors of {n} elements on the list's device")
     if m.dtype is torch.float32:
         return GS_MOMENTS_F32
     k = moment_scales(n)
     for t, nm in ((m_scale, "m_scale"), (v_scale, "v_scale")):
-        if t is None or not t.is_cuda or t.dtype is not torch.uint8 or not t.is_contiguous() or t.numel() < k:
-            raise ValueError(f"{nm}{label} must be a contiguous uint8 device tensor of {k} elements")
+        if t is None or t.get_device() != dev or t.dtype is not torch.uint8 or not t.is_contiguous() or t.numel() < k:
+            raise ValueError(f"{nm}{label} must be a contiguous uint8 tensor of {k} elements on the moments' device")
     return GS_MOMENTS_MXFP8
 
 
@@ -880,10 +880,10 @@ def read_adam_control(control: torch.Tensor) -> dict:
     return {k: v.item() for k, v in adam_control_views(control.cpu()).items()}
 
 
-def _control_ptr(control: torch.Tensor) -> int:
-    if not control.is_cuda or control.numel() * control.element_size() < ADAM_CONTROL_BYTES or \
+def _control_ptr(plan: AdamPlan, control: torch.Tensor) -> int:
+    if control.get_device() != plan.work.get_device() or control.numel() * control.element_size() < ADAM_CONTROL_BYTES or \
             control.data_ptr() % 8:
-        raise ValueError("control must be a device buffer of at least 64 bytes, 8-byte aligned")
+        raise ValueError("control must be a buffer of at least 64 bytes, 8-byte aligned, on the plan's device")
     return control.data_ptr()
 
 
@@ -893,7 +893,7 @@ def gs_grad_norm(plan: AdamPlan, control: torch.Tensor, max_norm: float = float(
     clip factor, step count and bias corrections, or a skipped step when the
     norm is not finite."""
     p = GsAdamwParams(beta1, beta2, 0.0, 1.0, max_norm, 0)
-    _check(load_library().gs_grad_norm(ctypes.byref(plan.c), ctypes.byref(p), _control_ptr(control),
+    _check(load_library().gs_grad_norm(ctypes.byref(plan.c), ctypes.byref(p), _control_ptr(plan, control),
                                        plan.on(stream)))
 
 
@@ -905,7 +905,7 @@ def gs_adamw(plan: AdamPlan, beta1: float = 0.9, beta2: float = 0.999, eps: floa
         raise ValueError("give either step or control")
     p = GsAdamwParams(beta1, beta2, eps, lr_scale, 1.0, seed)
     _check(load_library().gs_adamw(ctypes.byref(plan.c), ctypes.byref(p), 0 if step is None else step,
-                                   None if control is None else _control_ptr(control), plan.on(stream)))
+                                   None if control is None else _control_ptr(plan, control), plan.on(stream)))
 
 
 @dataclass
@@ -939,8 +939,9 @@ class AdamCarry:
             if not 1 <= w <= 64:
                 raise ValueError("width must lie in [1, 64]")
             n_in, n_out = a.m.numel() // w, a.m_out.numel() // w
-            form = _moments_of(a.m, a.v, a.m_scale, a.v_scale, n_in * w, "")
-            if _moments_of(a.m_out, a.v_out, a.m_scale_out, a.v_scale_out, n_out * w, "_out") != form:
+            dev = self.arrays[0].m.get_device()
+            form = _moments_of(a.m, a.v, a.m_scale, a.v_scale, n_in * w, dev, "")
+            if _moments_of(a.m_out, a.v_out, a.m_scale_out, a.v_scale_out, n_out * w, dev, "_out") != form:
                 raise ValueError("input and output moments must have the same form")
             self.in_rows, self.out_rows = min(self.in_rows, n_in), min(self.out_rows, n_out)
             rows.append(GsAdamwRows(_ptr(a.m), _ptr(a.v), _ptr(a.m_scale), _ptr(a.v_scale), _ptr(a.m_out),
@@ -955,6 +956,8 @@ def gs_adamw_carry(carry: AdamCarry, n_in: int, source: torch.Tensor, n_out: int
         raise ValueError("the arrays hold fewer rows")
     if not source.is_cuda or source.dtype != torch.int32 or not source.is_contiguous() or source.numel() < n_out:
         raise ValueError("source must be a contiguous int32 device tensor with a slot per output row")
+    if carry.arrays and source.get_device() != carry.arrays[0].m.get_device():
+        raise ValueError("source and the arrays must be on one device")
     _check(load_library().gs_adamw_carry(carry.c, len(carry.arrays), n_in, source.data_ptr(), n_out,
                                          _stream(stream)))
 

@@ -57,7 +57,7 @@ def streams(monkeypatch):
     monkeypatch.setattr(gsq, "_alloc_bytes", alloc)
     monkeypatch.setattr(gsq, "_stream", lambda s=None: 1 if s is None else s)
     monkeypatch.setattr(gsq, "_torch_stream", lambda s, device: 1 if s is None else s, raising=False)
-    monkeypatch.setattr(gsq, "_control_ptr", lambda c: 8)
+    monkeypatch.setattr(gsq, "_control_ptr", lambda *a: 8)
     monkeypatch.setattr(torch.cuda, "stream", Entered)
     return made
 
