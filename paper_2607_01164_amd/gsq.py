@@ -841,6 +841,7 @@ class AdamPlan:
                 self.work = _alloc_bytes(need, device)
             self.work.record_stream(_torch_stream(None, device))
             self._keep_tensors(s)
+        self.device = self.work.get_device()
         self.c = GsAdamwPlan(self.work.data_ptr(), int(self.work.numel()), -1, -1, 0, 0, 0, 0)
         _check(L.gs_plan_adamw(rows, len(self.tensors), ctypes.byref(self.c), h))
 
@@ -881,7 +882,7 @@ def read_adam_control(control: torch.Tensor) -> dict:
 
 
 def _control_ptr(plan: AdamPlan, control: torch.Tensor) -> int:
-    if control.get_device() != plan.work.get_device() or control.numel() * control.element_size() < ADAM_CONTROL_BYTES or \
+    if control.get_device() != plan.device or control.numel() * control.element_size() < ADAM_CONTROL_BYTES or \
             control.data_ptr() % 8:
         raise ValueError("control must be a buffer of at least 64 bytes, 8-byte aligned, on the plan's device")
     return control.data_ptr()

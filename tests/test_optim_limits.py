@@ -70,7 +70,7 @@ def test_arrays_on_several_devices(form, where):
 @pytest.mark.parametrize("where", [1, -1], ids=["another", "host"])
 def test_control_on_another_device(where):
     class Plan:
-        c, work = plan(), Tensor(torch.uint8, 0)
+        c, device = plan(), 0
 
         def on(self, stream):
             return 0
@@ -79,3 +79,22 @@ def test_control_on_another_device(where):
         gs.gs_grad_norm(Plan(), Tensor(torch.uint8, where))
     with pytest.raises(ValueError):
         gs.gs_adamw(Plan(), control=Tensor(torch.uint8, where))
+
+
+def test_moment_values_are_the_oracles():
+    """What codes and scales stand for, from an empty tensor to blocks that end
+    early, with the scale of a new tensor (byte 0) and both signs of NaN."""
+    import numpy as np
+    import optim_oracle as oo
+    r = np.random.default_rng(1)
+    for n in (0, 1, 31, 32, 33, 1000):
+        codes = r.integers(0, 256, n).astype(np.uint8)
+        scales = r.integers(1, 247, gs.moment_scales(n)).astype(np.uint8)
+        got = gs.moment_values(torch.from_numpy(codes), torch.from_numpy(scales))
+        assert got.dtype == torch.float32 and got.shape == (n,)
+        want = oo.values(codes, scales).astype(np.float32)
+        np.testing.assert_array_equal(got.numpy(), want)
+    zero = gs.moment_values(torch.zeros(40, dtype=torch.uint8), torch.zeros(2, dtype=torch.uint8))
+    assert zero.shape == (40,) and not zero.any()
+    rows = torch.full((2, 32), 0x38, dtype=torch.uint8)  # 1.0, of any shape
+    assert gs.moment_values(rows, torch.tensor([0, 130], dtype=torch.uint8)).tolist() == [2.0 ** -127] * 32 + [8.0] * 32

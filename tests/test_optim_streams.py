@@ -21,6 +21,9 @@ class Memory:
     def data_ptr(self):
         return 1 << 20
 
+    def get_device(self):
+        return 0
+
     def numel(self):
         return 1 << 20
 
