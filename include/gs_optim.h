@@ -28,10 +28,11 @@
  * up with probability equal to the share of the way ((k + 1/2) / 2^16 with
  * 16 random bits k). Rounding to the nearest would not do: with 1 - beta2 =
  * 0.001 a falling s moves by a hundredth of the grid's spacing a step, and
- * would never leave its place. A positive s never becomes 0 (it becomes the
- * smallest value of its block's grid), so that a remembered m is not divided
- * by a forgotten v. Values that are not finite are kept as NaN. All-zero
- * bytes are the state of a new tensor.
+ * would never leave its place. A positive s is never rounded to 0 (it becomes
+ * the smallest value of its block's grid), so that a remembered m is not
+ * divided by a forgotten v. What float32 itself forgets is forgotten: s s is 0
+ * for an s of 2^-75 or less, far below any eps in use. Values that are not
+ * finite are kept as NaN. All-zero bytes are the state of a new tensor.
  *
  * bfloat16 parameters are rounded up or down with the same kind of odds (16
  * random bits), since most updates are below half their spacing.
