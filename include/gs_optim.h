@@ -39,8 +39,9 @@
  *
  * The random bits of an element are a function of (seed, t, the tensor's
  * place in the list, the element's index) alone, so the same calls give
- * bit-identical results. With mix(x): x ^= x >> 16, x *= 0x7feb352d,
- * x ^= x >> 15, x *= 0x846ca68b, x ^= x >> 16 (32 bits):
+ * bit-identical results. With mix(x), an integer hash of low bias that
+ * C. Wellons published (32 bits): x ^= x >> 16, x *= 0x7feb352d,
+ * x ^= x >> 15, x *= 0x846ca68b, x ^= x >> 16:
  *   key  = mix(place + 0x9e3779b9), then key = mix(key ^ w) for w = t's low
  *          and high words, seed's low and high words, the index's high word
  *   bits = mix(index's low word ^ key)
@@ -125,8 +126,8 @@ size_t gs_adamw_plan_bytes(const gs_adamw_tensor *tensors, int64_t count);
 /*
  * Lays a list out for gs_grad_norm and gs_adamw. The host array is read
  * before the call returns; the plan holds the arrays' addresses, learning
- * rates and decays, so it is made again when one of these changes, and kept
- * as long as none does. Work of a plan: calls that share one follow each
+ * rates and decays, so it is made again when one of these changes (lr_scale
+ * changes all rates without that), and kept as long as none does. Work of a plan: calls that share one follow each
  * other.
  */
 gs_status gs_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, gs_adamw_plan *plan, hipStream_t stream);
@@ -138,7 +139,9 @@ gs_status gs_plan_adamw(const gs_adamw_tensor *tensors, int64_t count, gs_adamw_
  * bias corrections of the new t are set; otherwise the step is skipped:
  * skipped grows by one and a gs_adamw with this control changes nothing. Sums
  * in float64 in an order that depends on the plan alone: bit-identical
- * between calls. Only beta1, beta2 and max_norm of the settings are used.
+ * between calls. Only beta1, beta2 and max_norm of the settings are used;
+ * give gs_adamw the same beta1 and beta2: the corrections left here are of
+ * these, the averages of its own.
  */
 gs_status gs_grad_norm(const gs_adamw_plan *plan, const gs_adamw_params *params, gs_adamw_control *control,
                        hipStream_t stream);

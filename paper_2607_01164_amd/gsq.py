@@ -892,7 +892,7 @@ def gs_grad_norm(plan: AdamPlan, control: torch.Tensor, max_norm: float = float(
                  beta2: float = 0.999, stream=None) -> None:
     """The global gradient norm of a list, which opens a step of the control:
     clip factor, step count and bias corrections, or a skipped step when the
-    norm is not finite."""
+    norm is not finite. Give gs_adamw the same beta1 and beta2."""
     p = GsAdamwParams(beta1, beta2, 0.0, 1.0, max_norm, 0)
     _check(load_library().gs_grad_norm(ctypes.byref(plan.c), ctypes.byref(p), _control_ptr(plan, control),
                                        plan.on(stream)))
