@@ -556,8 +556,14 @@ AdamwPlanLayout adamw_plan_layout(void *work, int64_t items, int64_t norms) {
     return l;
 }
 
-// Sizes from which a call's data are past the 256 MB of the last-level
-// cache, so that keeping them there only drives out what could be read again.
+// Bytes that a call reads and writes from which it keeps nothing in the caches
+// (a step counts parameters and moments twice). It is the traffic of a call and
+// not the list's size that fills the 256 MB of the last-level cache. Measured
+// with float32 lists, two others of the same size stepped in between: 134 MB
+// 20.7 us kept, 23.1 not; 202 MB 34.9, 33.4; 269 MB 51, 44; 403 MB 75, 65; 8-bit
+// and bfloat16 lists alike, norms 96 MB 20.3, 20.2; 240 MB 47.5, 42.4. A list
+// that is stepped with nothing in between, which a training loop does not do,
+// is 6 to 10 % faster kept, up to 500 MB.
 constexpr int64_t kOnceBytes = (int64_t)256 << 20;
 
 gs_status check_adamw(const char *who, const gs_adamw_plan *plan, const gs_adamw_params *params) {

@@ -8,8 +8,9 @@
 namespace gs {
 
 constexpr int64_t kOptimChunk = 1024;  // elements of an item at most: a multiple of 32 that divides 2^32
-// Elements of a NormItem at most: with 4096 the norm of 0.3 to 1 M Gaussians
-// took 0.7 to 1.4 us longer (more sums to leave), below that it is as fast.
+// Elements of a NormItem at most: with 4096 the norm of 0.26 to 1 M Gaussians
+// takes 0.6 to 1.2 us longer (more sums to leave), that of fewer as long, and
+// that of 267 M bfloat16 elements 4 % less.
 constexpr int64_t kNormChunk = 16384;
 constexpr uint32_t kCarryMost = 4096;  // elements of a workgroup's rows in the carry at most
 
@@ -77,9 +78,9 @@ struct CarryArray {
     uint32_t width, rows, over, over_parts;
     uint32_t moments8, pad;
 };
-// 8-bit rows: 4 parts of a row a thread (for 2 M Gaussians 45 us; 50 with 2
-// parts, and with 8, which leave fewer workgroups resident); 32-bit rows: one
-// pass of 4 elements a thread.
+// 8-bit rows: 4 parts of a row a thread (2 M Gaussians take a tenth longer
+// with 2 parts, and with 8, which leave fewer workgroups resident; 262144 take
+// 0.9 us less with 2); 32-bit rows: one pass of 4 elements a thread.
 inline uint32_t carry_rows(uint32_t width, bool moments8) {
     const uint32_t most = moments8 ? (width < 4 ? 1024 * width : kCarryMost) : 1024;
     const uint32_t rows = most / width / 32 * 32;

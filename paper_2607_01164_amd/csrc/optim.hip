@@ -2,8 +2,9 @@
 // float32 or MXFP8 moments, the global gradient norm, and moments through a
 // densification's source map.
 //
-// Everything is elementwise or a sum, and bound by HBM: a large device copy
-// moves 5.0 TB/s on this part, an addition of two arrays 5.9. A list is cut
+// Everything is elementwise or a sum, and bound by HBM: on this part a device
+// copy of 1 to 4 GiB moves 4.9 to 5.2 TB/s, an addition of two such arrays 5.5
+// to 5.9, a fill 6.9, and these kernels' large lists 6.0 to 6.5. A list is cut
 // into pieces ("items") of at most one workgroup's work, and one launch
 // covers all tensors: a workgroup reads its item's record (addresses, length,
 // rates) with scalar loads and needs nothing else of the list.
@@ -28,7 +29,8 @@ typedef uint16_t h1a __attribute__((aligned(1)));
 
 constexpr int kFill = 24;  // tensors whose pieces one launch of k_fill_items writes: 2 KB of arguments
 // Neighbouring items that one XCD takes: 267 M elements with 8-bit moments
-// take 712 us with 32 or 64, 750 with 8, 725 with 256, 720 without.
+// take as long with 64, 2 % longer with 256, 3 % without, 5 % with 8; in
+// bfloat16 with float32 moments 1 % less with 64, with 256 and without.
 constexpr uint32_t kXcdItems = 32;
 constexpr int64_t kMaxGrid = 1 << 23;  // workgroups of a launch at most: 2^31 threads
 
@@ -414,7 +416,7 @@ __device__ __forceinline__ void step_quad(const OptimItem &it, const StepConst &
 // An item is one pass of the workgroup. In a shorter last one the lanes past
 // the end stay: those of its last block take part in the block's maximum. Its
 // lanes of four elements take vectors as well: 8000 tensors of 2047 elements
-// 81 us, 119 one by one (float32; 100 elements each 12.6, 10.7).
+// 82 us, 118 one by one (float32; 100 elements each 10.7, 9.0).
 template <bool PB, bool GB, bool M8, bool ONCE>
 __device__ __forceinline__ void step_item(const OptimItem &it, const StepConst &c) {
     static_assert(kOptimChunk == 4 * kBlock, "an item is four elements a thread");
@@ -436,15 +438,13 @@ __device__ __forceinline__ void step_item(const OptimItem &it, const StepConst &
 // lanes; 7 or 8 workgroups a CU hide the loads, and longer items with the
 // next pass loaded ahead were no faster (large lists 2 to 15 % slower).
 // float32 moments move 22 to 28 bytes an element, 8-bit ones 10 to 16, for
-// about 25 and 50 operations. ONCE (lists past the last-level cache): loads
-// and stores keep nothing: 2 M Gaussians with 8-bit moments 65 us instead of
-// 75; a list that the cache holds is faster without (262 k Gaussians 15.7 us,
-// 17.5 with). Measured, a step among others:
+// about 25 and 50 operations. ONCE (steps that move much, by the rule of the
+// caller): loads and stores keep nothing. Measured, a step among others:
 //   4096 Gaussians (49 k elements)        2.6 us
 //   262144 Gaussians (3.1 M)             13.9 us  6.3 TB/s
-//   2097152 Gaussians, 8 bits (25 M)     62.7 us  6.5 TB/s
-//   48 tensors (267 M), bf16             970 us   6.1 TB/s
-//   the same, float32 with 8 bits        694 us   6.2 TB/s
+//   2097152 Gaussians, 8 bits (25 M)     62.8 us  6.5 TB/s
+//   48 tensors (267 M), bf16             971 us   6.0 TB/s
+//   the same, float32 with 8 bits        693 us   6.2 TB/s
 // so large lists run at the memory's rate; what bounds a small one is the
 // launch and two trips to memory, the item's record and the elements.
 template <bool CONTROL, bool ONCE>
@@ -584,9 +584,9 @@ __device__ __forceinline__ bool leave_sum(const NormWork &work, double sum) {
 // never looks infinite, and the additions cost less than the loads. At most
 // 2048 workgroups (all that are resident) go over the items, and the last one
 // to finish adds their sums, so the norm is one launch. Measured:
-//   4096 Gaussians (49 k elements, float32)    5.3 us
-//   524288 Gaussians (6.3 M, float32)          9.3 us
-//   48 tensors (267 M, bf16)                  85 us    6.3 TB/s
+//   4096 Gaussians (49 k elements, float32)    5.4 us
+//   524288 Gaussians (6.3 M, float32)          9.2 us    2.7 TB/s
+//   48 tensors (267 M, bf16)                  84 us      6.3 TB/s
 // Small lists are bound by a chain of trips to memory: item, elements, the
 // sum's exchange, the count, the sums.
 template <bool ONCE>
@@ -854,12 +854,15 @@ __device__ __forceinline__ void carry_mxfp8(const CarryArray &a, uint32_t n_in, 
 // rows of one array. 16 bytes an element with float32 moments, 4 with 8-bit
 // ones, and the map. The outputs keep nothing in the caches: what is carried
 // is read once, and the inputs of neighbouring workgroups share lines (2 M
-// Gaussians with 8-bit moments 35 us, 44 with ordinary stores; loads that
-// keep nothing lose it again). Measured, a tenth pruned and a fifth added:
+// Gaussians with 8-bit moments take 1.28 times as long with ordinary stores,
+// 1.25 with loads that keep nothing). Measured, a tenth pruned and a fifth
+// added:
 //   262144 Gaussians, float32 moments     9.7 us  5.3 TB/s
-//   2097152 Gaussians, 8-bit moments     32 us    3.5 TB/s
-// The 8-bit form waits: for the map, then for the codes that it points to;
-// its arithmetic (32 operations an element) takes no time beside that.
+//   2097152 Gaussians, 8-bit moments     33 us    3.5 TB/s of what is needed
+// The 8-bit form reads 98 MB and writes 57 for the 113 that it needs, most of
+// the rest the map, which the workgroups of each array read again: 4.7 TB/s,
+// near a copy's rate. Its arithmetic (32 operations an element) takes no time
+// beside that.
 __global__ __launch_bounds__(kBlock) void k_carry(CarryArgs a, const int32_t *source) {
     __shared__ alignas(16) uint32_t lds[kCarryMost];
     const uint32_t block = a.block0 + xcd_group<kXcdItems>(blockIdx.x, gridDim.x);
