@@ -14,7 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libgsq.so")
 SOURCES = ["api.cpp", "primitives.hip", "index.hip", "sample.hip", "backward.hip", "train.hip", "densify.hip", "gauss_major.hip",
-           "optim.hip"]
+           "optim.hip", "shares.hip", "evict.hip", "draw.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = os.environ.get("GS_OFFLOAD_ARCH", "gfx950")
 

@@ -11,6 +11,7 @@
 #include <string>
 #include <vector>
 
+#include "budget.h"
 #include "internal.h"
 #include "optim.h"
 #include "radix.h"
@@ -582,7 +583,7 @@ extern "C" {
 
 const char *gs_last_error(void) { return g_err.c_str(); }
 
-int gs_version(void) { return 110; }
+int gs_version(void) { return 120; }
 
 void gs_profile_enable(int on) { g_prof_on = on != 0; }
 
@@ -1193,6 +1194,128 @@ gs_status gs_adamw_carry(const gs_adamw_rows *arrays, int32_t count, int64_t n_i
     if (!source || (uintptr_t)source % 4)
         return fail(GS_ERR_INVALID_ARGUMENT, "gs_adamw_carry: source is null or not aligned to its type");
     GS_TRY(launch_adamw_carry(arrays, count, n_in, source, n_out, stream), "gs_adamw_carry");
+    return GS_OK;
+}
+
+// ---------------------------------------------------------------------------
+// A budget of Gaussians (include/gs_budget.h).
+
+static const int64_t kGaussMost = (int64_t)1 << 31;
+
+size_t gs_shares_work_bytes(const gs_index *index, const gs_query *query) {
+    std::string why;
+    if (!index || index->n_pairs < 0 || !query_valid(query, &why)) return (size_t)-1;
+    return shares_layout(nullptr, query_count(query), query->kind == GS_QUERY_GRID).bytes;
+}
+
+gs_status gs_shares(const gs_gaussians *gauss, const gs_index *index, const gs_query *query, const void *plan,
+                    size_t plan_bytes, const float *influence, const float *gain, float decay, float *score,
+                    void *work, size_t work_bytes, hipStream_t stream) {
+    gs_status st = check_index("gs_shares", gauss, index);
+    if (st != GS_OK) return st;
+    if ((st = check_query("gs_shares", index, query)) != GS_OK) return st;
+    const int64_t n = gauss->n, nq = query_count(query);
+    if (nq > 0 && !influence) return fail(GS_ERR_INVALID_ARGUMENT, "gs_shares: influence is null");
+    if (n > 0 && !score) return fail(GS_ERR_INVALID_ARGUMENT, "gs_shares: score is null");
+    if (!(decay >= 0.0f) || !std::isfinite(decay))
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_shares: decay must be finite and >= 0");
+    const GridParams gp = grid_params(&index->grid);
+    const QueryParams qp = query_params(query, &index->grid);
+    const bool grid = query->kind == GS_QUERY_GRID;
+    const SharesWork sw = shares_layout(work, nq, grid);
+    if (!work || work_bytes < sw.bytes || !aligned(work))
+        return fail(GS_ERR_WORKSPACE, "gs_shares: workspace needs %zu bytes, 256-byte aligned (got %zu)", sw.bytes,
+                    work_bytes);
+    Plan p{};
+    if (!grid) {
+        const size_t need = plan_layout(nullptr, nq, gp.ncells).bytes;
+        if (!plan || plan_bytes < need || !aligned(plan))
+            return fail(GS_ERR_WORKSPACE, "gs_shares: plan needs %zu bytes (got %zu)", need, plan_bytes);
+        p = plan_layout(const_cast<void *>(plan), nq, gp.ncells);
+    }
+    const IndexWork w = index_layout(index->work, n, &index->grid, index->capacity);
+    const float T = cutoff_T(index->tau);
+    const SharesExact exact{gauss->mean, gauss->scale, gauss->rot, 2.0 * std::log(1.0 / (double)index->tau)};
+    GS_TRY(launch_shares(qp, gp, bwd_geom(gp, qp, T), w.rec, w.box, w.gorder, n, p.order, p.point_off, p.res.pos, T,
+                         exact, influence, gain, decay, score, sw, stream),
+           "gs_shares");
+    return GS_OK;
+}
+
+static bool params_valid(const gs_params *p) {
+    return p && p->mean && p->log_scale && p->rot && p->value_logit && p->weight_logit;
+}
+
+size_t gs_evict_work_bytes(int64_t n) { return n < 0 || n >= kGaussMost ? (size_t)-1 : evict_work_bytes(n); }
+
+gs_status gs_evict(const gs_params *in, int64_t n, const float *score, const uint8_t *pinned, int64_t budget,
+                   const gs_params *out, int32_t *source, float *score_out, void *work, size_t work_bytes,
+                   hipStream_t stream) {
+    if (n < 0 || n >= kGaussMost || budget < 0 || budget >= kGaussMost)
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_evict: counts out of range");
+    const int64_t keep = budget < n ? budget : n;
+    if (keep == 0) return GS_OK;
+    if (!params_valid(in) || !score) return fail(GS_ERR_INVALID_ARGUMENT, "gs_evict: input arrays are null");
+    if (!params_valid(out) || !source) return fail(GS_ERR_INVALID_ARGUMENT, "gs_evict: output arrays are null");
+    const size_t need = evict_work_bytes(n);
+    if (!work || work_bytes < need || !aligned(work))
+        return fail(GS_ERR_WORKSPACE, "gs_evict: workspace needs %zu bytes, 256-byte aligned (got %zu)", need,
+                    work_bytes);
+    GS_TRY(launch_evict(*in, n, score, pinned, keep, *out, source, score_out, work, stream), "gs_evict");
+    return GS_OK;
+}
+
+static bool draw_sizes_valid(int64_t rows, int64_t n, int64_t draws) {
+    const int64_t most = (int64_t)1 << 40;
+    return rows >= 0 && rows < kGaussMost && n >= 0 && n < kGaussMost && draws >= 0 && draws < kGaussMost &&
+           (rows == 0 || (n <= (most - 1) / rows && draws <= (most - 1) / rows));
+}
+
+size_t gs_draw_work_bytes(int64_t rows, int64_t n, int64_t draws) {
+    return draw_sizes_valid(rows, n, draws) ? draw_work_bytes(rows, n, draws) : (size_t)-1;
+}
+
+gs_status gs_draw(int64_t rows, int64_t n, const void *scores, int64_t stride, const int32_t *lengths,
+                  const gs_draw_params *params, int64_t draws, const double *uniform, int32_t *ids, float *prob,
+                  void *work, size_t work_bytes, hipStream_t stream) {
+    if (!draw_sizes_valid(rows, n, draws)) return fail(GS_ERR_INVALID_ARGUMENT, "gs_draw: sizes out of range");
+    if (!params) return fail(GS_ERR_INVALID_ARGUMENT, "gs_draw: params is null");
+    const gs_draw_params p = *params;
+    if (!(std::isfinite(p.temperature) && p.temperature >= 0.0))
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_draw: temperature must be finite and >= 0");
+    if (!(p.top_p >= 0.0 && p.top_p <= 1.0) || !(p.min_p >= 0.0 && p.min_p <= 1.0))
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_draw: top_p and min_p must lie in [0, 1]");
+    if (p.top_k < 0) return fail(GS_ERR_INVALID_ARGUMENT, "gs_draw: top_k must be >= 0");
+    if (p.type != GS_SCORE_F32 && p.type != GS_SCORE_BF16)
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_draw: unknown type of scores");
+    if (stride < n || stride >= (int64_t)1 << 40 ||
+        (rows > 1 && stride > (((int64_t)1 << 60) / (rows - 1))))
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_draw: stride must be at least n");
+    if (rows == 0 || draws == 0) return GS_OK;
+    if ((n > 0 && !scores) || !uniform || !ids) return fail(GS_ERR_INVALID_ARGUMENT, "gs_draw: null array");
+    const size_t need = draw_work_bytes(rows, n, draws);
+    if (!work || work_bytes < need || !aligned(work))
+        return fail(GS_ERR_WORKSPACE, "gs_draw: workspace needs %zu bytes, 256-byte aligned (got %zu)", need,
+                    work_bytes);
+    GS_TRY(launch_draw(rows, n, scores, stride, lengths, p, draws, uniform, ids, prob, work, stream), "gs_draw");
+    return GS_OK;
+}
+
+size_t gs_split_work_bytes(int64_t n) {
+    return n < 0 || n >= kGaussMost ? (size_t)-1 : align_up(sizeof(uint32_t) * (size_t)(n > 0 ? n : 1));
+}
+
+gs_status gs_split(const gs_params *set, int64_t n, const int32_t *ids, int64_t count, int32_t *source, float *score,
+                   void *work, size_t work_bytes, hipStream_t stream) {
+    if (n < 0 || count < 0 || n >= kGaussMost || count >= kGaussMost - n)
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_split: counts out of range");
+    if (count == 0) return GS_OK;
+    if (!params_valid(set) || !ids) return fail(GS_ERR_INVALID_ARGUMENT, "gs_split: null array");
+    const size_t need = gs_split_work_bytes(n);
+    if (!work || work_bytes < need || !aligned(work))
+        return fail(GS_ERR_WORKSPACE, "gs_split: workspace needs %zu bytes, 256-byte aligned (got %zu)", need,
+                    work_bytes);
+    GS_TRY(launch_split(*set, n, ids, count, source, score, (uint32_t *)work, stream), "gs_split");
     return GS_OK;
 }
 

@@ -246,63 +246,6 @@ __device__ __forceinline__ float bperm_f(uint32_t src, float v) {
     return __int_as_float(__builtin_amdgcn_ds_bpermute((int)src, __float_as_int(v)));
 }
 
-// The voxels a Gaussian's rows can hold on a grid: x0 .. x1 of its box, and
-// the rows y0 .. y0 + ny - 1, z0 .. z0 + nz - 1 that its cutoff ellipsoid
-// reaches. Q >= (U22 dz)^2, and over x and z Q is at least dy^2 U11^2 / (1 +
-// (U12 / U22)^2), which bound |dz| and |dy|; both ranges are cut to the box.
-// (The box's rows are whole cells; most of them miss the ellipsoid.)
-struct GridRows {
-    uint32_t x0, x1, y0, ny, z0, nz;
-};
-
-__device__ __forceinline__ GridRows grid_rows(const Record &r, const CellBox &b, const QueryParams &q,
-                                              const GridParams &g, const BwdGeom &bg) {
-    const uint32_t rx = (uint32_t)(q.dims[0] / g.cells[0]), ry = (uint32_t)(q.dims[1] / g.cells[1]);
-    const uint32_t rz = (uint32_t)(q.dims[2] / g.cells[2]);
-    GridRows o;
-    o.x0 = (uint32_t)b.lo.x * rx;
-    o.x1 = ((uint32_t)b.hi.x + 1u) * rx - 1u;
-    const float rt = __builtin_sqrtf(bg.T2);
-    const float t = r.f2.y / r.f2.z;
-    const float hy = rt * __builtin_sqrtf(fmaf_(t, t, 1.0f)) / r.f2.x, hz = rt / r.f2.z;
-    // rows whose centre lo + (v + 1/2) vsz lies in [mu - h, mu + h]; a range
-    // that is not a number leaves the box's
-    auto cut = [](float mu, float h, float lo, float iv, float slack, uint32_t v0, uint32_t v1, uint32_t &first,
-                  uint32_t &n) {
-        const float a = fmaxf(ceilf((mu - h - lo) * iv - 0.5f - slack), (float)v0);
-        const float c = fminf(floorf((mu + h - lo) * iv - 0.5f + slack), (float)v1);
-        const bool some = a <= c;
-        first = some ? (uint32_t)a : v0;
-        n = some ? (uint32_t)(c - a) + 1u : 0u;
-    };
-    cut(r.f0.y, hy, g.lo[1], bg.ivsz[1], bg.vslack[1], (uint32_t)b.lo.y * ry, ((uint32_t)b.hi.y + 1u) * ry - 1u, o.y0,
-        o.ny);
-    cut(r.f0.z, hz, g.lo[2], bg.ivsz[2], bg.vslack[2], (uint32_t)b.lo.z * rz, ((uint32_t)b.hi.z + 1u) * rz - 1u, o.z0,
-        o.nz);
-    return o;
-}
-
-// Voxel row (vy, vz) of a Gaussian with voxels x0 .. x1: the voxels within the
-// cutoff T2 (a run; first and number), and the row's y, z.
-__device__ __forceinline__ uint32_t grid_row(const Record &r, uint32_t x0, uint32_t x1, uint32_t vy, uint32_t vz,
-                                             const QueryParams &q, const GridParams &g, const BwdGeom &bg,
-                                             uint32_t &first, float &py, float &pz) {
-    first = 0;
-    py = g.lo[1] + ((float)vy + 0.5f) * q.vsz[1];
-    pz = g.lo[2] + ((float)vz + 0.5f) * q.vsz[2];
-    const float dy = py - r.f0.y, dz = pz - r.f0.z;
-    float xl, xh;
-    if (!slab_xrange(r, dy, dy, dz, dz, bg.T2, xl, xh)) return 0;
-    // voxels vx of the box with lo + (vx + 1/2) vsz in [xl, xh]
-    const float vmin = (float)x0, vmax = (float)x1;
-    const float a = fminf(fmaxf((xl - g.lo[0]) * bg.ivsz[0] - 0.5f - bg.vslack[0], vmin), vmax + 1.0f);
-    const float b = fminf(fmaxf((xh - g.lo[0]) * bg.ivsz[0] - 0.5f + bg.vslack[0], vmin - 1.0f), vmax);
-    const float v0 = ceilf(a), v1 = floorf(b);
-    if (v1 < v0) return 0;
-    first = (uint32_t)v0;
-    return (uint32_t)(v1 - v0) + 1u;
-}
-
 // PACK consecutive Gaussians of gorder per wavefront. The rows of the
 // wave's Gaussians are listed one Gaussian after the other and taken 64 at
 // a time, lane l setting up row l of the batch (its x-range from the

@@ -1,5 +1,5 @@
-"""Python binding of the C-ABI in include/gs.h, include/gs_train.h and
-include/gs_optim.h (ctypes).
+"""Python binding of the C-ABI in include/gs.h, include/gs_train.h,
+include/gs_optim.h and include/gs_budget.h (ctypes).
 
 Argument marshalling only: every step of sampling runs in the HIP library
 libgsq.so. torch provides device memory and the stream. Importing this module
@@ -36,13 +36,17 @@ EXPORTED = ("gs_query_size", "gs_index_work_bytes", "gs_build_index", "gs_plan_b
             "gs_loss_work_bytes", "gs_loss", "gs_densify_work_bytes", "gs_densify",
             "gs_sample_gaussian_major_work_bytes", "gs_sample_gaussian_major", "gs_backward_pair_count",
             "gs_sample_pair_counts", "gs_sample_backward_noalloc", "gs_plan_queries", "gs_sample_planned",
-            "gs_adamw_plan_bytes", "gs_plan_adamw", "gs_grad_norm", "gs_adamw", "gs_adamw_carry")
+            "gs_adamw_plan_bytes", "gs_plan_adamw", "gs_grad_norm", "gs_adamw", "gs_adamw_carry",
+            "gs_shares_work_bytes", "gs_shares", "gs_evict_work_bytes", "gs_evict", "gs_draw_work_bytes", "gs_draw",
+            "gs_split_work_bytes", "gs_split")
 
 GS_TYPE_F32 = 0
 GS_TYPE_BF16 = 1
 GS_MOMENTS_F32 = 0
 GS_MOMENTS_MXFP8 = 1
 GS_ADAMW_ROWS_MAX = 16
+GS_SCORE_F32 = 0
+GS_SCORE_BF16 = 1
 MOMENT_BLOCK = 32  # elements that share a scale of MXFP8 moments
 
 
@@ -114,6 +118,11 @@ class GsAdamwRows(ctypes.Structure):
                 ("v_scale", ctypes.c_void_p), ("m_out", ctypes.c_void_p), ("v_out", ctypes.c_void_p),
                 ("m_scale_out", ctypes.c_void_p), ("v_scale_out", ctypes.c_void_p), ("width", ctypes.c_int32),
                 ("moments", ctypes.c_int32)]
+
+
+class GsDrawParams(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_double), ("top_p", ctypes.c_double), ("min_p", ctypes.c_double),
+                ("top_k", ctypes.c_int64), ("logits", ctypes.c_int32), ("type", ctypes.c_int32)]
 
 
 ADAM_CONTROL_BYTES = 64  # gs_adamw_control: two int64, four float32, eight uint32
@@ -198,6 +207,22 @@ def load_library():
     L.gs_adamw.argtypes = [P(GsAdamwPlan), P(GsAdamwParams), i64, vp, vp]
     L.gs_adamw_carry.restype = ctypes.c_int
     L.gs_adamw_carry.argtypes = [P(GsAdamwRows), ctypes.c_int32, i64, vp, i64, vp]
+    L.gs_shares_work_bytes.restype = sz
+    L.gs_shares_work_bytes.argtypes = [P(GsIndex), P(GsQuery)]
+    L.gs_shares.restype = ctypes.c_int
+    L.gs_shares.argtypes = [P(GsGaussians), P(GsIndex), P(GsQuery), vp, sz, vp, vp, f32, vp, vp, sz, vp]
+    L.gs_evict_work_bytes.restype = sz
+    L.gs_evict_work_bytes.argtypes = [i64]
+    L.gs_evict.restype = ctypes.c_int
+    L.gs_evict.argtypes = [P(GsParams), i64, vp, vp, i64, P(GsParams), vp, vp, vp, sz, vp]
+    L.gs_draw_work_bytes.restype = sz
+    L.gs_draw_work_bytes.argtypes = [i64, i64, i64]
+    L.gs_draw.restype = ctypes.c_int
+    L.gs_draw.argtypes = [i64, i64, vp, i64, vp, P(GsDrawParams), i64, vp, vp, vp, vp, sz, vp]
+    L.gs_split_work_bytes.restype = sz
+    L.gs_split_work_bytes.argtypes = [i64]
+    L.gs_split.restype = ctypes.c_int
+    L.gs_split.argtypes = [P(GsParams), i64, vp, i64, vp, vp, vp, sz, vp]
     _LIB = L
     return L
 
@@ -961,6 +986,163 @@ def gs_adamw_carry(carry: AdamCarry, n_in: int, source: torch.Tensor, n_out: int
         raise ValueError("source and the arrays must be on one device")
     _check(load_library().gs_adamw_carry(carry.c, len(carry.arrays), n_in, source.data_ptr(), n_out,
                                          _stream(stream)))
+
+
+def _work_size(b: int, what: str) -> int:
+    if b == ctypes.c_size_t(-1).value:
+        raise GsError(GS_ERR_INVALID_ARGUMENT, f"malformed {what}")
+    return int(b)
+
+
+def _one_device(dev: int, **tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"{name} must be on the same device as the others")
+
+
+def _row_of(t: Optional[torch.Tensor], name: str, dtype, n: int) -> None:
+    """A contiguous device tensor of a type with n elements at least."""
+    if t is not None and (not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or t.numel() < n):
+        raise ValueError(f"{name} must be a contiguous {str(dtype)[6:]} device tensor of at least {n} elements")
+
+
+def _work_bytes(work: torch.Tensor) -> int:
+    if not work.is_cuda or not work.is_contiguous():
+        raise ValueError("work must be a contiguous device tensor")
+    return work.numel() * work.element_size()
+
+
+def shares_work_bytes(index: Index, query: Query) -> int:
+    q = query.c()
+    return _work_size(load_library().gs_shares_work_bytes(ctypes.byref(index.c), ctypes.byref(q)), "index or query")
+
+
+def alloc_shares_work(index: Index, query: Query, device) -> torch.Tensor:
+    return _alloc_bytes(shares_work_bytes(index, query), device)
+
+
+def gs_shares(gauss: Gaussians, index: Index, query: Query, plan: Optional[torch.Tensor], influence: torch.Tensor,
+              score: torch.Tensor, work: torch.Tensor, gain: Optional[torch.Tensor] = None, decay: float = 0.0,
+              stream=None) -> None:
+    """The attention weight a_i / I that every Gaussian gets from the queries
+    that gs_sample just sampled, added to its score: score <- decay score +
+    sum of gain a_i / I. influence is the sampler's output (elements set to 0
+    are left out); gain (None: 1) weighs the queries."""
+    g = gauss.c()
+    q = query.c()
+    nq = query.size()
+    _row_of(influence, "influence", torch.float32, nq)
+    _row_of(gain, "gain", torch.float32, nq)
+    _row_of(score, "score", torch.float32, gauss.n)
+    _one_device(gauss.mean.get_device(), influence=influence, gain=gain, score=score, plan=plan, work=work)
+    _check(load_library().gs_shares(ctypes.byref(g), ctypes.byref(index.c), ctypes.byref(q), _ptr(plan),
+                                    0 if plan is None else plan.numel(), influence.data_ptr(), _ptr(gain),
+                                    float(decay), score.data_ptr(), work.data_ptr(), _work_bytes(work),
+                                    _stream(stream)))
+
+
+def evict_work_bytes(n: int) -> int:
+    return _work_size(load_library().gs_evict_work_bytes(int(n)), "count")
+
+
+def alloc_evict_work(n: int, device) -> torch.Tensor:
+    return _alloc_bytes(evict_work_bytes(n), device)
+
+
+def gs_evict(params_in: ParamSet, n: int, score: torch.Tensor, budget: int, params_out: ParamSet,
+             source: torch.Tensor, work: torch.Tensor, pinned: Optional[torch.Tensor] = None,
+             score_out: Optional[torch.Tensor] = None, stream=None) -> int:
+    """Cuts the first n Gaussians of a set down to `budget`: the pinned ones
+    (uint8 flags) before the others, then by score; the kept ones keep their
+    order. Writes their rows, the source map (for gs_adamw_carry) and, if
+    wanted, their scores; returns min(budget, n), without waiting."""
+    keep = min(int(budget), int(n))
+    if n > params_in.rows:
+        raise ValueError("n exceeds the input rows")
+    if keep > params_out.rows:
+        raise ValueError("the output has fewer rows than the budget")
+    _row_of(score, "score", torch.float32, n)
+    _row_of(pinned, "pinned", torch.uint8, n)
+    _row_of(source, "source", torch.int32, keep)
+    _row_of(score_out, "score_out", torch.float32, keep)
+    _one_device(params_in.mean.get_device(), params_out=params_out.mean, score=score, pinned=pinned, source=source,
+                score_out=score_out, work=work)
+    _check(load_library().gs_evict(ctypes.byref(params_in.c()), int(n), score.data_ptr(), _ptr(pinned), int(budget),
+                                   ctypes.byref(params_out.c()), source.data_ptr(), _ptr(score_out),
+                                   work.data_ptr(), _work_bytes(work), _stream(stream)))
+    return keep
+
+
+def draw_work_bytes(rows: int, n: int, draws: int) -> int:
+    return _work_size(load_library().gs_draw_work_bytes(int(rows), int(n), int(draws)), "sizes")
+
+
+def alloc_draw_work(rows: int, n: int, draws: int, device) -> torch.Tensor:
+    return _alloc_bytes(draw_work_bytes(rows, n, draws), device)
+
+
+_SCORE_TYPES = {torch.float32: GS_SCORE_F32, torch.bfloat16: GS_SCORE_BF16}
+
+
+def gs_draw(scores: torch.Tensor, uniform: torch.Tensor, ids: torch.Tensor, work: torch.Tensor,
+            prob: Optional[torch.Tensor] = None, logits: bool = False, lengths: Optional[torch.Tensor] = None,
+            temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0, stream=None) -> None:
+    """Draws from rows of candidates, with replacement, by the given numbers:
+    scores [rows, n] or [n], float32 or bfloat16, weights (or logits), with
+    candidates of a row next to each other and any distance between rows;
+    uniform [rows, draws] or [draws], float64 in [0, 1). Writes ids (int32, -1:
+    nothing to draw) and the candidates' probabilities."""
+    if scores.dim() == 1:
+        rows, n, stride = 1, scores.numel(), scores.numel()
+        draws = uniform.numel()
+    elif scores.dim() == 2 and uniform.dim() == 2 and uniform.shape[0] == scores.shape[0]:
+        rows, n = (int(x) for x in scores.shape)
+        draws = int(uniform.shape[1])
+        stride = int(scores.stride(0)) if rows > 1 else n
+    else:
+        raise ValueError("scores and uniform must be [n] and [draws], or [rows, n] and [rows, draws]")
+    kind = _SCORE_TYPES.get(scores.dtype)
+    if kind is None or not scores.is_cuda or (n > 1 and scores.stride(-1) != 1):
+        raise ValueError("scores must be a float32 or bfloat16 device tensor with contiguous rows")
+    if n == 0:
+        stride = max(stride, 0)
+    elif stride < n:
+        raise ValueError("rows of scores must not overlap")
+    _row_of(uniform, "uniform", torch.float64, rows * draws)
+    _row_of(ids, "ids", torch.int32, rows * draws)
+    _row_of(prob, "prob", torch.float32, rows * draws)
+    _row_of(lengths, "lengths", torch.int32, rows)
+    _one_device(scores.get_device(), uniform=uniform, ids=ids, prob=prob, lengths=lengths, work=work)
+    p = GsDrawParams(float(temperature), float(top_p), float(min_p), int(top_k), 1 if logits else 0, kind)
+    _check(load_library().gs_draw(rows, n, scores.data_ptr(), stride, _ptr(lengths), ctypes.byref(p), draws,
+                                  uniform.data_ptr(), ids.data_ptr(), _ptr(prob), work.data_ptr(),
+                                  _work_bytes(work), _stream(stream)))
+
+
+def split_work_bytes(n: int) -> int:
+    return _work_size(load_library().gs_split_work_bytes(int(n)), "count")
+
+
+def alloc_split_work(n: int, device) -> torch.Tensor:
+    return _alloc_bytes(split_work_bytes(n), device)
+
+
+def gs_split(params: ParamSet, n: int, ids: torch.Tensor, source: Optional[torch.Tensor], work: torch.Tensor,
+             score: Optional[torch.Tensor] = None, stream=None) -> int:
+    """Copies the Gaussians `ids` (int32) behind the first n of a set, in
+    place; a Gaussian and its copies share its weight, and its score, evenly,
+    so the field stays the same. source gets -1 - id for the copies. Returns
+    the new count, without waiting."""
+    count = int(ids.numel())
+    if n + count > params.rows:
+        raise ValueError("the set has no room for the copies")
+    _row_of(ids, "ids", torch.int32, count)
+    _row_of(source, "source", torch.int32, n + count)
+    _row_of(score, "score", torch.float32, n + count)
+    _one_device(params.mean.get_device(), ids=ids, source=source, score=score, work=work)
+    _check(load_library().gs_split(ctypes.byref(params.c()), int(n), ids.data_ptr(), count, _ptr(source),
+                                   _ptr(score), work.data_ptr(), _work_bytes(work), _stream(stream)))
+    return int(n) + count
 
 
 def backward_pair_count(index: Index, query: Query, plan: Optional[torch.Tensor], work: torch.Tensor,
