@@ -316,8 +316,9 @@ float index_radius(float tau) {
     return (float)(rc * (1.0 + 1.0 / 1024.0));
 }
 
-// The backward's row geometry for a grid and query (see BwdGeom).
-BwdGeom bwd_geom(const GridParams &gp, const QueryParams &qp, float T) {
+// The backward's row geometry for a grid and query (see BwdGeom); voxels:
+// whether rows of voxels are walked.
+BwdGeom bwd_geom(const GridParams &gp, const QueryParams &qp, float T, bool voxels) {
     BwdGeom b;
     b.T2 = (float)((double)T * (1.0 + 1.0 / 128.0));
     for (int j = 0; j < 2; ++j) {
@@ -326,7 +327,7 @@ BwdGeom bwd_geom(const GridParams &gp, const QueryParams &qp, float T) {
     }
     for (int j = 0; j < 3; ++j) {
         b.ivsz[j] = b.vslack[j] = 0.0f;
-        if (qp.kind != GS_QUERY_GRID) continue;
+        if (!voxels) continue;
         const double lo = gp.lo[j], hi = gp.hi[j];
         b.ivsz[j] = (float)(1.0 / (double)qp.vsz[j]);
         b.vslack[j] = (float)(std::ldexp(1.0, -20) * (double)qp.dims[j] *
@@ -335,6 +336,10 @@ BwdGeom bwd_geom(const GridParams &gp, const QueryParams &qp, float T) {
     }
     b.K = (uint32_t)(kSub * gp.cells[0]);
     return b;
+}
+
+BwdGeom bwd_geom(const GridParams &gp, const QueryParams &qp, float T) {
+    return bwd_geom(gp, qp, T, qp.kind == GS_QUERY_GRID);
 }
 
 // Backward workspace layout.
@@ -1236,7 +1241,7 @@ gs_status gs_shares(const gs_gaussians *gauss, const gs_index *index, const gs_q
     const IndexWork w = index_layout(index->work, n, &index->grid, index->capacity);
     const float T = cutoff_T(index->tau);
     const SharesExact exact{gauss->mean, gauss->scale, gauss->rot, 2.0 * std::log(1.0 / (double)index->tau)};
-    GS_TRY(launch_shares(qp, gp, bwd_geom(gp, qp, T), w.rec, w.box, w.gorder, n, p.order, p.point_off, p.res.pos, T,
+    GS_TRY(launch_shares(qp, gp, bwd_geom(gp, qp, T, query->kind == GS_QUERY_GRID || query->kind == GS_QUERY_JITTER), w.rec, w.box, w.gorder, n, p.order, p.point_off, p.res.pos, T,
                          exact, influence, gain, decay, score, sw, stream),
            "gs_shares");
     return GS_OK;

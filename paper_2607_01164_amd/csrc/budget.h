@@ -9,8 +9,9 @@ namespace gs {
 
 // Accumulated attention weight (shares.hip).
 struct SharesWork {
-    float4 *pts;  // ordered queries, in the plan's order: position and f
-    float *f;     // grids: f of every voxel
+    float4 *pts;      // ordered queries, in the plan's or the voxels' order: position and f
+    float *f;         // grids: f of every voxel
+    uint32_t *stray;  // jittered grids: whether a position lies outside its voxel
     size_t bytes;
 };
 SharesWork shares_layout(void *work, int64_t nq, bool grid);

@@ -22,6 +22,11 @@ namespace {
 constexpr uint32_t kPack = 4;
 constexpr int64_t kPackMinGauss = 65536;
 constexpr uint32_t kXcdWaves = 4;
+// The rows of a Gaussian's queries: voxels of a grid; the plan's cells; voxels
+// of a jittered grid, every voxel with its query.
+enum { kWalkGrid = 0, kWalkPlan = 1, kWalkVoxels = 2 };
+// queries from which a jittered grid is walked by voxels
+constexpr int64_t kVoxelsLeast = 4096;
 // waves of one launch (a launch has fewer than 2^32 threads)
 constexpr uint64_t kWavesMost = (uint64_t)1 << 25;
 
@@ -47,6 +52,29 @@ __global__ __launch_bounds__(kBlock) void k_shares_stage_plan(int64_t n, const u
     if (k >= n) return;
     const float4 p = pos[k];
     pts[k] = make_float4(p.x, p.y, p.z, query_factor(influence, gain, order[k]));
+}
+
+// Jittered grids whose every voxel has its query: positions in the voxels'
+// order, and whether any lies outside its voxel (stray, cleared before).
+// Positions that rounding carries over the domain's border are outside.
+__global__ __launch_bounds__(kBlock) void k_shares_stage_voxels(QueryParams q, GridParams g,
+                                                                const float *__restrict__ influence,
+                                                                const float *__restrict__ gain,
+                                                                float4 *__restrict__ pts,
+                                                                uint32_t *__restrict__ stray) {
+    const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (i >= q.n) return;
+    float p[3];
+    bool valid, in = true, home = true;
+    query_position(q, g, (uint32_t)i, p[0], p[1], p[2], valid);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        const float u = q.points[3 * i + k];
+        home = home && u >= 0.0f && u <= 1.0f;
+        in = in && p[k] >= g.lo[k] && p[k] <= g.hi[k];
+    }
+    pts[i] = make_float4(p[0], p[1], p[2], in ? query_factor(influence, gain, i) : 0.0f);
+    if (!home) *stray = 1;
 }
 
 // Q <= 2 ln(1/tau) from the parameters themselves, in float64.
@@ -83,8 +111,10 @@ struct SharesArgs {
     const uint32_t *gorder;
     int64_t n_gauss;
     const uint32_t *point_off;
+    const uint32_t *order;
     const float4 *pts;
     const float *f;
+    const uint32_t *stray;
     SharesExact exact;
     float T, decay;
     float *score;
@@ -92,20 +122,86 @@ struct SharesArgs {
     uint64_t wave0;  // the launch's first wave
 };
 
-template <bool GRID>
+// The voxels of a jittered grid that a Gaussian can reach: a row (y, z) of
+// voxels holds points of the slab [y, y + 1] x [z, z + 1]. With e the part of
+// u = U d that depends on y and z alone, |e| over the slab is at least its value
+// at the slab's centre less `reach`, the largest |e| of half a voxel; so is Q
+// >= |e|^2. In x the row's centre moves by at most `shift` over the slab.
+struct VoxelReach {
+    float reach, shift;
+};
+__device__ __forceinline__ VoxelReach voxel_reach(const Record &r, const QueryParams &q) {
+    const float hy = 0.5f * q.vsz[1], hz = 0.5f * q.vsz[2];
+    const float e1 = fabsf(r.f2.x) * hy + fabsf(r.f2.y) * hz, e2 = fabsf(r.f2.z) * hz;
+    VoxelReach v;
+    v.reach = __builtin_sqrtf(fmaf_(e1, e1, e2 * e2)) * (1.0f + 0x1p-10f);
+    v.shift = (fabsf(r.f1.y) * hy + fabsf(r.f1.z) * hz) / fabsf(r.f1.x);
+    return v;
+}
+
+// Rows y0 .. y0 + ny - 1, z0 .. z0 + nz - 1 of voxels that meet the ellipsoid's box.
+__device__ __forceinline__ void voxel_rows(const Record &r, const QueryParams &q, const GridParams &g,
+                                           const BwdGeom &bg, uint32_t &y0, uint32_t &ny, uint32_t &z0,
+                                           uint32_t &nz) {
+    const float rt = __builtin_sqrtf(bg.T2);
+    const float t = r.f2.y / r.f2.z;
+    const float hy = rt * __builtin_sqrtf(fmaf_(t, t, 1.0f)) / r.f2.x, hz = rt / r.f2.z;
+    auto cut = [](float mu, float h, float lo, float iv, float slack, int32_t dim, uint32_t &first, uint32_t &n) {
+        const float a = fmaxf(floorf((mu - h - lo) * iv - slack), 0.0f);
+        const float c = fminf(floorf((mu + h - lo) * iv + slack), (float)(dim - 1));
+        const bool some = a <= c;
+        first = some ? (uint32_t)a : 0u;
+        n = some ? (uint32_t)(c - a) + 1u : 0u;
+    };
+    cut(r.f0.y, hy, g.lo[1], bg.ivsz[1], bg.vslack[1], q.dims[1], y0, ny);
+    cut(r.f0.z, hz, g.lo[2], bg.ivsz[2], bg.vslack[2], q.dims[2], z0, nz);
+}
+
+// The voxels of row (vy, vz) that the cutoff T2 can reach: first and number.
+__device__ __forceinline__ uint32_t voxel_row(const Record &r, const VoxelReach &v, uint32_t vy, uint32_t vz,
+                                              const QueryParams &q, const GridParams &g, const BwdGeom &bg,
+                                              uint32_t &first) {
+    const float dy = g.lo[1] + ((float)vy + 0.5f) * q.vsz[1] - r.f0.y;
+    const float dz = g.lo[2] + ((float)vz + 0.5f) * q.vsz[2] - r.f0.z;
+    const float e1 = fmaf_(r.f2.x, dy, r.f2.y * dz), e2 = r.f2.z * dz;
+    const float e = fmaxf(__builtin_sqrtf(fmaf_(e1, e1, e2 * e2)) * (1.0f - 0x1p-10f) - v.reach, 0.0f);
+    const float left = bg.T2 - e * e;
+    first = 0;
+    if (!(left >= 0.0f)) return 0;
+    const float iu = __builtin_amdgcn_rcpf(r.f1.x);
+    const float w = __builtin_sqrtf(left) * iu * (1.0f + 0x1p-10f) + v.shift;
+    const float c = r.f0.x - fmaf_(r.f1.y, dy, r.f1.z * dz) * iu;
+    const float m = (fabsf(r.f0.x) + fabsf(c) + w) * 0x1p-20f;
+    const float a = fmaxf(floorf((c - w - m - g.lo[0]) * bg.ivsz[0] - bg.vslack[0]), 0.0f);
+    const float b = fminf(floorf((c + w + m - g.lo[0]) * bg.ivsz[0] + bg.vslack[0]), (float)(q.dims[0] - 1));
+    if (!(a <= b)) return 0;
+    first = (uint32_t)a;
+    return (uint32_t)(b - a) + 1u;
+}
+
+// A wave takes `pack` Gaussians (consecutive in gorder). Their rows are listed
+// one Gaussian after the other and set up 64 at a time, a lane a row; the rows
+// with queries go to LDS. Then each Gaussian's rows are walked with its record
+// in scalars: 2^k lanes a row, the rows next to each other, so that short
+// rows share a step and a load reads whole stretches of memory.
+template <int WALK>
 __global__ __launch_bounds__(kWave) void k_shares(SharesArgs a) {
+    __shared__ uint2 s_row[kWave];   // first query, queries
+    __shared__ uint4 s_grid[kWave];  // grids: first x, y and z
     const uint32_t lane = threadIdx.x;
     const uint64_t first = (a.wave0 + xcd_group<kXcdWaves>(blockIdx.x, gridDim.x)) * a.pack;
     if (first >= (uint64_t)a.n_gauss) return;
     const uint32_t nk = (uint64_t)a.n_gauss - first < a.pack ? (uint32_t)((uint64_t)a.n_gauss - first) : a.pack;
     const float T = a.T;
+    // positions that leave their voxels: the plan's rows, through its order
+    const bool voxels = WALK == kWalkVoxels && *a.stray == 0;
     // lane i < nk describes Gaussian i of the wave: its rows
     uint32_t mgid = 0, mR = 0, mnx = 0, mny = 1, mx = 0, my = 0, mz = 0;
     if (lane < nk) {
         mgid = a.gorder[first + lane];
         const CellBox b = a.box[mgid];
         if (b.hi.x >= b.lo.x && a.q.n > 0) {
-            if (GRID) {
+            if (WALK == kWalkGrid) {
                 const GridRows r = grid_rows(a.rec[mgid], b, a.q, a.g, a.bg);
                 mx = r.x0;
                 mnx = r.x1;
@@ -113,6 +209,10 @@ __global__ __launch_bounds__(kWave) void k_shares(SharesArgs a) {
                 mny = r.ny;
                 mz = r.z0;
                 mR = r.ny * r.nz;
+            } else if (voxels) {
+                uint32_t nz;
+                voxel_rows(a.rec[mgid], a.q, a.g, a.bg, my, mny, mz, nz);
+                mR = mny * nz;
             } else {
                 mx = (uint32_t)b.lo.x;
                 mnx = (uint32_t)(b.hi.x - b.lo.x + 1);
@@ -127,9 +227,20 @@ __global__ __launch_bounds__(kWave) void k_shares(SharesArgs a) {
     const uint32_t Rw = __builtin_amdgcn_readlane(mRend, kWave - 1);
     const bool fdiv = wave_max_uniform(mR) < (1u << 21);
     float mtot = 0.0f;  // lane i < nk: Gaussian i's sum
+    float acc = 0.0f;   // of the Gaussian being walked
+    uint32_t cur = ~0u, cgid = 0;
+    Record c = {};
+    float margin = 0.0f;
+    auto finish = [&]() {
+        float t = row16_sum(acc);
+        t += swz_xor16(t);
+        t += perm_xor32(t, lane);
+        if (lane == cur) mtot = t;
+        acc = 0.0f;
+    };
     for (uint32_t rb = 0; rb < Rw; rb += kWave) {
-        // lane l takes row rb + l of the wave's list, of Gaussian i; lanes
-        // past the last row have none (the permutes run with every lane)
+        // lane l sets up row rb + l of the wave's list, of Gaussian i (the
+        // permutes run with every lane)
         const uint32_t gr = rb + lane;
         uint32_t i = 0;
         for (uint32_t t = 0; t < nk; ++t) i += __builtin_amdgcn_readlane(mRend, t) <= gr ? 1u : 0u;
@@ -137,61 +248,85 @@ __global__ __launch_bounds__(kWave) void k_shares(SharesArgs a) {
         auto perm = [&](uint32_t v) { return (uint32_t)__builtin_amdgcn_ds_bpermute((int)src, (int)v); };
         const uint32_t gid = perm(mgid), end = perm(mRend), R = perm(mR), nx = perm(mnx), ny = perm(mny);
         const uint32_t x0 = perm(mx), y0 = perm(my), z0 = perm(mz);
-        float acc = 0.0f;
+        uint32_t start = 0, len = 0, vx = 0;
+        float py = 0.0f, pz = 0.0f;
         if (gr < Rw) {
             const Record r = a.rec[gid];
-            const float margin = cutoff_margin(a.exact, gid, T);
-            uint32_t yy, zz, start;
+            uint32_t yy, zz;
             row_yz(gr - (end - R), ny, fdiv, yy, zz);
-            // whether a pair of this Q' at p is within the cutoff
-            auto within = [&](float Q, float px, float py, float pz) {
-                bool in = Q <= T;
-                if (__builtin_fabsf(Q - T) <= margin) in = within_exact(a.exact, gid, px, py, pz);
-                return in;
-            };
-            if (GRID) {
-                uint32_t vx;
-                float py, pz;
-                const uint32_t len = grid_row(r, x0, nx, y0 + yy, z0 + zz, a.q, a.g, a.bg, vx, py, pz);
-                const float *f = a.f + ((size_t)vx + (size_t)(uint32_t)a.q.dims[0] *
-                                                         ((y0 + yy) + (size_t)(uint32_t)a.q.dims[1] * (z0 + zz)));
-                const float dy = py - r.f0.y, dz = pz - r.f0.z;
-                const float c0 = fmaf_(r.f1.y, dy, r.f1.z * dz);
-                const float u1 = fmaf_(r.f2.x, dy, r.f2.y * dz), u2 = r.f2.z * dz;
-                const float c1 = fmaf_(u1, u1, u2 * u2);
-                for (uint32_t e = 0; e < len; ++e) {
-                    const float px = a.g.lo[0] + ((float)(vx + e) + 0.5f) * a.q.vsz[0];
-                    const float u0 = fmaf_(r.f1.x, px - r.f0.x, c0);
-                    const float Q = fmaf_(u0, u0, c1);
-                    const float v = exp2_hw(-Q) * f[e];
-                    acc += within(Q, px, py, pz) ? v : 0.0f;
+            const uint32_t vy = y0 + yy, vz = z0 + zz;
+            if (WALK == kWalkGrid)
+                len = grid_row(r, x0, nx, vy, vz, a.q, a.g, a.bg, vx, py, pz);
+            else if (voxels)
+                len = voxel_row(r, voxel_reach(r, a.q), vy, vz, a.q, a.g, a.bg, vx);
+            else
+                len = plan_row(r, x0, nx, vy, vz, a.g, a.bg, a.point_off, start);
+            if (WALK == kWalkGrid || voxels)
+                start = (uint32_t)a.q.dims[0] * (vy + (uint32_t)a.q.dims[1] * vz) + vx;
+        }
+        const uint64_t some = __ballot(len > 0);
+        __builtin_amdgcn_wave_barrier();
+        if (len > 0) {
+            const uint32_t at = (uint32_t)__popcll(some & (((uint64_t)1 << lane) - 1));
+            s_row[at] = make_uint2(start, len);
+            if (WALK == kWalkGrid) s_grid[at] = make_uint4(vx, __float_as_uint(py), __float_as_uint(pz), 0);
+        }
+        __builtin_amdgcn_wave_barrier();
+        const uint32_t nrows = Rw - rb < (uint32_t)kWave ? Rw - rb : (uint32_t)kWave;
+        const uint32_t ia = __builtin_amdgcn_readlane(i, 0), ib = __builtin_amdgcn_readlane(i, nrows - 1);
+        for (uint32_t gi = ia; gi <= ib; ++gi) {
+            const uint32_t gend = __builtin_amdgcn_readlane(mRend, gi), gR = __builtin_amdgcn_readlane(mR, gi);
+            if (gR == 0) continue;
+            if (gi != cur) {
+                if (cur != ~0u) finish();
+                cur = gi;
+                cgid = __builtin_amdgcn_readlane(mgid, gi);
+                c = load_record_uniform(a.rec, cgid);
+                margin = readfirst_f(cutoff_margin(a.exact, cgid, T));
+            }
+            // its rows in this batch, and those of them with queries
+            const uint32_t la = gend - gR > rb ? gend - gR - rb : 0u;
+            const uint32_t lb = gend - rb < nrows ? gend - rb : nrows;
+            const uint64_t below_a = ((uint64_t)1 << la) - 1;
+            const uint64_t below_b = lb < (uint32_t)kWave ? ((uint64_t)1 << lb) - 1 : ~(uint64_t)0;
+            const uint32_t ra = (uint32_t)__popcll(some & below_a), rz = (uint32_t)__popcll(some & below_b);
+            if (ra == rz) continue;
+            // lanes of a row: the power of two from its longest row on
+            const uint32_t longest = wave_max_uniform(lane >= la && lane < lb ? len : 0u);
+            const uint32_t shift = longest > 32u ? 6u : longest > 16u ? 5u : longest > 8u ? 4u : 3u;
+            const uint32_t wide = 1u << shift, mine = lane & (wide - 1), own = lane >> shift;
+            for (uint32_t r0 = ra; r0 < rz; r0 += (uint32_t)kWave >> shift) {
+                const uint32_t row = r0 + own;
+                uint2 w = make_uint2(0, 0);
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (row < rz) {
+                    w = s_row[row];
+                    if (WALK == kWalkGrid) v = s_grid[row];
                 }
-            } else {
-                const uint32_t len = plan_row(r, x0, nx, y0 + yy, z0 + zz, a.g, a.bg, a.point_off, start);
-                const float4 *p = a.pts + start;
-                for (uint32_t e = 0; e < len; ++e) {
-                    const float4 t = p[e];
-                    const float Q = record_q(r, t.x, t.y, t.z);
-                    const float v = exp2_hw(-Q) * t.w;
-                    acc += within(Q, t.x, t.y, t.z) ? v : 0.0f;
+                for (uint32_t e = mine; e < w.y; e += wide) {
+                    float px, py, pz, f;
+                    if (WALK == kWalkGrid) {
+                        px = a.g.lo[0] + ((float)(v.x + e) + 0.5f) * a.q.vsz[0];
+                        py = __uint_as_float(v.y);
+                        pz = __uint_as_float(v.z);
+                        f = a.f[(size_t)w.x + e];
+                    } else {
+                        const size_t k = (size_t)w.x + e;
+                        const float4 t = a.pts[WALK == kWalkVoxels && !voxels ? (size_t)a.order[k] : k];
+                        px = t.x;
+                        py = t.y;
+                        pz = t.z;
+                        f = t.w;
+                    }
+                    const float Q = record_q(c, px, py, pz);
+                    bool in = Q <= T;
+                    if (__builtin_fabsf(Q - T) <= margin) in = within_exact(a.exact, cgid, px, py, pz);
+                    if (in) acc = fmaf_(exp2_hw(-Q), f, acc);
                 }
             }
         }
-        // inclusive sums over the lanes of one Gaussian
-#pragma unroll
-        for (uint32_t o = 1; o < (uint32_t)kWave; o <<= 1) {
-            const float v = __shfl_up(acc, o, kWave);
-            const uint32_t j = __shfl_up(i, o, kWave);
-            if (lane >= o && j == i) acc += v;
-        }
-        // the last row of Gaussian `lane` in this batch has its sum
-        const uint32_t beg = mRend - mR;
-        const uint32_t la = beg > rb ? beg : rb, lb = mRend < rb + kWave ? mRend : rb + kWave;
-        const bool some = lane < nk && la < lb;
-        const float v = __int_as_float(
-            __builtin_amdgcn_ds_bpermute(some ? (int)((lb - 1 - rb) << 2) : 0, __float_as_int(acc)));
-        if (some) mtot += v;
     }
+    if (cur != ~0u) finish();
     if (lane < nk) {
         const float add = a.rec[mgid].f0.w * mtot;
         a.score[mgid] = a.decay > 0.0f ? fmaf_(a.decay, a.score[mgid], add) : add;
@@ -202,12 +337,16 @@ size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 }  // namespace
 
+bool walks_voxels(const QueryParams &q) { return q.kind == 3 && !q.voxel_ids && q.n >= kVoxelsLeast; }
+
 SharesWork shares_layout(void *work, int64_t nq, bool grid) {
     SharesWork w;
     const size_t m = (size_t)(nq > 0 ? nq : 1);
-    w.pts = grid ? nullptr : (float4 *)work;
-    w.f = grid ? (float *)work : nullptr;
-    w.bytes = al256(m * (grid ? sizeof(float) : sizeof(float4)));
+    w.stray = (uint32_t *)work;
+    char *rest = work ? (char *)work + 256 : nullptr;
+    w.pts = grid ? nullptr : (float4 *)rest;
+    w.f = grid ? (float *)rest : nullptr;
+    w.bytes = 256 + al256(m * (grid ? sizeof(float) : sizeof(float4)));
     return w;
 }
 
@@ -217,16 +356,20 @@ hipError_t launch_shares(const QueryParams &q, const GridParams &g, const BwdGeo
                          const float *influence, const float *gain, float decay, float *score,
                          const SharesWork &w, hipStream_t s) {
     if (n_gauss <= 0) return hipSuccess;
-    const bool grid = q.kind == 0;
+    const int walk = q.kind == 0 ? kWalkGrid : walks_voxels(q) ? kWalkVoxels : kWalkPlan;
     hipError_t e;
     if (q.n > 0) {
         const dim3 nb((uint32_t)((q.n + kBlock - 1) / kBlock));
         prof_begin("shares_stage", s);
-        if (grid)
+        if (walk == kWalkGrid) {
             hipLaunchKernelGGL(k_shares_stage_grid, nb, dim3(kBlock), 0, s, q.n, influence, gain, w.f);
-        else
+        } else if (walk == kWalkVoxels) {
+            if ((e = fill_u32(w.stray, 0u, 1, s)) != hipSuccess) return e;
+            hipLaunchKernelGGL(k_shares_stage_voxels, nb, dim3(kBlock), 0, s, q, g, influence, gain, w.pts, w.stray);
+        } else {
             hipLaunchKernelGGL(k_shares_stage_plan, nb, dim3(kBlock), 0, s, q.n, order, plan_pos, influence, gain,
                                w.pts);
+        }
         prof_end("shares_stage", s);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
@@ -239,24 +382,28 @@ hipError_t launch_shares(const QueryParams &q, const GridParams &g, const BwdGeo
     a.gorder = gorder;
     a.n_gauss = n_gauss;
     a.point_off = point_off;
+    a.order = order;
     a.pts = w.pts;
     a.f = w.f;
+    a.stray = w.stray;
     a.exact = exact;
     a.T = T;
     a.decay = decay;
     a.score = score;
     // a wave's rows are counted in 32 bits
-    const int64_t rows = grid ? (int64_t)q.dims[1] * q.dims[2] : (int64_t)g.cells[1] * g.cells[2];
+    const int64_t rows = walk == kWalkPlan ? (int64_t)g.cells[1] * g.cells[2] : (int64_t)q.dims[1] * q.dims[2];
     a.pack = n_gauss < kPackMinGauss || rows > ((int64_t)1 << 31) / kPack ? 1u : kPack;
     const uint64_t waves = ((uint64_t)n_gauss + a.pack - 1) / a.pack;
     prof_begin("shares", s);
     for (a.wave0 = 0; a.wave0 < waves; a.wave0 += kWavesMost) {
         const uint64_t left = waves - a.wave0;
         const dim3 wb((uint32_t)(left < kWavesMost ? left : kWavesMost));
-        if (grid)
-            hipLaunchKernelGGL(k_shares<true>, wb, dim3(kWave), 0, s, a);
+        if (walk == kWalkGrid)
+            hipLaunchKernelGGL(k_shares<kWalkGrid>, wb, dim3(kWave), 0, s, a);
+        else if (walk == kWalkVoxels)
+            hipLaunchKernelGGL(k_shares<kWalkVoxels>, wb, dim3(kWave), 0, s, a);
         else
-            hipLaunchKernelGGL(k_shares<false>, wb, dim3(kWave), 0, s, a);
+            hipLaunchKernelGGL(k_shares<kWalkPlan>, wb, dim3(kWave), 0, s, a);
     }
     prof_end("shares", s);
     return hipGetLastError();
