@@ -6,6 +6,8 @@
 // three counting passes over the scores find digit by digit; what lies above
 // it stays, and as many of its equals, by index, as the budget leaves. Bound
 // by the rows of the kept ones, read and written once.
+#include <type_traits>
+
 #include "budget.h"
 
 namespace gs {
@@ -21,176 +23,372 @@ __device__ __forceinline__ uint32_t score_key(float s) {
 }
 
 // Digits of the key: pinned and its top 11 bits, the next 11, the last 10.
+constexpr uint32_t kDigits = 3;
 constexpr uint32_t kBins0 = 4096, kBins1 = 2048, kBins2 = 1024;
 constexpr uint32_t kBinsAll = kBins0 + kBins1 + kBins2;
-constexpr uint32_t kTile = 1024;        // Gaussians of a tile: 4 a thread
-constexpr uint32_t kBlocksMost = 1024;  // workgroups of a pass, each over a stretch of tiles
+constexpr uint32_t bins_of(int digit) { return digit == 0 ? kBins0 : digit == 1 ? kBins1 : kBins2; }
+constexpr uint32_t bins_before(int digit) { return digit == 0 ? 0 : digit == 1 ? kBins0 : kBins0 + kBins1; }
+constexpr uint32_t kEach = 4;                 // Gaussians of a thread in a tile
+constexpr uint32_t kTile = kBlock * kEach;
+constexpr uint32_t kBlocksMost = 1024;        // workgroups of a pass, each over a stretch of tiles
+// The counting passes end with an atomic add for every bin that a workgroup
+// met, and those to one address wait for each other (1024 workgroups: 15 us
+// of a pass of 20): few, large workgroups, and kCopies of the counts.
+constexpr uint32_t kCountThreads = 1024;
+constexpr uint32_t kCountBlocks = 256;
+constexpr uint32_t kCopies = 4;
+constexpr uint32_t kSmallThreads = 1024;
+constexpr int64_t kSmall = 16384;             // sets that one workgroup selects from
 
 struct Key {
     uint32_t key, pin;
 };
-__device__ __forceinline__ Key load_key(const float *score, const uint8_t *pinned, int64_t i) {
-    return Key{score_key(score[i]), pinned && pinned[i] ? 1u : 0u};
-}
 
-// Where the cut lies so far: the digits found, and how many Gaussians are
-// still to be taken among those that have them.
+// Where the cut lies so far: the digits found of its key, and how many
+// Gaussians are still to be taken among those that have them.
 struct Cut {
-    uint32_t pin, key;  // of the cut's key, the digits found
-    uint32_t need;
+    uint32_t pin, key, need, pad;
 };
 
-// The bin of a histogram in which the need-th element from the top lies; need
-// becomes its rank in there. For the whole workgroup (kBlock threads); lds:
-// kWavesPerBlock + 2 words. need is at least 1 and at most the sum.
-template <uint32_t BINS>
-__device__ uint32_t find_bin(const uint32_t *__restrict__ hist, uint32_t &need, uint32_t *lds) {
-    constexpr uint32_t kEach = BINS / kBlock;
-    // thread 0 has the top bins
-    const uint32_t top = BINS - 1 - threadIdx.x * kEach;
-    uint32_t c[kEach], sum = 0, total;
-#pragma unroll
-    for (uint32_t j = 0; j < kEach; ++j) sum += c[j] = hist[top - j];
-    uint32_t above = block_excl_scan(sum, lds, &total);
-#pragma unroll
-    for (uint32_t j = 0; j < kEach; ++j) {
-        if (above < need && need <= above + c[j]) {
-            lds[kWavesPerBlock] = top - j;
-            lds[kWavesPerBlock + 1] = need - above;
-        }
-        above += c[j];
-    }
-    __syncthreads();
-    const uint32_t bin = lds[kWavesPerBlock];
-    need = lds[kWavesPerBlock + 1];
-    __syncthreads();
-    return bin;
+template <int DIGIT>
+__device__ __forceinline__ uint32_t digit_of(Key k) {
+    return DIGIT == 0 ? k.pin << 11 | k.key >> 21 : DIGIT == 1 ? k.key >> 10 & 2047u : k.key & 1023u;
 }
-
-// The first PASS digits of the cut.
-template <int PASS>
-__device__ Cut find_cut(const uint32_t *hist, uint32_t keep, uint32_t *lds) {
-    Cut c{0, 0, keep};
-    if (PASS > 0) {
-        const uint32_t b = find_bin<kBins0>(hist, c.need, lds);
-        c.pin = b >> 11;
-        c.key = b << 21;
-    }
-    if (PASS > 1) c.key |= find_bin<kBins1>(hist + kBins0, c.need, lds) << 10;
-    if (PASS > 2) c.key |= find_bin<kBins2>(hist + kBins0 + kBins1, c.need, lds);
-    return c;
+template <int DIGIT>
+__device__ __forceinline__ bool has_digits(Key k, const Cut &c) {
+    if (DIGIT == 0) return true;
+    return k.pin == c.pin && ((k.key ^ c.key) >> (DIGIT == 1 ? 21 : 10)) == 0;
 }
-
-// Counts of digit PASS over the Gaussians that have the cut's earlier digits.
-template <int PASS>
-__global__ __launch_bounds__(kBlock) void k_evict_count(int64_t n, int64_t stretch, const float *__restrict__ score,
-                                                        const uint8_t *__restrict__ pinned, uint32_t keep,
-                                                        uint32_t *__restrict__ hist) {
-    constexpr uint32_t kBins = PASS == 0 ? kBins0 : PASS == 1 ? kBins1 : kBins2;
-    __shared__ uint32_t s_hist[kBins];
-    __shared__ uint32_t lds[kWavesPerBlock + 2];
-    for (uint32_t b = threadIdx.x; b < kBins; b += kBlock) s_hist[b] = 0;
-    const Cut cut = find_cut<PASS>(hist, keep, lds);
-    __syncthreads();
-    const int64_t i0 = (int64_t)blockIdx.x * stretch, i1 = i0 + stretch < n ? i0 + stretch : n;
-    for (int64_t i = i0 + threadIdx.x; i < i1; i += kBlock) {
-        const Key k = load_key(score, pinned, i);
-        if (PASS == 0) {
-            atomicAdd(&s_hist[k.pin << 11 | k.key >> 21], 1u);
-        } else if (PASS == 1) {
-            if (k.pin == cut.pin && ((k.key ^ cut.key) >> 21) == 0) atomicAdd(&s_hist[k.key >> 10 & 2047u], 1u);
-        } else {
-            if (k.pin == cut.pin && ((k.key ^ cut.key) >> 10) == 0) atomicAdd(&s_hist[k.key & 1023u], 1u);
-        }
-    }
-    __syncthreads();
-    uint32_t *out = hist + (PASS == 0 ? 0u : PASS == 1 ? kBins0 : kBins0 + kBins1);
-    for (uint32_t b = threadIdx.x; b < kBins; b += kBlock)
-        if (s_hist[b]) atomicAdd(&out[b], s_hist[b]);
-}
-
 __device__ __forceinline__ bool above_cut(Key k, const Cut &c) {
     return k.pin > c.pin || (k.pin == c.pin && k.key > c.key);
 }
 __device__ __forceinline__ bool at_cut(Key k, const Cut &c) { return k.pin == c.pin && k.key == c.key; }
 
+// Keys of Gaussians i .. i + 3, those below i1; returns how many.
+__device__ __forceinline__ uint32_t load_keys(const float *score, const uint8_t *pinned, int64_t i, int64_t i1,
+                                              Key k[kEach]) {
+    typedef float f4a __attribute__((ext_vector_type(4), aligned(4)));
+    const uint32_t m = i + kEach <= i1 ? kEach : i < i1 ? (uint32_t)(i1 - i) : 0u;
+    float v[kEach] = {};
+    uint32_t pin = 0;
+    if (m == kEach) {
+        const f4a q = *(const f4a *)(score + i);
+        v[0] = q.x;
+        v[1] = q.y;
+        v[2] = q.z;
+        v[3] = q.w;
+        if (pinned) __builtin_memcpy(&pin, pinned + i, 4);
+    } else {
+        for (uint32_t t = 0; t < m; ++t) {
+            v[t] = score[i + t];
+            if (pinned) pin |= (uint32_t)pinned[i + t] << (8 * t);
+        }
+    }
+#pragma unroll
+    for (uint32_t t = 0; t < kEach; ++t) k[t] = Key{score_key(v[t]), (pin >> (8 * t) & 255u) ? 1u : 0u};
+    return m;
+}
+
+// Adds 1 to a bin for every active lane. Scores repeat (a Gaussian that no
+// query reached has none), and lanes that meet in a bin wait for each other:
+// the bins of the first lanes are counted for all lanes at once. (2 M scores,
+// 0.6 of them 0: a pass 23 -> 8 us.)
+__device__ __forceinline__ void hist_add(uint32_t *hist, uint32_t bin, bool active) {
+    uint64_t todo = __ballot(active);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        if (todo == 0) return;
+        const uint32_t leader = (uint32_t)__builtin_ctzll(todo);
+        const uint32_t b = __builtin_amdgcn_readlane(bin, leader);
+        const uint64_t same = __ballot(active && bin == b);
+        if (lane_id() == leader) atomicAdd(&hist[b], (uint32_t)__popcll(same));
+        active = active && bin != b;
+        todo &= ~same;
+    }
+    if (active) atomicAdd(&hist[bin], 1u);
+}
+
+// Exclusive sums over a workgroup of NT threads; *total gets the sum.
+template <int NT>
+__device__ __forceinline__ uint32_t group_scan(uint32_t x, uint32_t *lds, uint32_t *total) {
+    constexpr uint32_t kWaves = NT / kWave;
+    const uint32_t wave = threadIdx.x / kWave;
+    const uint32_t incl = wave_incl_sum(x);
+    __syncthreads();
+    if (threadIdx.x % kWave == kWave - 1) lds[wave] = incl;
+    __syncthreads();
+    uint32_t before = 0, all = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < kWaves; ++w) {
+        const uint32_t v = lds[w];
+        if (w < wave) before += v;
+        all += v;
+    }
+    *total = all;
+    return before + incl - x;
+}
+
+// The cut with its next digit, from that digit's counts: the bin in which
+// the need-th Gaussian from the top lies. need is at least 1 and at most the
+// sum. lds: NT / kWave + 2 words.
+template <int NT, int DIGIT, int COPIES>
+__device__ Cut next_digit(Cut cut, const uint32_t *hist, uint32_t *lds) {
+    constexpr uint32_t kBins = bins_of(DIGIT), kMine = kBins / NT > 0 ? kBins / NT : 1;
+    const uint32_t top = kBins - 1 - threadIdx.x * kMine;  // thread 0 has the top bins
+    uint32_t c[kMine], sum = 0, total;
+#pragma unroll
+    for (uint32_t j = 0; j < kMine; ++j) {
+        c[j] = 0;
+        if (threadIdx.x * kMine + j < kBins) {
+#pragma unroll
+            for (int r = 0; r < COPIES; ++r) c[j] += hist[r * kBinsAll + top - j];
+        }
+        sum += c[j];
+    }
+    uint32_t above = group_scan<NT>(sum, lds, &total);
+#pragma unroll
+    for (uint32_t j = 0; j < kMine; ++j) {
+        if (above < cut.need && cut.need <= above + c[j]) {
+            lds[NT / kWave] = top - j;
+            lds[NT / kWave + 1] = cut.need - above;
+        }
+        above += c[j];
+    }
+    __syncthreads();
+    const uint32_t bin = lds[NT / kWave];
+    cut.need = lds[NT / kWave + 1];
+    if (DIGIT == 0) {
+        cut.pin = bin >> 11;
+        cut.key = bin << 21;
+    } else {
+        cut.key |= DIGIT == 1 ? bin << 10 : bin;
+    }
+    return cut;
+}
+
+// The cut after digit DIGIT, given what a pass before kept of the earlier
+// ones; the first workgroup keeps it for the passes after.
+template <int NT, int DIGIT>
+__device__ Cut cut_after(const uint32_t *hist, Cut *cuts, uint32_t keep, uint32_t *lds) {
+    Cut c{0, 0, keep, 0};
+    if (DIGIT > 0) c = cuts[DIGIT > 0 ? DIGIT - 1 : 0];
+    c = next_digit<NT, DIGIT, kCopies>(c, hist + bins_before(DIGIT), lds);
+    if (blockIdx.x == 0 && threadIdx.x == 0) cuts[DIGIT] = c;
+    return c;
+}
+
+// Counts of a digit over the Gaussians that have the cut's earlier digits.
+template <int DIGIT>
+__global__ __launch_bounds__(kCountThreads) void k_evict_count(int64_t n, int64_t stretch, const float *__restrict__ score,
+                                                        const uint8_t *__restrict__ pinned, uint32_t keep,
+                                                        uint32_t *hist, Cut *cuts) {
+    constexpr uint32_t kBins = bins_of(DIGIT);
+    __shared__ uint32_t s_hist[kBins];
+    __shared__ uint32_t lds[kCountThreads / kWave + 2];
+    for (uint32_t b = threadIdx.x; b < kBins; b += kCountThreads) s_hist[b] = 0;
+    Cut cut{};
+    if (DIGIT > 0) cut = cut_after<kCountThreads, DIGIT ? DIGIT - 1 : 0>(hist, cuts, keep, lds);
+    __syncthreads();
+    const int64_t i0 = (int64_t)blockIdx.x * stretch, i1 = i0 + stretch < n ? i0 + stretch : n;
+    for (int64_t t0 = i0; t0 < i1; t0 += kCountThreads * kEach) {
+        Key k[kEach];
+        const uint32_t m = load_keys(score, pinned, t0 + threadIdx.x * kEach, i1, k);
+#pragma unroll
+        for (uint32_t t = 0; t < kEach; ++t) hist_add(s_hist, digit_of<DIGIT>(k[t]), t < m && has_digits<DIGIT>(k[t], cut));
+    }
+    __syncthreads();
+    uint32_t *out = hist + blockIdx.x % kCopies * kBinsAll + bins_before(DIGIT);
+    for (uint32_t b = threadIdx.x; b < kBins; b += kCountThreads)
+        if (s_hist[b]) atomicAdd(&out[b], s_hist[b]);
+}
+
 // Per stretch, the Gaussians above the cut and at it.
 __global__ __launch_bounds__(kBlock) void k_evict_stretch(int64_t n, int64_t stretch,
                                                           const float *__restrict__ score,
                                                           const uint8_t *__restrict__ pinned, uint32_t keep,
-                                                          const uint32_t *__restrict__ hist,
+                                                          const uint32_t *hist, Cut *cuts,
                                                           uint2 *__restrict__ sums) {
     __shared__ uint32_t lds[kWavesPerBlock + 2];
-    const Cut cut = find_cut<3>(hist, keep, lds);
+    const Cut cut = cut_after<kBlock, kDigits - 1>(hist, cuts, keep, lds);
     const int64_t i0 = (int64_t)blockIdx.x * stretch, i1 = i0 + stretch < n ? i0 + stretch : n;
     uint32_t above = 0, at = 0;
-    for (int64_t i = i0 + threadIdx.x; i < i1; i += kBlock) {
-        const Key k = load_key(score, pinned, i);
-        above += above_cut(k, cut) ? 1u : 0u;
-        at += at_cut(k, cut) ? 1u : 0u;
+    for (int64_t t0 = i0; t0 < i1; t0 += kTile) {
+        Key k[kEach];
+        const uint32_t m = load_keys(score, pinned, t0 + threadIdx.x * kEach, i1, k);
+#pragma unroll
+        for (uint32_t t = 0; t < kEach; ++t) {
+            above += t < m && above_cut(k[t], cut) ? 1u : 0u;
+            at += t < m && at_cut(k[t], cut) ? 1u : 0u;
+        }
     }
     uint32_t total_above, total_at;
-    block_excl_scan(above, lds, &total_above);
-    block_excl_scan(at, lds, &total_at);
+    group_scan<kBlock>(above, lds, &total_above);
+    group_scan<kBlock>(at, lds, &total_at);
     if (threadIdx.x == 0) sums[blockIdx.x] = make_uint2(total_above, total_at);
 }
 
-// Sources of the kept Gaussians, in the order of their indices.
-__global__ __launch_bounds__(kBlock) void k_evict_source(int64_t n, int64_t stretch,
-                                                         const float *__restrict__ score,
-                                                         const uint8_t *__restrict__ pinned, uint32_t keep,
-                                                         const uint32_t *__restrict__ hist,
-                                                         const uint2 *__restrict__ sums,
-                                                         int32_t *__restrict__ source) {
-    __shared__ uint32_t lds[kWavesPerBlock + 2];
-    const Cut cut = find_cut<3>(hist, keep, lds);
+// A Gaussian's free parameters: one access an array. (Accesses of 4 bytes to
+// a line that is still on its way wait for it one by one: 419430 copies out
+// of 2 M Gaussians took 87 us with them.)
+typedef float f3a __attribute__((ext_vector_type(3), aligned(4)));
+typedef float f4a __attribute__((ext_vector_type(4), aligned(4)));
+struct Row {
+    f3a mean, log_scale;
+    f4a rot;
+    float value, weight;
+};
+// (a vector of three floats takes the place of four in C: rows are addressed
+// as floats)
+__device__ __forceinline__ Row load_row(const gs_params &p, int64_t i) {
+    Row r;
+    __builtin_memcpy(&r.mean, p.mean + 3 * i, 12);
+    __builtin_memcpy(&r.log_scale, p.log_scale + 3 * i, 12);
+    r.rot = *(const f4a *)(p.rot + 4 * i);
+    r.value = p.value_logit[i];
+    r.weight = p.weight_logit[i];
+    return r;
+}
+__device__ __forceinline__ void store_row(const gs_params &p, int64_t d, const Row &r) {
+    __builtin_memcpy(p.mean + 3 * d, &r.mean, 12);
+    __builtin_memcpy(p.log_scale + 3 * d, &r.log_scale, 12);
+    *(f4a *)(p.rot + 4 * d) = r.rot;
+    p.value_logit[d] = r.value;
+    p.weight_logit[d] = r.weight;
+}
+
+// A row of the output.
+__device__ __forceinline__ void keep_row(const gs_params &in, const float *score, int64_t i, const gs_params &out,
+                                         float *score_out, int64_t d) {
+    const Row r = load_row(in, i);
+    if (score_out) score_out[d] = score[i];
+    store_row(out, d, r);
+}
+
+// The kept Gaussians of every stretch, in the order of their indices: a
+// tile's go to LDS, then their rows are copied side by side.
+__global__ __launch_bounds__(kBlock) void k_evict_keep(int64_t n, int64_t stretch, const float *__restrict__ score,
+                                                       const uint8_t *__restrict__ pinned,
+                                                       const Cut *__restrict__ cuts, const uint2 *__restrict__ sums,
+                                                       gs_params in, gs_params out, int32_t *__restrict__ source,
+                                                       float *__restrict__ score_out) {
+    __shared__ uint32_t lds[kWavesPerBlock];
+    __shared__ uint32_t s_kept[kTile];
+    const Cut cut = cuts[kDigits - 1];
     uint32_t above = 0, at = 0;
     for (uint32_t b = threadIdx.x; b < blockIdx.x; b += kBlock) {
         above += sums[b].x;
         at += sums[b].y;
     }
     uint32_t before, ties;  // above the cut and at it, in earlier stretches
-    block_excl_scan(above, lds, &before);
-    block_excl_scan(at, lds, &ties);
+    group_scan<kBlock>(above, lds, &before);
+    group_scan<kBlock>(at, lds, &ties);
     const int64_t i0 = (int64_t)blockIdx.x * stretch, i1 = i0 + stretch < n ? i0 + stretch : n;
-    for (int64_t t0 = i0; t0 < i1; t0 += kBlock) {
-        const int64_t i = t0 + threadIdx.x;
-        const bool in = i < i1;
-        const Key k = in ? load_key(score, pinned, i) : Key{0, 0};
-        const uint32_t up = in && above_cut(k, cut) ? 1u : 0u, tie = in && at_cut(k, cut) ? 1u : 0u;
-        uint32_t ups, more;
-        const uint32_t rank = before + block_excl_scan(up, lds, &ups);
-        const uint32_t place = ties + block_excl_scan(tie, lds, &more);
-        const uint32_t taken = place < cut.need ? place : cut.need;  // equals kept before this one
-        if (up || (tie && place < cut.need)) source[rank + taken] = (int32_t)i;
+    for (int64_t t0 = i0; t0 < i1; t0 += kTile) {
+        const int64_t i = t0 + threadIdx.x * kEach;
+        Key k[kEach];
+        const uint32_t m = load_keys(score, pinned, i, i1, k);
+        uint32_t mine = 0, total;  // above: low half, at: high half
+#pragma unroll
+        for (uint32_t t = 0; t < kEach; ++t)
+            if (t < m) mine += above_cut(k[t], cut) ? 1u : at_cut(k[t], cut) ? 0x10000u : 0u;
+        uint32_t run = group_scan<kBlock>(mine, lds, &total);
+        const uint32_t taken = ties < cut.need ? ties : cut.need;  // equals kept in earlier tiles
+        const uint32_t room = cut.need - taken;                    // and still to be kept
+#pragma unroll
+        for (uint32_t t = 0; t < kEach; ++t) {
+            const bool up = t < m && above_cut(k[t], cut), tie = t < m && at_cut(k[t], cut);
+            const uint32_t equals = run >> 16, kept = equals < room ? equals : room;
+            if (up || (tie && equals < room)) s_kept[(run & 0xFFFFu) + kept] = (uint32_t)(i + t);
+            run += up ? 1u : tie ? 0x10000u : 0u;
+        }
+        const uint32_t more = total >> 16, ups = total & 0xFFFFu;
+        const uint32_t count = ups + (more < room ? more : room);
+        const int64_t first = (int64_t)before + taken;
+        __syncthreads();
+        for (uint32_t r = threadIdx.x; r < count; r += kBlock) {
+            const uint32_t from = s_kept[r];
+            source[first + r] = (int32_t)from;
+            keep_row(in, score, from, out, score_out, first + r);
+        }
         before += ups;
         ties += more;
+        __syncthreads();
     }
 }
 
-// The rows of the kept Gaussians.
+// Small sets: the whole selection in one workgroup, its keys in registers.
+__global__ __launch_bounds__(kSmallThreads) void k_evict_small(int n, const float *__restrict__ score,
+                                                               const uint8_t *__restrict__ pinned, uint32_t keep,
+                                                               int32_t *__restrict__ source) {
+    constexpr int kTiles = (int)(kSmall / (kSmallThreads * kEach));
+    __shared__ uint32_t s_hist[kBins0];
+    __shared__ uint32_t lds[kSmallThreads / kWave + 2];
+    Key k[kTiles][kEach];
+    uint32_t m[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+        m[t] = load_keys(score, pinned, (t * kSmallThreads + threadIdx.x) * kEach, n, k[t]);
+    Cut cut{0, 0, keep, 0};
+    auto digit = [&](auto which) {
+        constexpr int D = decltype(which)::value;
+        for (uint32_t b = threadIdx.x; b < bins_of(D); b += kSmallThreads) s_hist[b] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+            if (t * (int)(kSmallThreads * kEach) >= n) continue;
+#pragma unroll
+            for (uint32_t j = 0; j < kEach; ++j) hist_add(s_hist, digit_of<D>(k[t][j]), j < m[t] && has_digits<D>(k[t][j], cut));
+        }
+        __syncthreads();
+        cut = next_digit<kSmallThreads, D, 1>(cut, s_hist, lds);
+        __syncthreads();
+    };
+    digit(std::integral_constant<int, 0>());
+    digit(std::integral_constant<int, 1>());
+    digit(std::integral_constant<int, 2>());
+    uint32_t before = 0, ties = 0;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        if (t * (int)(kSmallThreads * kEach) >= n) continue;
+        uint32_t mine = 0, total;
+#pragma unroll
+        for (uint32_t j = 0; j < kEach; ++j)
+            if (j < m[t]) mine += above_cut(k[t][j], cut) ? 1u : at_cut(k[t][j], cut) ? 0x10000u : 0u;
+        uint32_t run = group_scan<kSmallThreads>(mine, lds, &total) + (ties << 16) + before;
+#pragma unroll
+        for (uint32_t j = 0; j < kEach; ++j) {
+            const bool up = j < m[t] && above_cut(k[t][j], cut), tie = j < m[t] && at_cut(k[t][j], cut);
+            const uint32_t equals = run >> 16, kept = equals < cut.need ? equals : cut.need;
+            if (up || (tie && equals < cut.need))
+                source[(run & 0xFFFFu) + kept] = (t * (int)kSmallThreads + (int)threadIdx.x) * (int)kEach + (int)j;
+            run += up ? 1u : tie ? 0x10000u : 0u;
+        }
+        before += total & 0xFFFFu;
+        ties += total >> 16;
+    }
+}
+
 __global__ __launch_bounds__(kBlock) void k_evict_rows(int64_t keep, gs_params in, const float *__restrict__ score,
                                                        const int32_t *__restrict__ source, gs_params out,
                                                        float *__restrict__ score_out) {
     const int64_t d = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (d >= keep) return;
-    const int64_t i = source[d];
-#pragma unroll
-    for (int a = 0; a < 3; ++a) {
-        out.mean[3 * d + a] = in.mean[3 * i + a];
-        out.log_scale[3 * d + a] = in.log_scale[3 * i + a];
-    }
-#pragma unroll
-    for (int a = 0; a < 4; ++a) out.rot[4 * d + a] = in.rot[4 * i + a];
-    out.value_logit[d] = in.value_logit[i];
-    out.weight_logit[d] = in.weight_logit[i];
-    if (score_out) score_out[d] = score[i];
+    if (d < keep) keep_row(in, score, source[d], out, score_out, d);
 }
 
 // Copies. Counting the draws of a Gaussian touches only those drawn: their
 // counts are cleared, then raised by integer atomics (any order gives the
 // same), then every copy works out the shared weight from the logit that it
 // took along; the copies of one Gaussian write the same number to it.
+// Below one draw in so many Gaussians only the drawn ones' counts are cleared
+// (2 M Gaussians: all of them 4 us, 419430 draws' one by one 10 us).
+constexpr int64_t kClearAll = 16;
+
+__global__ __launch_bounds__(kBlock) void k_split_fill(int64_t n, uint32_t *__restrict__ copies) {
+    // the workspace is aligned and its size is a multiple of 256 bytes
+    const int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) * 4;
+    if (i < n) *(uint4 *)(copies + i) = make_uint4(1u, 1u, 1u, 1u);
+}
+
 __global__ __launch_bounds__(kBlock) void k_split_clear(int64_t n, const int32_t *__restrict__ ids, int64_t count,
                                                         uint32_t *__restrict__ copies) {
     const int64_t j = (int64_t)blockIdx.x * kBlock + threadIdx.x;
@@ -205,18 +403,22 @@ __global__ __launch_bounds__(kBlock) void k_split_rows(gs_params set, int64_t n,
     const int64_t j = (int64_t)blockIdx.x * kBlock + threadIdx.x;
     if (j >= count) return;
     const int64_t i = ids[j], d = n + j;
-    const bool some = i >= 0 && i < n;
-    if (some) atomicAdd(&copies[i], 1u);
-#pragma unroll
-    for (int a = 0; a < 3; ++a) {
-        set.mean[3 * d + a] = some ? set.mean[3 * i + a] : __uint_as_float(0x7FC00000u);
-        set.log_scale[3 * d + a] = some ? set.log_scale[3 * i + a] : 0.0f;
+    Row r;
+    float share = 0.0f;
+    if (i >= 0 && i < n) {
+        r = load_row(set, i);
+        if (score) share = score[i];
+        atomicAdd(&copies[i], 1u);
+    } else {
+        const float nan = __uint_as_float(0x7FC00000u);
+        r.mean = f3a{nan, nan, nan};
+        r.log_scale = f3a{0.0f, 0.0f, 0.0f};
+        r.rot = f4a{1.0f, 0.0f, 0.0f, 0.0f};
+        r.value = 0.0f;
+        r.weight = -__builtin_inff();
     }
-#pragma unroll
-    for (int a = 0; a < 4; ++a) set.rot[4 * d + a] = some ? set.rot[4 * i + a] : (a == 0 ? 1.0f : 0.0f);
-    set.value_logit[d] = some ? set.value_logit[i] : 0.0f;
-    set.weight_logit[d] = some ? set.weight_logit[i] : -__builtin_inff();
-    if (score) score[d] = some ? score[i] : 0.0f;
+    store_row(set, d, r);
+    if (score) score[d] = share;
     if (source) source[d] = i >= 0 ? (int32_t)(-1 - i) : -1;
 }
 
@@ -242,6 +444,7 @@ __global__ __launch_bounds__(kBlock) void k_split_weights(gs_params set, int64_t
 
 struct EvictWork {
     uint32_t *hist;
+    Cut *cuts;
     uint2 *sums;
     size_t bytes;
 };
@@ -249,8 +452,10 @@ EvictWork evict_layout(void *base) {
     EvictWork w;
     char *b = (char *)base;
     w.hist = (uint32_t *)b;
-    w.sums = (uint2 *)(b + al256(sizeof(uint32_t) * kBinsAll));
-    w.bytes = al256(sizeof(uint32_t) * kBinsAll) + al256(sizeof(uint2) * kBlocksMost);
+    w.cuts = (Cut *)(b + sizeof(uint32_t) * kBinsAll * kCopies);
+    const size_t head = al256(sizeof(uint32_t) * kBinsAll * kCopies + sizeof(Cut) * kDigits);
+    w.sums = (uint2 *)(b + head);
+    w.bytes = head + al256(sizeof(uint2) * kBlocksMost);
     return w;
 }
 
@@ -264,23 +469,33 @@ hipError_t launch_evict(const gs_params &in, int64_t n, const float *score, cons
                         const gs_params &out, int32_t *source, float *score_out, void *work, hipStream_t s) {
     if (keep <= 0) return hipSuccess;
     const EvictWork w = evict_layout(work);
+    const dim3 tb(kBlock);
+    const uint32_t k = (uint32_t)keep;
+    if (n <= kSmall) {
+        prof_begin("evict", s);
+        hipLaunchKernelGGL(k_evict_small, dim3(1), dim3(kSmallThreads), 0, s, (int)n, score, pinned, k, source);
+        hipLaunchKernelGGL(k_evict_rows, blocks_of(keep), tb, 0, s, keep, in, score, source, out, score_out);
+        prof_end("evict", s);
+        return hipGetLastError();
+    }
     // a stretch of whole tiles for every workgroup
     const int64_t tiles = (n + kTile - 1) / kTile;
-    const int64_t each = (tiles + kBlocksMost - 1) / kBlocksMost;
-    const int64_t stretch = each * kTile;
-    const dim3 nb((uint32_t)((n + stretch - 1) / stretch)), tb(kBlock);
-    const uint32_t k = (uint32_t)keep;
+    const int64_t stretch = (tiles + kBlocksMost - 1) / kBlocksMost * kTile;
+    const dim3 nb((uint32_t)((n + stretch - 1) / stretch));
+    const int64_t ctiles = (n + kCountThreads * kEach - 1) / (kCountThreads * kEach);
+    const int64_t cstretch = (ctiles + kCountBlocks - 1) / kCountBlocks * (kCountThreads * kEach);
+    const dim3 cb((uint32_t)((n + cstretch - 1) / cstretch)), ct(kCountThreads);
     hipError_t e;
     prof_begin("evict_select", s);
-    if ((e = fill_u32(w.hist, 0u, kBinsAll, s)) != hipSuccess) return e;
-    hipLaunchKernelGGL(k_evict_count<0>, nb, tb, 0, s, n, stretch, score, pinned, k, w.hist);
-    hipLaunchKernelGGL(k_evict_count<1>, nb, tb, 0, s, n, stretch, score, pinned, k, w.hist);
-    hipLaunchKernelGGL(k_evict_count<2>, nb, tb, 0, s, n, stretch, score, pinned, k, w.hist);
-    hipLaunchKernelGGL(k_evict_stretch, nb, tb, 0, s, n, stretch, score, pinned, k, w.hist, w.sums);
-    hipLaunchKernelGGL(k_evict_source, nb, tb, 0, s, n, stretch, score, pinned, k, w.hist, w.sums, source);
+    if ((e = fill_u32(w.hist, 0u, kBinsAll * kCopies, s)) != hipSuccess) return e;
+    hipLaunchKernelGGL(k_evict_count<0>, cb, ct, 0, s, n, cstretch, score, pinned, k, w.hist, w.cuts);
+    hipLaunchKernelGGL(k_evict_count<1>, cb, ct, 0, s, n, cstretch, score, pinned, k, w.hist, w.cuts);
+    hipLaunchKernelGGL(k_evict_count<2>, cb, ct, 0, s, n, cstretch, score, pinned, k, w.hist, w.cuts);
+    hipLaunchKernelGGL(k_evict_stretch, nb, tb, 0, s, n, stretch, score, pinned, k, w.hist, w.cuts, w.sums);
     prof_end("evict_select", s);
     prof_begin("evict_rows", s);
-    hipLaunchKernelGGL(k_evict_rows, blocks_of(keep), tb, 0, s, keep, in, score, source, out, score_out);
+    hipLaunchKernelGGL(k_evict_keep, nb, tb, 0, s, n, stretch, score, pinned, w.cuts, w.sums, in, out, source,
+                       score_out);
     prof_end("evict_rows", s);
     return hipGetLastError();
 }
@@ -290,7 +505,11 @@ hipError_t launch_split(const gs_params &set, int64_t n, const int32_t *ids, int
     if (count <= 0) return hipSuccess;
     const dim3 nb = blocks_of(count), tb(kBlock);
     prof_begin("split", s);
-    hipLaunchKernelGGL(k_split_clear, nb, tb, 0, s, n, ids, count, copies);
+    if (n > 0 && count >= n / kClearAll) {
+        hipLaunchKernelGGL(k_split_fill, blocks_of((n + 3) / 4), tb, 0, s, n, copies);
+    } else {
+        hipLaunchKernelGGL(k_split_clear, nb, tb, 0, s, n, ids, count, copies);
+    }
     hipLaunchKernelGGL(k_split_rows, nb, tb, 0, s, set, n, ids, count, source, score, copies);
     hipLaunchKernelGGL(k_split_weights, nb, tb, 0, s, set, n, ids, count, score, copies);
     prof_end("split", s);
