@@ -425,56 +425,67 @@ __global__ __launch_bounds__(NT) void k_draw_rows(DrawArgs a) {
 
 // ---- rows over many workgroups --------------------------------------------
 
-// A row is cut into stretches, a workgroup each, and a stretch into slices of
-// kSlice candidates, a wave each, four a lane.
+// The filters' passes cut a row into stretches, a large workgroup each; the
+// running masses are made in parts, kParts to a stretch, of slices of kSlice
+// candidates, a wave each, and quads of four, a lane each.
 constexpr uint32_t kThreads = 1024;
+constexpr uint32_t kParts = 4;
 constexpr uint32_t kSlice = 4 * kWave;
 constexpr int64_t kTile = 4 * kThreads;
+constexpr int64_t kPartTile = 4 * kBlock;
 constexpr uint32_t kStretches = 256;  // of all rows, about; of a row, at most
-constexpr uint32_t kBins = 2048;      // of a digit: 11, 11, 10 bits
+// A pass ends with an atomic add for every bin that a workgroup met, 20 to
+// 25 of them in a nanosecond on the whole chip: the first digit, which every
+// candidate has, gets few bins, the later ones the rest. Adds to one address
+// wait for each other, so rows of many stretches have copies of their bins.
 constexpr uint32_t kDigits = 3;
-// A pass ends with an atomic add for every bin that a workgroup met; those to
-// one address wait for each other, so rows of many stretches have copies of
-// their bins.
+constexpr uint32_t kBinsAll = 512 + 2048 + 4096;
+__device__ __host__ constexpr uint32_t bins_of(int digit) { return digit == 0 ? 512u : digit == 1 ? 2048u : 4096u; }
+__device__ __host__ constexpr uint32_t bins_before(int digit) {
+    return digit == 0 ? 0u : digit == 1 ? 512u : 512u + 2048u;
+}
 constexpr uint32_t kCopies = 4, kCopiesFrom = 64;
-// Up to one draw in so many candidates, a wave works out the masses of the
-// slice that a draw falls in; from there on every candidate's running mass is
-// written out, 8 bytes each, and a draw is a search. (A wave takes 300
-// instructions a draw: 10000 draws from 2 M candidates take it 6 us, as long
-// as the 16 MB.)
-constexpr int64_t kDrawSparse = 128;
 
-// What a row's passes have found so far; slot p: after digit p.
+// What a row's passes have found; slot p: after digit p.
 struct RowState {
+    uint32_t top, least, lift;                       // the row's keys, see Ends
     uint32_t count_z[kDigits], count_need[kDigits];  // top-k
-    uint32_t mass_z[kDigits], kept_ties;             // top-p; at the end what both keep
+    uint32_t mass_z[kDigits];                        // top-p
     uint64_t mass_left[kDigits];                     // mass that may still stand before
-    uint32_t kept_key, pad;
+    uint32_t in_key, in_ties;                        // what top-k leaves
+    uint32_t kept_key, kept_ties;                    // what both leave
+    uint32_t ranked, pad;                            // whether some equals of kept_key go
 };
+// The workgroups of a row are counted as they end a pass, in groups first (adds
+// to one address wait for each other).
+constexpr uint32_t kGroups = 16;
+constexpr uint32_t kTickets = kGroups + 1;
+constexpr uint32_t kPasses = 2 * kDigits;
 
 struct LongWork {
     RowState *state;      // [rows]
+    uint32_t *tickets;    // [rows][kPasses][kTickets]
     uint2 *ends;          // [rows][stretches] largest key, largest ~key
-    uint32_t *counts;     // [rows][copies][kDigits][kBins]
-    uint64_t *masses;     // [rows][copies][kDigits][kBins]
-    uint32_t *ties;       // [rows][stretches]
-    uint64_t *sums;       // [rows][stretches]
-    uint64_t *slice_run;  // [rows][stretches][slices]: mass up to the slice's end, in the stretch
-    uint32_t *slice_tie;  // [rows][stretches][slices]: equals of the last key before the slice, in the row
-    uint64_t *run;        // [rows][n]: mass in the slice (null: not kept)
-    int64_t stretch;
-    uint32_t stretches, slices, copies;
+    uint32_t *counts;     // [rows][copies][kBinsAll]
+    uint64_t *masses;     // [rows][copies][kBinsAll]
+    uint32_t *ties;       // [rows][parts] equals of the last key
+    uint64_t *sums;       // [rows][parts] masses
+    uint64_t *slice_run;  // [rows][parts][slices] mass up to the slice's end, in the part
+    uint64_t *quad_run;   // [rows][quads] mass up to the quad's end, in the slice
+    int64_t stretch, part, quads;
+    uint32_t stretches, parts, slices, copies;
     size_t bytes;
 };
 
-bool draws_sparse(int64_t n, int64_t draws) { return draws <= n / kDrawSparse; }
-
-LongWork long_layout(void *base, int64_t rows, int64_t n, int64_t draws) {
+LongWork long_layout(void *base, int64_t rows, int64_t n) {
     LongWork w;
     const int64_t most = rows >= (int64_t)kStretches ? 1 : (int64_t)kStretches / rows;
     w.stretch = ((n + most - 1) / most + kTile - 1) / kTile * kTile;
     w.stretches = (uint32_t)((n + w.stretch - 1) / w.stretch);
-    w.slices = (uint32_t)(w.stretch / kSlice);
+    w.part = w.stretch / kParts;
+    w.parts = (uint32_t)((n + w.part - 1) / w.part);
+    w.slices = (uint32_t)(w.part / kSlice);
+    w.quads = (n + 3) / 4;
     w.copies = w.stretches >= kCopiesFrom ? kCopies : 1;
     size_t off = 0;
     auto take = [&](size_t bytes) {
@@ -482,16 +493,16 @@ LongWork long_layout(void *base, int64_t rows, int64_t n, int64_t draws) {
         off += al256(bytes);
         return p;
     };
-    const size_t r = (size_t)rows, c = r * w.stretches;
+    const size_t r = (size_t)rows;
     w.state = (RowState *)take(sizeof(RowState) * r);
-    w.ends = (uint2 *)take(8 * c);
-    w.counts = (uint32_t *)take(4 * r * w.copies * kDigits * kBins);
-    w.masses = (uint64_t *)take(8 * r * w.copies * kDigits * kBins);
-    w.ties = (uint32_t *)take(4 * c);
-    w.sums = (uint64_t *)take(8 * c);
-    w.slice_run = (uint64_t *)take(8 * c * w.slices);
-    w.slice_tie = (uint32_t *)take(4 * c * w.slices);
-    w.run = draws_sparse(n, draws) ? nullptr : (uint64_t *)take(8 * r * (size_t)n);
+    w.tickets = (uint32_t *)take(4 * r * kPasses * kTickets);
+    w.ends = (uint2 *)take(8 * r * w.stretches);
+    w.counts = (uint32_t *)take(4 * r * w.copies * kBinsAll);
+    w.masses = (uint64_t *)take(8 * r * w.copies * kBinsAll);
+    w.ties = (uint32_t *)take(4 * r * w.parts);
+    w.sums = (uint64_t *)take(8 * r * w.parts);
+    w.slice_run = (uint64_t *)take(8 * r * w.parts * w.slices);
+    w.quad_run = (uint64_t *)take(8 * r * (size_t)w.quads);
     w.bytes = off;
     return w;
 }
@@ -501,43 +512,55 @@ LongWork long_layout(void *base, int64_t rows, int64_t n, int64_t draws) {
 struct Ends {
     uint32_t top, least, lift;
 };
+__device__ __forceinline__ Ends state_ends(const RowState &s) { return Ends{s.top, s.least, s.lift}; }
 __device__ __forceinline__ uint32_t offset_of(uint32_t key, const Ends &e) { return (key - e.least) << e.lift; }
 __device__ __forceinline__ uint32_t offset_key(uint32_t z, const Ends &e) { return e.least + (z >> e.lift); }
 __device__ __forceinline__ uint32_t digit_of(uint32_t z, int digit) {
-    return digit == 0 ? z >> 21 : digit == 1 ? z >> 10 & 2047u : z & 1023u;
+    return digit == 0 ? z >> 23 : digit == 1 ? z >> 12 & 2047u : z & 4095u;
 }
-__device__ __forceinline__ uint32_t digit_shift(int digit) { return digit == 0 ? 21u : digit == 1 ? 10u : 0u; }
+__device__ __forceinline__ uint32_t digit_shift(int digit) { return digit == 0 ? 23u : digit == 1 ? 12u : 0u; }
 // whether an offset has the digits before `digit` of another
 __device__ __forceinline__ bool same_before(uint32_t a, uint32_t b, int digit) {
     return digit == 0 || ((a ^ b) >> digit_shift(digit - 1)) == 0;
 }
 
+template <int NT>
 __device__ __forceinline__ Ends row_ends(const LongWork &w, int64_t row, uint64_t *lds) {
+    static_assert(NT >= (int)kStretches, "a stretch a thread");
     uint2 e = make_uint2(0, 0);
     if (threadIdx.x < w.stretches) e = w.ends[row * w.stretches + threadIdx.x];
-    const uint32_t top = group_max<kThreads>(e.x, lds), over = group_max<kThreads>(e.y, lds);
+    const uint32_t top = group_max<NT>(e.x, lds), over = group_max<NT>(e.y, lds);
     const uint32_t spread = top ? top - ~over : 0u;
     return Ends{top, ~over, (uint32_t)__builtin_clz(spread | 1u)};
+}
+
+// A word that other workgroups have added to in this launch.
+template <typename V>
+__device__ __forceinline__ V agent_load(const V *p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // The bin from the top in which the running sum passes `most` (above <= most <
 // above + its count); left: what `most` is more than the sum above it. False if
 // the sum of all is no more than `most`. share (not 2^64 - 1): most is that
 // share of the sum. extra is added to bin extra_bin.
-template <typename V>
+template <int NT, int DIGIT, typename V>
 __device__ bool cross_bin(const V *hist, uint32_t copies, uint64_t most, uint64_t share, uint32_t extra_bin,
                           uint64_t extra, uint32_t *bin, uint64_t *left, uint64_t *lds) {
-    constexpr uint32_t kMine = kBins / kThreads;
-    uint64_t *out = lds + kThreads / kWave;
+    constexpr uint32_t kBins = bins_of(DIGIT), kMine = kBins > NT ? kBins / NT : 1;
+    uint64_t *out = lds + NT / kWave;
     const uint32_t top = kBins - 1 - threadIdx.x * kMine;
     uint64_t c[kMine], sum = 0, total;
 #pragma unroll
     for (uint32_t j = 0; j < kMine; ++j) {
-        c[j] = top - j == extra_bin ? extra : 0;
-        for (uint32_t r = 0; r < copies; ++r) c[j] += hist[(size_t)r * kDigits * kBins + top - j];
+        c[j] = 0;
+        if (threadIdx.x * kMine + j < kBins) {
+            if (top - j == extra_bin) c[j] = extra;
+            for (uint32_t r = 0; r < copies; ++r) c[j] += agent_load(&hist[(size_t)r * kBinsAll + bins_before(DIGIT) + top - j]);
+        }
         sum += c[j];
     }
-    uint64_t above = group_scan<kThreads>(sum, lds, &total);
+    uint64_t above = group_scan<NT>(sum, lds, &total);
     if (share != ~(uint64_t)0) most = share_of(share, total);
     if (threadIdx.x == 0) {
         out[0] = 0;
@@ -558,83 +581,109 @@ __device__ bool cross_bin(const V *hist, uint32_t copies, uint64_t most, uint64_
     return most < total;
 }
 
-// top-k's offset with its digit `digit`, which pass `digit` counted; the row's
-// first workgroup keeps it for the later passes.
-__device__ Kept count_digit(const DrawArgs &a, const LongWork &w, int64_t row, int digit, bool keep, uint64_t *lds) {
+// Whether this workgroup is the last of its row to end a pass: it sees what the
+// others have added. Only atomics pass between the workgroups, and all of
+// them work on memory that the whole chip sees: each wave waits for its own to
+// be done, and the last workgroup reads with atomic loads. (A fence for the
+// whole chip would write the caches back: 70 us a pass.)
+__device__ bool last_of_row(const LongWork &w, int64_t row, uint32_t at, int pass, uint64_t *lds) {
+    uint32_t *t = w.tickets + ((size_t)row * kPasses + pass) * kTickets;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const uint32_t g = at % kGroups, groups = w.stretches < kGroups ? w.stretches : kGroups;
+        const uint32_t members = (w.stretches - g + kGroups - 1) / kGroups;
+        bool last = __hip_atomic_fetch_add(&t[g], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == members;
+        if (last)
+            last = __hip_atomic_fetch_add(&t[kGroups], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 == groups;
+        lds[0] = last;
+    }
+    __syncthreads();
+    const bool last = lds[0] != 0;
+    __syncthreads();
+    return last;
+}
+
+// The digit that a pass of top-k has counted, by the row's last workgroup.
+template <int DIGIT>
+__device__ void end_count(const DrawArgs &a, const LongWork &w, int64_t row, const Ends &e, uint64_t *lds) {
     RowState &s = w.state[row];
-    const uint32_t z0 = digit ? s.count_z[digit - 1] : 0u;
-    const uint32_t n0 = digit ? s.count_need[digit - 1] : a.top_k;
+    const uint32_t z0 = DIGIT ? s.count_z[DIGIT ? DIGIT - 1 : 0] : 0u;
+    const uint32_t n0 = DIGIT ? s.count_need[DIGIT ? DIGIT - 1 : 0] : a.top_k;
     uint64_t left;
     uint32_t b;
-    const bool found = cross_bin(w.counts + ((size_t)row * w.copies * kDigits + digit) * kBins, w.copies,
-                                 (uint64_t)n0 - 1, ~(uint64_t)0, kBins, 0, &b, &left, lds);
-    // (need 0: the row has fewer than top_k candidates)
-    const Kept k{z0 | b << digit_shift(digit), n0 && found ? (uint32_t)left + 1u : 0u};
-    if (keep && threadIdx.x == 0) {
-        s.count_z[digit] = k.key;
-        s.count_need[digit] = k.ties;
+    const bool found = cross_bin<kThreads, DIGIT>(w.counts + (size_t)row * w.copies * kBinsAll, w.copies,
+                                                  (uint64_t)n0 - 1, ~(uint64_t)0, ~0u, 0, &b, &left, lds);
+    if (threadIdx.x != 0) return;
+    // (need 0: the row has fewer than top_k candidates, and keeps them all)
+    const uint32_t z = z0 | b << digit_shift(DIGIT), need = n0 && found ? (uint32_t)left + 1u : 0u;
+    s.count_z[DIGIT] = z;
+    s.count_need[DIGIT] = need;
+    if (DIGIT == kDigits - 1) {
+        const bool all = need == 0 || e.top == 0;
+        s.in_key = s.kept_key = all ? 0u : offset_key(z, e);
+        s.in_ties = s.kept_ties = all ? 0xFFFFFFFFu : need;
+        s.ranked = !all;
     }
-    return k;
 }
 
-// What top-k leaves, after its passes; digit: whether its last digit is still
-// to be read off.
-__device__ Kept count_kept(const DrawArgs &a, const LongWork &w, int64_t row, const Ends &e, bool digit, bool keep,
-                           uint64_t *lds) {
-    Kept k{0, 0xFFFFFFFFu};
-    if (a.top_k >= (uint32_t)a.n) return k;
-    if (digit) {
-        k = count_digit(a, w, row, kDigits - 1, keep, lds);
-    } else {
-        k.key = w.state[row].count_z[kDigits - 1];
-        k.ties = w.state[row].count_need[kDigits - 1];
-    }
-    // a row of fewer than top_k candidates keeps them all
-    if (k.ties == 0 || e.top == 0) return Kept{0, 0xFFFFFFFFu};
-    return Kept{offset_key(k.key, e), k.ties};
+// What top-k left.
+__device__ __forceinline__ Kept count_kept(const DrawArgs &a, const LongWork &w, int64_t row) {
+    if (a.top_k >= (uint32_t)a.n) return Kept{0, 0xFFFFFFFFu};
+    return Kept{w.state[row].in_key, w.state[row].in_ties};
 }
 
-// The same of top-p's offset, by masses; `in`: what top-k left.
-__device__ Kept mass_digit(const DrawArgs &a, const LongWork &w, int64_t row, int digit, bool keep, Kept in,
-                           const Ends &e, const Scale &scale, uint64_t *left, uint64_t *lds) {
+// The same of top-p's digits, by masses.
+template <int DIGIT>
+__device__ void end_mass(const DrawArgs &a, const LongWork &w, int64_t row, const Kept &in, const Ends &e,
+                         const Scale &scale, uint64_t *lds) {
     RowState &s = w.state[row];
-    const uint32_t z0 = digit ? s.mass_z[digit - 1] : 0u;
+    const uint32_t z0 = DIGIT ? s.mass_z[DIGIT ? DIGIT - 1 : 0] : 0u;
     // top-k's equals, which the histogram leaves out
     const uint64_t extra = in.key ? mass_of(a, in.key, scale) * in.ties : 0;
     const uint32_t zi = in.key ? offset_of(in.key, e) : 0u;
-    const uint32_t extra_bin = in.key && same_before(zi, z0, digit) ? digit_of(zi, digit) : kBins;
+    const uint32_t extra_bin = in.key && same_before(zi, z0, DIGIT) ? digit_of(zi, DIGIT) : ~0u;
     uint32_t b;
-    cross_bin(w.masses + ((size_t)row * w.copies * kDigits + digit) * kBins, w.copies,
-              digit ? s.mass_left[digit ? digit - 1 : 0] : 0, digit ? ~(uint64_t)0 : a.share, extra_bin, extra, &b,
-              left, lds);
-    const Kept k{z0 | b << digit_shift(digit), 0};
-    if (keep && threadIdx.x == 0) {
-        s.mass_z[digit] = k.key;
-        s.mass_left[digit] = *left;
+    uint64_t left;
+    cross_bin<kThreads, DIGIT>(w.masses + (size_t)row * w.copies * kBinsAll, w.copies,
+                               DIGIT ? s.mass_left[DIGIT ? DIGIT - 1 : 0] : 0, DIGIT ? ~(uint64_t)0 : a.share,
+                               extra_bin, extra, &b, &left, lds);
+    if (threadIdx.x != 0) return;
+    const uint32_t z = z0 | b << digit_shift(DIGIT);
+    s.mass_z[DIGIT] = z;
+    s.mass_left[DIGIT] = left;
+    if (DIGIT == kDigits - 1) {
+        const uint32_t key = e.top ? offset_key(z, e) : 0u;
+        const uint64_t q = mass_of(a, key, scale);
+        uint64_t ties = q ? left / q + 1 : 0;
+        if (key == in.key && ties > in.ties) ties = in.ties;
+        s.kept_key = key;
+        s.kept_ties = ties < 0xFFFFFFFFu ? (uint32_t)ties : 0xFFFFFFFFu;
+        s.ranked = 1;
     }
-    return k;
 }
 
 struct Place {
-    int64_t row, i0, i1;  // the stretch of the row, cut to its length
-    uint32_t stretch;
+    int64_t row, i0, i1;  // the stretch (or part) of the row, cut to its length
+    uint32_t at;          // its number in the row
 };
-__device__ __forceinline__ Place place_of(const DrawArgs &a, const LongWork &w, uint64_t block) {
+__device__ __forceinline__ Place place_of(const DrawArgs &a, uint32_t pieces, int64_t length, uint64_t block) {
     Place p;
-    p.row = (int64_t)(block / w.stretches);
-    p.stretch = (uint32_t)(block % w.stretches);
+    p.row = (int64_t)(block / pieces);
+    p.at = (uint32_t)(block % pieces);
     const int64_t len = row_length(a, p.row);
-    p.i0 = (int64_t)p.stretch * w.stretch;
-    p.i1 = p.i0 + w.stretch < len ? p.i0 + w.stretch : len;
+    p.i0 = (int64_t)p.at * length;
+    p.i1 = p.i0 + length < len ? p.i0 + length : len;
     return p;
 }
 
 // Largest and smallest keys; clears the row's bins for the passes that follow.
 __global__ __launch_bounds__(kThreads) void k_draw_ends(DrawArgs a, LongWork w, uint64_t block0) {
     __shared__ uint64_t lds[kThreads / kWave];
-    const Place p = place_of(a, w, block0 + blockIdx.x);
-    const uint32_t bins = w.copies * kDigits * kBins;
-    for (uint32_t b = p.stretch * kThreads + threadIdx.x; b < bins; b += w.stretches * kThreads) {
+    const Place p = place_of(a, w.stretches, w.stretch, block0 + blockIdx.x);
+    const uint32_t bins = w.copies * kBinsAll;
+    if (p.at == 0 && threadIdx.x < kPasses * kTickets) w.tickets[(size_t)p.row * kPasses * kTickets + threadIdx.x] = 0;
+    for (uint32_t b = p.at * kThreads + threadIdx.x; b < bins; b += w.stretches * kThreads) {
         if (a.top_k < (uint32_t)a.n) w.counts[(size_t)p.row * bins + b] = 0;
         if (a.top_p) w.masses[(size_t)p.row * bins + b] = 0;
     }
@@ -650,19 +699,31 @@ __global__ __launch_bounds__(kThreads) void k_draw_ends(DrawArgs a, LongWork w, 
     }
     top = group_max<kThreads>(top, lds);
     over = group_max<kThreads>(over, lds);
-    if (threadIdx.x == 0) w.ends[p.row * w.stretches + p.stretch] = make_uint2(top, over);
+    if (threadIdx.x == 0) w.ends[p.row * w.stretches + p.at] = make_uint2(top, over);
+}
+
+// The ends of a row in its first pass, which keeps them, and in the others.
+__device__ __forceinline__ Ends pass_ends(const LongWork &w, const Place &p, bool first, uint64_t *lds) {
+    RowState &s = w.state[p.row];
+    if (!first) return state_ends(s);
+    const Ends e = row_ends<kThreads>(w, p.row, lds);
+    if (p.at == 0 && threadIdx.x == 0) {
+        s.top = e.top;
+        s.least = e.least;
+        s.lift = e.lift;
+    }
+    return e;
 }
 
 // Counts of a digit of the offsets that have top-k's earlier digits.
 template <int DIGIT>
 __global__ __launch_bounds__(kThreads) void k_draw_count(DrawArgs a, LongWork w, uint64_t block0) {
-    __shared__ uint32_t s_hist[kBins];
+    __shared__ uint32_t s_hist[bins_of(DIGIT)];
     __shared__ uint64_t lds[kThreads / kWave + 2];
-    const Place p = place_of(a, w, block0 + blockIdx.x);
-    for (uint32_t b = threadIdx.x; b < kBins; b += kThreads) s_hist[b] = 0;
-    const Ends e = row_ends(w, p.row, lds);
-    uint32_t z0 = 0;
-    if (DIGIT > 0) z0 = count_digit(a, w, p.row, DIGIT - 1, p.stretch == 0, lds).key;
+    const Place p = place_of(a, w.stretches, w.stretch, block0 + blockIdx.x);
+    for (uint32_t b = threadIdx.x; b < bins_of(DIGIT); b += kThreads) s_hist[b] = 0;
+    const Ends e = pass_ends(w, p, DIGIT == 0, lds);
+    const uint32_t z0 = DIGIT ? w.state[p.row].count_z[DIGIT ? DIGIT - 1 : 0] : 0u;
     __syncthreads();
     for (int64_t i = p.i0 + threadIdx.x * 4; i < p.i1; i += kTile) {
         uint32_t k[4];
@@ -674,24 +735,23 @@ __global__ __launch_bounds__(kThreads) void k_draw_count(DrawArgs a, LongWork w,
         }
     }
     __syncthreads();
-    uint32_t *out = w.counts + (((size_t)p.row * w.copies + p.stretch % w.copies) * kDigits + DIGIT) * kBins;
-    for (uint32_t b = threadIdx.x; b < kBins; b += kThreads)
+    uint32_t *out = w.counts + ((size_t)p.row * w.copies + p.at % w.copies) * kBinsAll + bins_before(DIGIT);
+    for (uint32_t b = threadIdx.x; b < bins_of(DIGIT); b += kThreads)
         if (s_hist[b]) atomicAdd(&out[b], s_hist[b]);
+    if (last_of_row(w, p.row, p.at, DIGIT, lds)) end_count<DIGIT>(a, w, p.row, e, lds);
 }
 
 // Masses of a digit of the offsets that have top-p's earlier digits.
 template <int DIGIT>
 __global__ __launch_bounds__(kThreads) void k_draw_mass(DrawArgs a, LongWork w, uint64_t block0) {
-    __shared__ unsigned long long s_hist[kBins];
+    __shared__ unsigned long long s_hist[bins_of(DIGIT)];
     __shared__ uint64_t lds[kThreads / kWave + 2];
-    const Place p = place_of(a, w, block0 + blockIdx.x);
-    for (uint32_t b = threadIdx.x; b < kBins; b += kThreads) s_hist[b] = 0;
-    const Ends e = row_ends(w, p.row, lds);
+    const Place p = place_of(a, w.stretches, w.stretch, block0 + blockIdx.x);
+    for (uint32_t b = threadIdx.x; b < bins_of(DIGIT); b += kThreads) s_hist[b] = 0;
+    const Ends e = pass_ends(w, p, DIGIT == 0 && a.top_k >= (uint32_t)a.n, lds);
     const Scale scale = scale_of(a, e.top);
-    const Kept in = count_kept(a, w, p.row, e, DIGIT == 0, p.stretch == 0, lds);
-    uint32_t z0 = 0;
-    uint64_t left;
-    if (DIGIT > 0) z0 = mass_digit(a, w, p.row, DIGIT - 1, p.stretch == 0, in, e, scale, &left, lds).key;
+    const Kept in = count_kept(a, w, p.row);
+    const uint32_t z0 = DIGIT ? w.state[p.row].mass_z[DIGIT ? DIGIT - 1 : 0] : 0u;
     __syncthreads();
     for (int64_t i = p.i0 + threadIdx.x * 4; i < p.i1; i += kTile) {
         uint32_t k[4];
@@ -707,62 +767,25 @@ __global__ __launch_bounds__(kThreads) void k_draw_mass(DrawArgs a, LongWork w, 
     }
     __syncthreads();
     unsigned long long *out = (unsigned long long *)(
-        w.masses + (((size_t)p.row * w.copies + p.stretch % w.copies) * kDigits + DIGIT) * kBins);
-    for (uint32_t b = threadIdx.x; b < kBins; b += kThreads)
+        w.masses + ((size_t)p.row * w.copies + p.at % w.copies) * kBinsAll + bins_before(DIGIT));
+    for (uint32_t b = threadIdx.x; b < bins_of(DIGIT); b += kThreads)
         if (s_hist[b]) atomicAdd(&out[b], s_hist[b]);
+    if (last_of_row(w, p.row, p.at, kDigits + DIGIT, lds)) end_mass<DIGIT>(a, w, p.row, in, e, scale, lds);
 }
 
-// What both filters keep; every workgroup of a row works it out.
-__device__ Kept row_kept(const DrawArgs &a, const LongWork &w, int64_t row, const Ends &e, const Scale &scale,
-                         uint64_t *lds) {
-    if (a.form == kBest) return Kept{e.top, 1};
-    const Kept in = count_kept(a, w, row, e, !a.top_p, false, lds);
-    if (!a.top_p) return in;
-    uint64_t left;
-    const Kept k = mass_digit(a, w, row, kDigits - 1, false, in, e, scale, &left, lds);
-    const uint32_t key = e.top ? offset_key(k.key, e) : 0u;
-    const uint64_t q = mass_of(a, key, scale);
-    uint64_t ties = q ? left / q + 1 : 0;
-    if (key == in.key && ties > in.ties) ties = in.ties;
-    return Kept{key, ties < 0xFFFFFFFFu ? (uint32_t)ties : 0xFFFFFFFFu};
+// The row's largest key and what the filters keep of it.
+__device__ __forceinline__ uint32_t row_kept(const DrawArgs &a, const LongWork &w, int64_t row, Kept *kept,
+                                             uint64_t *lds) {
+    if (a.top_p || a.top_k < (uint32_t)a.n) {
+        const RowState &s = w.state[row];
+        *kept = Kept{s.kept_key, s.kept_ties};
+        return s.top;
+    }
+    const uint32_t top = row_ends<kBlock>(w, row, lds).top;
+    *kept = a.form == kBest ? Kept{top, 1} : Kept{0, 0};
+    return top;
 }
 
-// Equals of the last key, per stretch; the row's first workgroup keeps what
-// the filters keep.
-__global__ __launch_bounds__(kThreads) void k_draw_ties(DrawArgs a, LongWork w, uint64_t block0) {
-    __shared__ uint64_t lds[kThreads / kWave + 2];
-    const Place p = place_of(a, w, block0 + blockIdx.x);
-    const Ends e = row_ends(w, p.row, lds);
-    const Kept kept = row_kept(a, w, p.row, e, scale_of(a, e.top), lds);
-    uint32_t ties = 0;
-    for (int64_t i = p.i0 + threadIdx.x * 4; i < p.i1; i += kTile) {
-        uint32_t k[4];
-        load_keys(a, p.row, i, p.i1, k);
-#pragma unroll
-        for (int t = 0; t < 4; ++t) ties += k[t] == kept.key ? 1u : 0u;
-    }
-    ties = group_sum<kThreads>(ties, lds);
-    if (threadIdx.x == 0) {
-        w.ties[p.row * w.stretches + p.stretch] = ties;
-        if (p.stretch == 0) {
-            w.state[p.row].kept_key = kept.key;
-            w.state[p.row].kept_ties = kept.ties;
-        }
-    }
-}
-
-// q of four candidates of which `before` equals of the last key come earlier.
-template <bool CUT>
-__device__ __forceinline__ void masses_of(const DrawArgs &a, const Scale &scale, const Kept &kept, const uint32_t k[4],
-                                          uint32_t before, uint64_t q[4]) {
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        bool stays = !CUT || k[t] > kept.key;
-        if (CUT && k[t] == kept.key) stays = before++ < kept.ties;
-        q[t] = stays ? mass_of(a, k[t], scale) : 0;
-        if ((double)q[t] < a.least) q[t] = 0;
-    }
-}
 __device__ __forceinline__ uint32_t ties_of(const Kept &kept, const uint32_t k[4]) {
     uint32_t n = 0;
 #pragma unroll
@@ -770,105 +793,91 @@ __device__ __forceinline__ uint32_t ties_of(const Kept &kept, const uint32_t k[4
     return n;
 }
 
-// Running masses of the slices of a stretch, and where wanted of their
-// candidates. CUT: whether a filter by order is on.
+// Equals of the last key, per part.
+__global__ __launch_bounds__(kBlock) void k_draw_ties(DrawArgs a, LongWork w, uint64_t block0) {
+    __shared__ uint64_t lds[kWavesPerBlock + 2];
+    const Place p = place_of(a, w.parts, w.part, block0 + blockIdx.x);
+    Kept kept;
+    row_kept(a, w, p.row, &kept, lds);
+    uint32_t ties = 0;
+    for (int64_t i = p.i0 + threadIdx.x * 4; i < p.i1; i += kPartTile) {
+        uint32_t k[4];
+        load_keys(a, p.row, i, p.i1, k);
+        ties += ties_of(kept, k);
+    }
+    ties = group_sum<kBlock>(ties, lds);
+    if (threadIdx.x == 0) w.ties[p.row * w.parts + p.at] = ties;
+}
+
+// q of a candidate by itself: what the filters leave of it if it stays.
+__device__ __forceinline__ uint64_t mass_left(const DrawArgs &a, const Scale &scale, uint32_t key) {
+    const uint64_t q = mass_of(a, key, scale);
+    return (double)q < a.least ? 0 : q;
+}
+
+// Running masses of the quads of a slice, the slices of a part, and the parts'
+// sums. CUT: whether a filter by order is on.
 template <bool CUT>
-__global__ __launch_bounds__(kThreads) void k_draw_run(DrawArgs a, LongWork w, uint64_t block0) {
-    __shared__ uint64_t lds[kThreads / kWave];
-    const Place p = place_of(a, w, block0 + blockIdx.x);
+__global__ __launch_bounds__(kBlock) void k_draw_run(DrawArgs a, LongWork w, uint64_t block0) {
+    __shared__ uint64_t lds[kWavesPerBlock];
+    const uint64_t block = block0 + blockIdx.x;
+    const Place p = place_of(a, w.parts, w.part, block);
     const uint32_t lane = threadIdx.x % kWave;
-    const Ends e = row_ends(w, p.row, lds);
-    const Scale scale = scale_of(a, e.top);
-    Kept kept{0, 0};
+    Kept kept;
+    const Scale scale = scale_of(a, row_kept(a, w, p.row, &kept, lds));
     uint32_t place = 0;  // equals before
     if (CUT) {
-        kept = Kept{w.state[p.row].kept_key, w.state[p.row].kept_ties};
-        place = group_sum<kThreads>(threadIdx.x < p.stretch ? w.ties[p.row * w.stretches + threadIdx.x] : 0u, lds);
+        for (uint32_t b = threadIdx.x; b < p.at; b += kBlock) place += w.ties[p.row * w.parts + b];
+        place = group_sum<kBlock>(place, lds);
     }
     uint64_t run = 0;
-    const int64_t end = p.i0 + w.stretch < a.n ? p.i0 + w.stretch : a.n;
-    for (int64_t t0 = p.i0; t0 < end; t0 += kTile) {
+    const int64_t end = p.i0 + w.part < a.n ? p.i0 + w.part : a.n;
+    for (int64_t t0 = p.i0; t0 < end; t0 += kPartTile) {
         const int64_t j = t0 + threadIdx.x * 4;
-        uint32_t k[4];
+        uint32_t k[4], before = 0, all;
         load_keys(a, p.row, j, p.i1, k);
-        uint32_t before = 0, all;
         if (CUT) {
-            before = place + group_scan<kThreads>(ties_of(kept, k), lds, &all);
+            before = place + group_scan<kBlock>(ties_of(kept, k), lds, &all);
             place += all;
         }
-        uint64_t q[4], total;
-        masses_of<CUT>(a, scale, kept, k, before, q);
-        const uint64_t mine = q[0] + q[1] + q[2] + q[3];
-        const uint64_t to = run + group_scan<kThreads>(mine, lds, &total) + mine;  // up to this lane's end
-        const uint64_t at = (uint64_t)blockIdx.x + block0;
-        const size_t slice = at * w.slices + (size_t)((t0 - p.i0) / kSlice) + threadIdx.x / kWave;
-        if (lane == kWave - 1) w.slice_run[slice] = to;
-        if (CUT && lane == 0) w.slice_tie[slice] = before;
-        if (w.run && j < end) {
-            // from the slice's start
-            const uint64_t from = to - mine;
-            const uint64_t r = from - ((uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(from >> 32)) << 32 |
-                                 (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)from));
-            uint64_t *out = w.run + p.row * a.n + j;
-            const uint64_t r0 = r + q[0], r1 = r0 + q[1], r2 = r1 + q[2], r3 = r2 + q[3];
-            if (j + 4 <= end) {
-                typedef uint64_t u2 __attribute__((ext_vector_type(2), aligned(8)));
-                *(u2 *)out = u2{r0, r1};
-                *(u2 *)(out + 2) = u2{r2, r3};
-            } else {
-                out[0] = r0;
-                if (j + 1 < end) out[1] = r1;
-                if (j + 2 < end) out[2] = r2;
-            }
+        uint64_t mine = 0, total;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            bool stays = k[t] > kept.key;
+            if (CUT && k[t] == kept.key) stays = before++ < kept.ties;
+            if (stays) mine += mass_left(a, scale, k[t]);
         }
+        const uint64_t upto = wave_scan(mine);  // in the slice
+        if (j < end) w.quad_run[p.row * w.quads + j / 4] = upto;
+        const uint64_t slice = run + group_scan<kBlock>(mine, lds, &total) + mine;
+        if (lane == kWave - 1) w.slice_run[block * w.slices + (size_t)((t0 - p.i0) / kSlice) + threadIdx.x / kWave] = slice;
         run += total;
     }
-    if (threadIdx.x == 0) w.sums[p.row * w.stretches + p.stretch] = run;
+    if (threadIdx.x == 0) w.sums[p.row * w.parts + p.at] = run;
 }
 
-// Running masses of a row's stretches, in LDS (kBlock threads).
-__device__ __forceinline__ uint64_t stretch_runs(const LongWork &w, int64_t row, uint64_t *s_run, uint64_t *lds) {
-    static_assert(kStretches == kBlock, "a stretch a thread");
-    uint64_t total;
-    const uint64_t sum = threadIdx.x < w.stretches ? w.sums[row * w.stretches + threadIdx.x] : 0;
-    s_run[threadIdx.x] = group_scan<kBlock>(sum, lds, &total) + sum;
-    __syncthreads();
-    return total;
-}
-
-// The stretch and slice that mass r of a row falls in; r becomes what it is
-// into the slice.
-struct Found {
-    uint32_t stretch, slice;
-};
-__device__ __forceinline__ Found find_slice(const DrawArgs &a, const LongWork &w, int64_t row, const uint64_t *s_run,
-                                            uint64_t &r) {
-    Found f{0, 0};
-#pragma unroll
-    for (uint32_t step = kStretches / 2; step > 0; step /= 2)
-        if (s_run[f.stretch + step - 1] <= r) f.stretch += step;
-    if (f.stretch) r -= s_run[f.stretch - 1];
-    const uint64_t *v = w.slice_run + ((size_t)row * w.stretches + f.stretch) * w.slices;
-    const int64_t rest = a.n - (int64_t)f.stretch * w.stretch;
-    uint32_t hi = (uint32_t)(rest < w.stretch ? (rest + kSlice - 1) / kSlice : w.slices) - 1;
-    while (f.slice < hi) {
-        const uint32_t mid = (f.slice + hi) / 2;
-        if (v[mid] > r)
-            hi = mid;
-        else
-            f.slice = mid + 1;
-    }
-    if (f.slice) r -= v[f.slice - 1];
-    return f;
-}
-
-// The draws, a thread each: a workgroup takes kBlock of a row's.
+// The draws, a thread each: a workgroup takes kBlock of a row's. The part is
+// found in LDS, the slice and the quad in their running masses, and the
+// candidate from the scores of its quad.
+template <bool CUT>
 __global__ __launch_bounds__(kBlock) void k_draw_search(DrawArgs a, LongWork w, uint64_t groups, uint64_t block0) {
-    __shared__ uint64_t s_run[kStretches];
+    constexpr uint32_t kMost = kStretches * kParts, kMine = kMost / kBlock;
+    __shared__ uint64_t s_run[kMost];
     __shared__ uint64_t lds[kWavesPerBlock];
     const int64_t row = (int64_t)((block0 + blockIdx.x) / groups);
     const int64_t d = (int64_t)((block0 + blockIdx.x) % groups) * kBlock + threadIdx.x;
-    const uint64_t total = stretch_runs(w, row, s_run, lds);
+    uint64_t c[kMine], sum = 0, total;
+#pragma unroll
+    for (uint32_t j = 0; j < kMine; ++j) {
+        const uint32_t at = threadIdx.x * kMine + j;
+        sum += c[j] = at < w.parts ? w.sums[row * w.parts + at] : 0;
+    }
+    uint64_t run = group_scan<kBlock>(sum, lds, &total);
+#pragma unroll
+    for (uint32_t j = 0; j < kMine; ++j) s_run[threadIdx.x * kMine + j] = run += c[j];
+    Kept kept;
+    const Scale scale = scale_of(a, row_kept(a, w, row, &kept, lds));
+    __syncthreads();
     if (d >= a.draws) return;
     const int64_t at = row * a.draws + d;
     if (total == 0) {
@@ -876,59 +885,61 @@ __global__ __launch_bounds__(kBlock) void k_draw_search(DrawArgs a, LongWork w, 
         return;
     }
     uint64_t r = share_of(uniform_bits(a.uniform[at]), total);
-    const Found f = find_slice(a, w, row, s_run, r);
-    const int64_t first = (int64_t)f.stretch * w.stretch + (int64_t)f.slice * kSlice;
-    const uint64_t *v = w.run + row * a.n + first;
-    uint32_t lo = 0, last = (uint32_t)((first + kSlice < a.n ? (int64_t)kSlice : a.n - first) - 1);
-    while (lo < last) {
-        const uint32_t mid = (lo + last) / 2;
-        if (v[mid] > r)
-            last = mid;
-        else
-            lo = mid + 1;
-    }
-    write_draw(a, at, first + lo, v[lo] - (lo ? v[lo - 1] : 0), total);
-}
-
-// The draws, a wave each, from the scores of their slices.
-template <bool CUT>
-__global__ __launch_bounds__(kBlock) void k_draw_slice(DrawArgs a, LongWork w, uint64_t groups, uint64_t block0) {
-    __shared__ uint64_t s_run[kStretches];
-    __shared__ uint64_t lds[kThreads / kWave];
-    const int64_t row = (int64_t)((block0 + blockIdx.x) / groups);
-    const int64_t d = (int64_t)((block0 + blockIdx.x) % groups) * kWavesPerBlock + threadIdx.x / kWave;
-    const uint32_t lane = threadIdx.x % kWave;
-    const uint64_t total = stretch_runs(w, row, s_run, lds);
-    uint32_t top = 0;
-    if (threadIdx.x < w.stretches) top = w.ends[row * w.stretches + threadIdx.x].x;
-    const Scale scale = scale_of(a, group_max<kBlock>(top, lds));
-    if (d >= a.draws) return;
-    const int64_t at = row * a.draws + d;
-    if (total == 0) {
-        if (lane == 0) write_draw(a, at, -1, 0, 1);
-        return;
-    }
-    uint64_t r = share_of(uniform_bits(a.uniform[at]), total);
-    const Found f = find_slice(a, w, row, s_run, r);
-    const int64_t first = (int64_t)f.stretch * w.stretch + (int64_t)f.slice * kSlice;
-    Kept kept{0, 0};
-    uint32_t k[4], before = 0;
-    load_keys(a, row, first + lane * 4, row_length(a, row), k);
-    if (CUT) {
-        kept = Kept{w.state[row].kept_key, w.state[row].kept_ties};
-        const uint32_t mine = ties_of(kept, k);
-        before = w.slice_tie[((size_t)row * w.stretches + f.stretch) * w.slices + f.slice] + wave_scan(mine) - mine;
-    }
-    uint64_t q[4];
-    masses_of<CUT>(a, scale, kept, k, before, q);
-    const uint64_t mine = q[0] + q[1] + q[2] + q[3];
-    uint64_t run = wave_scan(mine) - mine;
-    // the one lane and candidate whose mass holds r
+    uint32_t part = 0;
+#pragma unroll
+    for (uint32_t step = kMost / 2; step > 0; step /= 2)
+        if (s_run[part + step - 1] <= r) part += step;
+    if (part) r -= s_run[part - 1];
+    // the first entry of a running sum that is more than r; r: what is left
+    auto find = [&](const uint64_t *v, uint32_t count) {
+        uint32_t lo = 0, hi = count - 1;
+        uint64_t below = 0;
+        while (lo < hi) {
+            const uint32_t mid = (lo + hi) / 2;
+            const uint64_t x = v[mid];
+            if (x > r) {
+                hi = mid;
+            } else {
+                lo = mid + 1;
+                below = x;
+            }
+        }
+        r -= below;
+        return lo;
+    };
+    const int64_t rest = a.n - (int64_t)part * w.part;
+    const uint32_t slice = find(w.slice_run + ((size_t)row * w.parts + part) * w.slices,
+                                (uint32_t)(rest < w.part ? (rest + kSlice - 1) / kSlice : w.slices));
+    const int64_t first = (int64_t)part * w.part + (int64_t)slice * kSlice;
+    const uint64_t *quads = w.quad_run + row * w.quads + first / 4;
+    const uint32_t quad = find(quads, first + kSlice < a.n ? kSlice / 4 : (uint32_t)((a.n - first + 3) / 4));
+    const int64_t j = first + quad * 4;
+    uint32_t k[4];
+    load_keys(a, row, j, row_length(a, row), k);
+    uint64_t q[4], larger = 0, equal = 0;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-        if (run <= r && r < run + q[t]) write_draw(a, at, first + lane * 4 + t, q[t], total);
-        run += q[t];
+        q[t] = k[t] > kept.key || (CUT && k[t] == kept.key) ? mass_left(a, scale, k[t]) : 0;
+        if (k[t] > kept.key) larger += q[t];
     }
+    if (CUT && kept.key) equal = mass_left(a, scale, kept.key);
+    // how many of the equals stay: what is in the quad's mass
+    uint64_t staying = 0;
+    if (equal) staying = (quads[quad] - (quad ? quads[quad - 1] : 0) - larger) / equal;
+    uint32_t id = 0;
+    uint64_t mass = 0, upto = 0;
+    bool found = false;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        if (CUT && k[t] == kept.key && (staying == 0 || staying-- == 0)) q[t] = 0;
+        upto += q[t];
+        if (!found && upto > r) {
+            found = true;
+            id = t;
+            mass = q[t];
+        }
+    }
+    write_draw(a, at, j + id, mass, total);
 }
 
 constexpr int64_t kRowSmall = 512, kRowMiddle = 4096, kRowLarge = 16384;
@@ -936,8 +947,8 @@ constexpr uint64_t kBlocksMost = (uint64_t)1 << 21;  // workgroups of a launch (
 
 }  // namespace
 
-size_t draw_work_bytes(int64_t rows, int64_t n, int64_t draws) {
-    return n <= kRowLarge || rows == 0 ? 256 : long_layout(nullptr, rows, n, draws).bytes;
+size_t draw_work_bytes(int64_t rows, int64_t n, int64_t) {
+    return n <= kRowLarge || rows == 0 ? 256 : long_layout(nullptr, rows, n).bytes;
 }
 
 hipError_t launch_draw(int64_t rows, int64_t n, const void *scores, int64_t stride, const int32_t *lengths,
@@ -978,12 +989,12 @@ hipError_t launch_draw(int64_t rows, int64_t n, const void *scores, int64_t stri
         prof_end("draw_rows", s);
         return hipGetLastError();
     }
-    const LongWork w = long_layout(work, rows, n, draws);
+    const LongWork w = long_layout(work, rows, n);
     auto over = [](uint64_t blocks, auto launch) {
         for (uint64_t b = 0; b < blocks; b += kBlocksMost)
             launch(dim3((uint32_t)(blocks - b < kBlocksMost ? blocks - b : kBlocksMost)), b);
     };
-    const uint64_t blocks = (uint64_t)rows * w.stretches;
+    const uint64_t blocks = (uint64_t)rows * w.stretches, parts = (uint64_t)rows * w.parts;
     const dim3 tb(kThreads), pb(kBlock);
     prof_begin("draw_filter", s);
     over(blocks, [&](dim3 nb, uint64_t b) { hipLaunchKernelGGL(k_draw_ends, nb, tb, 0, s, a, w, b); });
@@ -998,24 +1009,17 @@ hipError_t launch_draw(int64_t rows, int64_t n, const void *scores, int64_t stri
         over(blocks, [&](dim3 nb, uint64_t b) { hipLaunchKernelGGL(k_draw_mass<2>, nb, tb, 0, s, a, w, b); });
     }
     const bool cut = a.top_k != 0xFFFFFFFFu || a.top_p || a.form == kBest;
-    if (cut) over(blocks, [&](dim3 nb, uint64_t b) { hipLaunchKernelGGL(k_draw_ties, nb, tb, 0, s, a, w, b); });
+    if (cut) over(parts, [&](dim3 nb, uint64_t b) { hipLaunchKernelGGL(k_draw_ties, nb, pb, 0, s, a, w, b); });
     prof_end("draw_filter", s);
     prof_begin("draw_pick", s);
-    if (cut)
-        over(blocks, [&](dim3 nb, uint64_t b) { hipLaunchKernelGGL(k_draw_run<true>, nb, tb, 0, s, a, w, b); });
-    else
-        over(blocks, [&](dim3 nb, uint64_t b) { hipLaunchKernelGGL(k_draw_run<false>, nb, tb, 0, s, a, w, b); });
-    const uint64_t each = w.run ? kBlock : kWavesPerBlock;
-    const uint64_t groups = ((uint64_t)draws + each - 1) / each;
-    if (w.run)
-        over((uint64_t)rows * groups,
-             [&](dim3 nb, uint64_t b) { hipLaunchKernelGGL(k_draw_search, nb, pb, 0, s, a, w, groups, b); });
-    else if (cut)
-        over((uint64_t)rows * groups,
-             [&](dim3 nb, uint64_t b) { hipLaunchKernelGGL(k_draw_slice<true>, nb, pb, 0, s, a, w, groups, b); });
-    else
-        over((uint64_t)rows * groups,
-             [&](dim3 nb, uint64_t b) { hipLaunchKernelGGL(k_draw_slice<false>, nb, pb, 0, s, a, w, groups, b); });
+    const uint64_t groups = ((uint64_t)draws + kBlock - 1) / kBlock, draw_blocks = (uint64_t)rows * groups;
+    if (cut) {
+        over(parts, [&](dim3 nb, uint64_t b) { hipLaunchKernelGGL(k_draw_run<true>, nb, pb, 0, s, a, w, b); });
+        over(draw_blocks, [&](dim3 nb, uint64_t b) { hipLaunchKernelGGL(k_draw_search<true>, nb, pb, 0, s, a, w, groups, b); });
+    } else {
+        over(parts, [&](dim3 nb, uint64_t b) { hipLaunchKernelGGL(k_draw_run<false>, nb, pb, 0, s, a, w, b); });
+        over(draw_blocks, [&](dim3 nb, uint64_t b) { hipLaunchKernelGGL(k_draw_search<false>, nb, pb, 0, s, a, w, groups, b); });
+    }
     prof_end("draw_pick", s);
     return hipGetLastError();
 }
