@@ -437,40 +437,47 @@ constexpr uint32_t kStretches = 256;  // of all rows, about; of a row, at most
 // A pass ends with an atomic add for every bin that a workgroup met, 20 to
 // 25 of them in a nanosecond on the whole chip: the first digit, which every
 // candidate has, gets few bins, the later ones the rest. Adds to one address
-// wait for each other, so rows of many stretches have copies of their bins.
+// wait for each other, so rows of many stretches have copies of its bins.
 constexpr uint32_t kDigits = 3;
-constexpr uint32_t kBinsAll = 512 + 2048 + 4096;
-__device__ __host__ constexpr uint32_t bins_of(int digit) { return digit == 0 ? 512u : digit == 1 ? 2048u : 4096u; }
-__device__ __host__ constexpr uint32_t bins_before(int digit) {
-    return digit == 0 ? 0u : digit == 1 ? 512u : 512u + 2048u;
-}
 constexpr uint32_t kCopies = 4, kCopiesFrom = 64;
+constexpr uint32_t kBins0 = 512, kBins1 = 4096, kBins2 = 2048;
+constexpr uint32_t kBinsAll = kCopies * kBins0 + kBins1 + kBins2;
+__device__ constexpr uint32_t bins_of(int digit) { return digit == 0 ? kBins0 : digit == 1 ? kBins1 : kBins2; }
+__device__ constexpr uint32_t bins_before(int digit) {
+    return digit == 0 ? 0u : digit == 1 ? kCopies * kBins0 : kCopies * kBins0 + kBins1;
+}
 
+// The digits found of an offset; left: candidates to be taken (top-k) or mass
+// that may still stand before (top-p) among those that have them.
+struct Digit {
+    uint64_t left;
+    uint32_t z, pad;
+};
 // What a row's passes have found; slot p: after digit p.
 struct RowState {
     uint32_t top, least, lift;                       // the row's keys, see Ends
-    uint32_t count_z[kDigits], count_need[kDigits];  // top-k
-    uint32_t mass_z[kDigits];                        // top-p
-    uint64_t mass_left[kDigits];                     // mass that may still stand before
+    uint32_t pad;
+    Digit count[kDigits], mass[kDigits];             // top-k, top-p
     uint32_t in_key, in_ties;                        // what top-k leaves
     uint32_t kept_key, kept_ties;                    // what both leave
-    uint32_t ranked, pad;                            // whether some equals of kept_key go
+    uint64_t ranked;                                 // whether some equals of kept_key go
 };
 // The workgroups of a row are counted as they end a pass, in groups first (adds
 // to one address wait for each other).
 constexpr uint32_t kGroups = 16;
 constexpr uint32_t kTickets = kGroups + 1;
-constexpr uint32_t kPasses = 2 * kDigits;
+constexpr uint32_t kPasses = 2;  // that end with the last workgroup: top-k's and top-p's last
 
 struct LongWork {
     RowState *state;      // [rows]
     uint32_t *tickets;    // [rows][kPasses][kTickets]
     uint2 *ends;          // [rows][stretches] largest key, largest ~key
-    uint32_t *counts;     // [rows][copies][kBinsAll]
-    uint64_t *masses;     // [rows][copies][kBinsAll]
+    uint32_t *counts;     // [rows][kBinsAll]
+    uint64_t *masses;     // [rows][kBinsAll]
     uint32_t *ties;       // [rows][parts] equals of the last key
     uint64_t *sums;       // [rows][parts] masses
     uint64_t *slice_run;  // [rows][parts][slices] mass up to the slice's end, in the part
+    uint64_t *oct_run;    // [rows][parts][slices][8] mass up to the end of eight quads, in the slice
     uint64_t *quad_run;   // [rows][quads] mass up to the quad's end, in the slice
     int64_t stretch, part, quads;
     uint32_t stretches, parts, slices, copies;
@@ -497,12 +504,13 @@ LongWork long_layout(void *base, int64_t rows, int64_t n) {
     w.state = (RowState *)take(sizeof(RowState) * r);
     w.tickets = (uint32_t *)take(4 * r * kPasses * kTickets);
     w.ends = (uint2 *)take(8 * r * w.stretches);
-    w.counts = (uint32_t *)take(4 * r * w.copies * kBinsAll);
-    w.masses = (uint64_t *)take(8 * r * w.copies * kBinsAll);
+    w.counts = (uint32_t *)take(4 * r * kBinsAll);
+    w.masses = (uint64_t *)take(8 * r * kBinsAll);
     w.ties = (uint32_t *)take(4 * r * w.parts);
     w.sums = (uint64_t *)take(8 * r * w.parts);
-    w.slice_run = (uint64_t *)take(8 * r * w.parts * w.slices);
-    w.quad_run = (uint64_t *)take(8 * r * (size_t)w.quads);
+    w.slice_run = (uint64_t *)take(8 * (r * w.parts * w.slices + 8));
+    w.oct_run = (uint64_t *)take(64 * r * w.parts * w.slices);
+    w.quad_run = (uint64_t *)take(8 * (r * (size_t)w.quads + 8));
     w.bytes = off;
     return w;
 }
@@ -516,9 +524,9 @@ __device__ __forceinline__ Ends state_ends(const RowState &s) { return Ends{s.to
 __device__ __forceinline__ uint32_t offset_of(uint32_t key, const Ends &e) { return (key - e.least) << e.lift; }
 __device__ __forceinline__ uint32_t offset_key(uint32_t z, const Ends &e) { return e.least + (z >> e.lift); }
 __device__ __forceinline__ uint32_t digit_of(uint32_t z, int digit) {
-    return digit == 0 ? z >> 23 : digit == 1 ? z >> 12 & 2047u : z & 4095u;
+    return digit == 0 ? z >> 23 : digit == 1 ? z >> 11 & 4095u : z & 2047u;
 }
-__device__ __forceinline__ uint32_t digit_shift(int digit) { return digit == 0 ? 23u : digit == 1 ? 12u : 0u; }
+__device__ __forceinline__ uint32_t digit_shift(int digit) { return digit == 0 ? 23u : digit == 1 ? 11u : 0u; }
 // whether an offset has the digits before `digit` of another
 __device__ __forceinline__ bool same_before(uint32_t a, uint32_t b, int digit) {
     return digit == 0 || ((a ^ b) >> digit_shift(digit - 1)) == 0;
@@ -541,12 +549,13 @@ __device__ __forceinline__ V agent_load(const V *p) {
 }
 
 // The bin from the top in which the running sum passes `most` (above <= most <
-// above + its count); left: what `most` is more than the sum above it. False if
+// above + its count); left: what `most` is more than the sum above it, in_bin:
+// its count. False if
 // the sum of all is no more than `most`. share (not 2^64 - 1): most is that
 // share of the sum. extra is added to bin extra_bin.
 template <int NT, int DIGIT, typename V>
 __device__ bool cross_bin(const V *hist, uint32_t copies, uint64_t most, uint64_t share, uint32_t extra_bin,
-                          uint64_t extra, uint32_t *bin, uint64_t *left, uint64_t *lds) {
+                          uint64_t extra, uint32_t *bin, uint64_t *left, uint64_t *in_bin, uint64_t *lds) {
     constexpr uint32_t kBins = bins_of(DIGIT), kMine = kBins > NT ? kBins / NT : 1;
     uint64_t *out = lds + NT / kWave;
     const uint32_t top = kBins - 1 - threadIdx.x * kMine;
@@ -556,7 +565,8 @@ __device__ bool cross_bin(const V *hist, uint32_t copies, uint64_t most, uint64_
         c[j] = 0;
         if (threadIdx.x * kMine + j < kBins) {
             if (top - j == extra_bin) c[j] = extra;
-            for (uint32_t r = 0; r < copies; ++r) c[j] += agent_load(&hist[(size_t)r * kBinsAll + bins_before(DIGIT) + top - j]);
+            for (uint32_t r = 0; r < (DIGIT ? 1u : copies); ++r)
+                c[j] += agent_load(&hist[r * kBins0 + bins_before(DIGIT) + top - j]);
         }
         sum += c[j];
     }
@@ -565,6 +575,7 @@ __device__ bool cross_bin(const V *hist, uint32_t copies, uint64_t most, uint64_
     if (threadIdx.x == 0) {
         out[0] = 0;
         out[1] = 0;
+        out[2] = 0;
     }
     __syncthreads();
 #pragma unroll
@@ -572,12 +583,14 @@ __device__ bool cross_bin(const V *hist, uint32_t copies, uint64_t most, uint64_
         if (above <= most && most < above + c[j]) {
             out[0] = top - j;
             out[1] = most - above;
+            out[2] = c[j];
         }
         above += c[j];
     }
     __syncthreads();
     *bin = (uint32_t)out[0];
     *left = out[1];
+    *in_bin = out[2];
     return most < total;
 }
 
@@ -604,27 +617,35 @@ __device__ bool last_of_row(const LongWork &w, int64_t row, uint32_t at, int pas
     return last;
 }
 
-// The digit that a pass of top-k has counted, by the row's last workgroup.
+// A digit is read off its counts by every workgroup of the next pass on its
+// own (all at once: 2 M candidates, 7 to 8 us a pass; by the last workgroup of
+// its pass 11 us), the last digit by the last workgroup of its pass, since the
+// passes after it are of many small workgroups. keep: whether to keep it.
+
+// top-k's offset with the digit that pass DIGIT has counted.
+// (before: with the digits before; what another workgroup of this launch
+// keeps is not to be read.)
 template <int DIGIT>
-__device__ void end_count(const DrawArgs &a, const LongWork &w, int64_t row, const Ends &e, uint64_t *lds) {
+__device__ Digit end_count(const DrawArgs &a, const LongWork &w, int64_t row, const Ends &e, const Digit &before,
+                           bool keep, uint64_t *lds) {
     RowState &s = w.state[row];
-    const uint32_t z0 = DIGIT ? s.count_z[DIGIT ? DIGIT - 1 : 0] : 0u;
-    const uint32_t n0 = DIGIT ? s.count_need[DIGIT ? DIGIT - 1 : 0] : a.top_k;
-    uint64_t left;
+    const uint32_t z0 = DIGIT ? before.z : 0u, n0 = DIGIT ? (uint32_t)before.left : a.top_k;
+    uint64_t left, in_bin;
     uint32_t b;
-    const bool found = cross_bin<kThreads, DIGIT>(w.counts + (size_t)row * w.copies * kBinsAll, w.copies,
-                                                  (uint64_t)n0 - 1, ~(uint64_t)0, ~0u, 0, &b, &left, lds);
-    if (threadIdx.x != 0) return;
+    const bool found = cross_bin<kThreads, DIGIT>(w.counts + (size_t)row * kBinsAll, w.copies,
+                                                  (uint64_t)n0 - 1, ~(uint64_t)0, ~0u, 0, &b, &left, &in_bin, lds);
     // (need 0: the row has fewer than top_k candidates, and keeps them all)
     const uint32_t z = z0 | b << digit_shift(DIGIT), need = n0 && found ? (uint32_t)left + 1u : 0u;
-    s.count_z[DIGIT] = z;
-    s.count_need[DIGIT] = need;
+    const Digit d{need, z, 0};
+    if (!keep || threadIdx.x != 0) return d;
+    s.count[DIGIT] = d;
     if (DIGIT == kDigits - 1) {
         const bool all = need == 0 || e.top == 0;
         s.in_key = s.kept_key = all ? 0u : offset_key(z, e);
         s.in_ties = s.kept_ties = all ? 0xFFFFFFFFu : need;
-        s.ranked = !all;
+        s.ranked = !all && need < in_bin;
     }
+    return d;
 }
 
 // What top-k left.
@@ -635,23 +656,23 @@ __device__ __forceinline__ Kept count_kept(const DrawArgs &a, const LongWork &w,
 
 // The same of top-p's digits, by masses.
 template <int DIGIT>
-__device__ void end_mass(const DrawArgs &a, const LongWork &w, int64_t row, const Kept &in, const Ends &e,
-                         const Scale &scale, uint64_t *lds) {
+__device__ Digit end_mass(const DrawArgs &a, const LongWork &w, int64_t row, const Kept &in, const Ends &e,
+                          const Scale &scale, const Digit &before, bool keep, uint64_t *lds) {
     RowState &s = w.state[row];
-    const uint32_t z0 = DIGIT ? s.mass_z[DIGIT ? DIGIT - 1 : 0] : 0u;
+    const uint32_t z0 = DIGIT ? before.z : 0u;
     // top-k's equals, which the histogram leaves out
     const uint64_t extra = in.key ? mass_of(a, in.key, scale) * in.ties : 0;
     const uint32_t zi = in.key ? offset_of(in.key, e) : 0u;
     const uint32_t extra_bin = in.key && same_before(zi, z0, DIGIT) ? digit_of(zi, DIGIT) : ~0u;
     uint32_t b;
-    uint64_t left;
-    cross_bin<kThreads, DIGIT>(w.masses + (size_t)row * w.copies * kBinsAll, w.copies,
-                               DIGIT ? s.mass_left[DIGIT ? DIGIT - 1 : 0] : 0, DIGIT ? ~(uint64_t)0 : a.share,
-                               extra_bin, extra, &b, &left, lds);
-    if (threadIdx.x != 0) return;
+    uint64_t left, in_bin;
+    cross_bin<kThreads, DIGIT>(w.masses + (size_t)row * kBinsAll, w.copies,
+                               DIGIT ? before.left : 0, DIGIT ? ~(uint64_t)0 : a.share,
+                               extra_bin, extra, &b, &left, &in_bin, lds);
     const uint32_t z = z0 | b << digit_shift(DIGIT);
-    s.mass_z[DIGIT] = z;
-    s.mass_left[DIGIT] = left;
+    const Digit d{left, z, 0};
+    if (!keep || threadIdx.x != 0) return d;
+    s.mass[DIGIT] = d;
     if (DIGIT == kDigits - 1) {
         const uint32_t key = e.top ? offset_key(z, e) : 0u;
         const uint64_t q = mass_of(a, key, scale);
@@ -659,8 +680,11 @@ __device__ void end_mass(const DrawArgs &a, const LongWork &w, int64_t row, cons
         if (key == in.key && ties > in.ties) ties = in.ties;
         s.kept_key = key;
         s.kept_ties = ties < 0xFFFFFFFFu ? (uint32_t)ties : 0xFFFFFFFFu;
-        s.ranked = 1;
+        // the bin's mass is that of all equals that could stay; of those that
+        // top-k cut, some are not in it
+        s.ranked = q && (ties * q < in_bin || (key == in.key && in.ties != 0xFFFFFFFFu));
     }
+    return d;
 }
 
 struct Place {
@@ -681,7 +705,7 @@ __device__ __forceinline__ Place place_of(const DrawArgs &a, uint32_t pieces, in
 __global__ __launch_bounds__(kThreads) void k_draw_ends(DrawArgs a, LongWork w, uint64_t block0) {
     __shared__ uint64_t lds[kThreads / kWave];
     const Place p = place_of(a, w.stretches, w.stretch, block0 + blockIdx.x);
-    const uint32_t bins = w.copies * kBinsAll;
+    const uint32_t bins = kBinsAll;
     if (p.at == 0 && threadIdx.x < kPasses * kTickets) w.tickets[(size_t)p.row * kPasses * kTickets + threadIdx.x] = 0;
     for (uint32_t b = p.at * kThreads + threadIdx.x; b < bins; b += w.stretches * kThreads) {
         if (a.top_k < (uint32_t)a.n) w.counts[(size_t)p.row * bins + b] = 0;
@@ -719,11 +743,14 @@ __device__ __forceinline__ Ends pass_ends(const LongWork &w, const Place &p, boo
 template <int DIGIT>
 __global__ __launch_bounds__(kThreads) void k_draw_count(DrawArgs a, LongWork w, uint64_t block0) {
     __shared__ uint32_t s_hist[bins_of(DIGIT)];
-    __shared__ uint64_t lds[kThreads / kWave + 2];
+    __shared__ uint64_t lds[kThreads / kWave + 3];
     const Place p = place_of(a, w.stretches, w.stretch, block0 + blockIdx.x);
     for (uint32_t b = threadIdx.x; b < bins_of(DIGIT); b += kThreads) s_hist[b] = 0;
     const Ends e = pass_ends(w, p, DIGIT == 0, lds);
-    const uint32_t z0 = DIGIT ? w.state[p.row].count_z[DIGIT ? DIGIT - 1 : 0] : 0u;
+    Digit before{};
+    if (DIGIT > 1) before = w.state[p.row].count[DIGIT > 1 ? DIGIT - 2 : 0];
+    if (DIGIT > 0) before = end_count<DIGIT ? DIGIT - 1 : 0>(a, w, p.row, e, before, p.at == 0, lds);
+    const uint32_t z0 = before.z;
     __syncthreads();
     for (int64_t i = p.i0 + threadIdx.x * 4; i < p.i1; i += kTile) {
         uint32_t k[4];
@@ -735,23 +762,27 @@ __global__ __launch_bounds__(kThreads) void k_draw_count(DrawArgs a, LongWork w,
         }
     }
     __syncthreads();
-    uint32_t *out = w.counts + ((size_t)p.row * w.copies + p.at % w.copies) * kBinsAll + bins_before(DIGIT);
+    uint32_t *out = w.counts + (size_t)p.row * kBinsAll + bins_before(DIGIT) + (DIGIT ? 0u : p.at % w.copies * kBins0);
     for (uint32_t b = threadIdx.x; b < bins_of(DIGIT); b += kThreads)
         if (s_hist[b]) atomicAdd(&out[b], s_hist[b]);
-    if (last_of_row(w, p.row, p.at, DIGIT, lds)) end_count<DIGIT>(a, w, p.row, e, lds);
+    if (DIGIT == kDigits - 1 && last_of_row(w, p.row, p.at, 0, lds))
+        end_count<DIGIT>(a, w, p.row, e, before, true, lds);
 }
 
 // Masses of a digit of the offsets that have top-p's earlier digits.
 template <int DIGIT>
 __global__ __launch_bounds__(kThreads) void k_draw_mass(DrawArgs a, LongWork w, uint64_t block0) {
     __shared__ unsigned long long s_hist[bins_of(DIGIT)];
-    __shared__ uint64_t lds[kThreads / kWave + 2];
+    __shared__ uint64_t lds[kThreads / kWave + 3];
     const Place p = place_of(a, w.stretches, w.stretch, block0 + blockIdx.x);
     for (uint32_t b = threadIdx.x; b < bins_of(DIGIT); b += kThreads) s_hist[b] = 0;
     const Ends e = pass_ends(w, p, DIGIT == 0 && a.top_k >= (uint32_t)a.n, lds);
     const Scale scale = scale_of(a, e.top);
     const Kept in = count_kept(a, w, p.row);
-    const uint32_t z0 = DIGIT ? w.state[p.row].mass_z[DIGIT ? DIGIT - 1 : 0] : 0u;
+    Digit before{};
+    if (DIGIT > 1) before = w.state[p.row].mass[DIGIT > 1 ? DIGIT - 2 : 0];
+    if (DIGIT > 0) before = end_mass<DIGIT ? DIGIT - 1 : 0>(a, w, p.row, in, e, scale, before, p.at == 0, lds);
+    const uint32_t z0 = before.z;
     __syncthreads();
     for (int64_t i = p.i0 + threadIdx.x * 4; i < p.i1; i += kTile) {
         uint32_t k[4];
@@ -767,10 +798,11 @@ __global__ __launch_bounds__(kThreads) void k_draw_mass(DrawArgs a, LongWork w, 
     }
     __syncthreads();
     unsigned long long *out = (unsigned long long *)(
-        w.masses + ((size_t)p.row * w.copies + p.at % w.copies) * kBinsAll + bins_before(DIGIT));
+        w.masses + (size_t)p.row * kBinsAll + bins_before(DIGIT) + (DIGIT ? 0u : p.at % w.copies * kBins0));
     for (uint32_t b = threadIdx.x; b < bins_of(DIGIT); b += kThreads)
         if (s_hist[b]) atomicAdd(&out[b], s_hist[b]);
-    if (last_of_row(w, p.row, p.at, kDigits + DIGIT, lds)) end_mass<DIGIT>(a, w, p.row, in, e, scale, lds);
+    if (DIGIT == kDigits - 1 && last_of_row(w, p.row, p.at, 1, lds))
+        end_mass<DIGIT>(a, w, p.row, in, e, scale, before, true, lds);
 }
 
 // The row's largest key and what the filters keep of it.
@@ -793,12 +825,18 @@ __device__ __forceinline__ uint32_t ties_of(const Kept &kept, const uint32_t k[4
     return n;
 }
 
+// Whether some of the equals of the last key go, so that their order counts.
+__device__ __forceinline__ bool row_ranked(const DrawArgs &a, const LongWork &w, int64_t row) {
+    return a.form == kBest || ((a.top_p || a.top_k < (uint32_t)a.n) && w.state[row].ranked);
+}
+
 // Equals of the last key, per part.
 __global__ __launch_bounds__(kBlock) void k_draw_ties(DrawArgs a, LongWork w, uint64_t block0) {
     __shared__ uint64_t lds[kWavesPerBlock + 2];
     const Place p = place_of(a, w.parts, w.part, block0 + blockIdx.x);
     Kept kept;
     row_kept(a, w, p.row, &kept, lds);
+    if (!row_ranked(a, w, p.row)) return;
     uint32_t ties = 0;
     for (int64_t i = p.i0 + threadIdx.x * 4; i < p.i1; i += kPartTile) {
         uint32_t k[4];
@@ -826,7 +864,8 @@ __global__ __launch_bounds__(kBlock) void k_draw_run(DrawArgs a, LongWork w, uin
     Kept kept;
     const Scale scale = scale_of(a, row_kept(a, w, p.row, &kept, lds));
     uint32_t place = 0;  // equals before
-    if (CUT) {
+    const bool ranked = CUT && row_ranked(a, w, p.row);
+    if (ranked) {
         for (uint32_t b = threadIdx.x; b < p.at; b += kBlock) place += w.ties[p.row * w.parts + b];
         place = group_sum<kBlock>(place, lds);
     }
@@ -836,7 +875,7 @@ __global__ __launch_bounds__(kBlock) void k_draw_run(DrawArgs a, LongWork w, uin
         const int64_t j = t0 + threadIdx.x * 4;
         uint32_t k[4], before = 0, all;
         load_keys(a, p.row, j, p.i1, k);
-        if (CUT) {
+        if (ranked) {
             before = place + group_scan<kBlock>(ties_of(kept, k), lds, &all);
             place += all;
         }
@@ -844,16 +883,40 @@ __global__ __launch_bounds__(kBlock) void k_draw_run(DrawArgs a, LongWork w, uin
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             bool stays = k[t] > kept.key;
-            if (CUT && k[t] == kept.key) stays = before++ < kept.ties;
+            if (CUT && k[t] == kept.key) stays = !ranked || before++ < kept.ties;
             if (stays) mine += mass_left(a, scale, k[t]);
         }
         const uint64_t upto = wave_scan(mine);  // in the slice
         if (j < end) w.quad_run[p.row * w.quads + j / 4] = upto;
         const uint64_t slice = run + group_scan<kBlock>(mine, lds, &total) + mine;
-        if (lane == kWave - 1) w.slice_run[block * w.slices + (size_t)((t0 - p.i0) / kSlice) + threadIdx.x / kWave] = slice;
+        const size_t at = block * w.slices + (size_t)((t0 - p.i0) / kSlice) + threadIdx.x / kWave;
+        if (lane % 8 == 7) w.oct_run[at * 8 + lane / 8] = upto;
+        if (lane == kWave - 1) w.slice_run[at] = slice;
         run += total;
     }
     if (threadIdx.x == 0) w.sums[p.row * w.parts + p.at] = run;
+}
+
+// The first of `count` <= 8 running sums that is more than r; r: what is left.
+// All eight are loaded at once (the array has room for them): a draw waits for
+// the memory once a level, not three times.
+__device__ __forceinline__ uint32_t pick8(const uint64_t *v, uint32_t count, uint64_t &r) {
+    typedef uint64_t u2 __attribute__((ext_vector_type(2), aligned(8)));
+    u2 x[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) x[t] = *(const u2 *)(v + 2 * t);
+    uint32_t at = 0;
+    uint64_t below = 0;
+#pragma unroll
+    for (uint32_t t = 0; t < 7; ++t) {
+        const uint64_t y = t & 1 ? x[t / 2].y : x[t / 2].x;
+        if (t + 1 < count && y <= r) {
+            at = t + 1;
+            below = y;
+        }
+    }
+    r -= below;
+    return at;
 }
 
 // The draws, a thread each: a workgroup takes kBlock of a row's. The part is
@@ -890,29 +953,38 @@ __global__ __launch_bounds__(kBlock) void k_draw_search(DrawArgs a, LongWork w, 
     for (uint32_t step = kMost / 2; step > 0; step /= 2)
         if (s_run[part + step - 1] <= r) part += step;
     if (part) r -= s_run[part - 1];
-    // the first entry of a running sum that is more than r; r: what is left
-    auto find = [&](const uint64_t *v, uint32_t count) {
-        uint32_t lo = 0, hi = count - 1;
-        uint64_t below = 0;
-        while (lo < hi) {
-            const uint32_t mid = (lo + hi) / 2;
-            const uint64_t x = v[mid];
-            if (x > r) {
-                hi = mid;
-            } else {
-                lo = mid + 1;
-                below = x;
-            }
-        }
-        r -= below;
-        return lo;
-    };
     const int64_t rest = a.n - (int64_t)part * w.part;
-    const uint32_t slice = find(w.slice_run + ((size_t)row * w.parts + part) * w.slices,
-                                (uint32_t)(rest < w.part ? (rest + kSlice - 1) / kSlice : w.slices));
+    uint32_t slice = 0, slices = (uint32_t)(rest < w.part ? (rest + kSlice - 1) / kSlice : w.slices);
+    const size_t slice0 = ((size_t)row * w.parts + part) * w.slices;
+    uint64_t below = 0;
+    while (slices > 8) {
+        const uint32_t half = slices / 2;
+        const uint64_t x = w.slice_run[slice0 + slice + half - 1];
+        if (x <= r) {
+            slice += half;
+            slices -= half;
+            below = x;
+        } else {
+            slices = half;
+        }
+    }
+    // (running sums of the part up to here: the first of the eight are compared
+    // with r itself)
+    const uint64_t in_part = r;
+    slice += pick8(w.slice_run + slice0 + slice, slices, r);
+    r = r == in_part ? in_part - below : r;
     const int64_t first = (int64_t)part * w.part + (int64_t)slice * kSlice;
+    const uint32_t count = first + kSlice < a.n ? kSlice / 4 : (uint32_t)((a.n - first + 3) / 4);
+    const uint64_t in_slice = r;
+    const uint32_t oct = pick8(w.oct_run + (slice0 + slice) * 8, (count + 7) / 8, r);
     const uint64_t *quads = w.quad_run + row * w.quads + first / 4;
-    const uint32_t quad = find(quads, first + kSlice < a.n ? kSlice / 4 : (uint32_t)((a.n - first + 3) / 4));
+    const uint64_t oct_from = in_slice - r;
+    r = in_slice;
+    uint32_t quad = pick8(quads + oct * 8, count - oct * 8 < 8 ? count - oct * 8 : 8, r);
+    uint64_t quad_from = in_slice - r;
+    if (quad == 0) quad_from = oct_from;
+    r = in_slice - quad_from;
+    quad += oct * 8;
     const int64_t j = first + quad * 4;
     uint32_t k[4];
     load_keys(a, row, j, row_length(a, row), k);
@@ -925,7 +997,7 @@ __global__ __launch_bounds__(kBlock) void k_draw_search(DrawArgs a, LongWork w, 
     if (CUT && kept.key) equal = mass_left(a, scale, kept.key);
     // how many of the equals stay: what is in the quad's mass
     uint64_t staying = 0;
-    if (equal) staying = (quads[quad] - (quad ? quads[quad - 1] : 0) - larger) / equal;
+    if (equal) staying = (quads[quad] - quad_from - larger) / equal;
     uint32_t id = 0;
     uint64_t mass = 0, upto = 0;
     bool found = false;
