@@ -14,6 +14,8 @@
 // masses stay in registers, the running mass goes to LDS, where the draws
 // search it. Longer rows are cut into stretches over many workgroups, with a
 // launch for each pass, and the running mass in the workspace.
+#include <type_traits>
+
 #include "budget.h"
 
 namespace gs {
@@ -36,51 +38,93 @@ struct DrawArgs {
     uint64_t share;   // floor(top_p 2^53)
     uint32_t top_k;   // 2^32 - 1: off
     uint32_t top_p;   // whether top_p is on
-    uint32_t logits, bf16, form;
+    uint32_t bf16, form;
+    uint32_t flip;    // logits: all ones, weights: 0
+    float floor;      // scores are drawn above it: -infinity, 0
     int32_t bits;     // k
 };
 
-// A score's place in the order as an unsigned number; 0: never drawn.
+// A score's place in the order as an unsigned number; 0: never drawn. (Without
+// a branch: floor and flip stand for the form of the scores.)
 __device__ __forceinline__ uint32_t key_of(const DrawArgs &a, uint32_t b) {
     const float x = __uint_as_float(b);
-    if (!a.logits) return x > 0.0f ? b : 0u;
-    if (!(x > -__builtin_inff())) return 0u;
     const uint32_t c = __float_as_uint(x + 0.0f);  // -0 as 0
-    return c ^ ((uint32_t)((int32_t)c >> 31) | 0x80000000u);
+    const uint32_t k = c ^ (((uint32_t)((int32_t)c >> 31) | 0x80000000u) & a.flip);
+    return x > a.floor ? k : 0u;
 }
 __device__ __forceinline__ uint32_t score_key(const DrawArgs &a, int64_t at) {
     return key_of(a, a.bf16 ? (uint32_t)((const uint16_t *)a.scores)[at] << 16 : ((const uint32_t *)a.scores)[at]);
 }
 __device__ __forceinline__ double key_score(const DrawArgs &a, uint32_t key) {
-    const uint32_t b = !a.logits ? key : (key & 0x80000000u) ? key ^ 0x80000000u : ~key;
-    return (double)__uint_as_float(b);
+    return (double)__uint_as_float(key ^ (((uint32_t)((int32_t)~key >> 31) | 0x80000000u) & a.flip));
 }
 
-// Keys of candidates j .. j + 3 of a row, 0 from len on.
-__device__ __forceinline__ void load_keys(const DrawArgs &a, int64_t row, int64_t j, int64_t len, uint32_t k[4]) {
+// Keys of U quads of a row, `apart` candidates from each other, the first at j:
+// 0 from `end` on (a multiple of 4, or the row's length). No load depends on
+// another's branch: a quad that passes the row's end is read from its last four
+// candidates and moved down, one past `end` is read from there too, for
+// nothing.
+template <int U>
+__device__ __forceinline__ void load_quads(const DrawArgs &a, int64_t row, uint32_t j, uint32_t apart, uint32_t end,
+                                           uint32_t len, uint32_t k[U][4]) {
     typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(4)));
     typedef uint32_t u2 __attribute__((ext_vector_type(2), aligned(2)));
-    const int64_t at = row * a.stride + j;
-    if (j + 4 <= len) {
-        if (a.bf16) {
-            const u2 v = *(const u2 *)((const uint16_t *)a.scores + at);
-            k[0] = v.x << 16;
-            k[1] = v.x & 0xFFFF0000u;
-            k[2] = v.y << 16;
-            k[3] = v.y & 0xFFFF0000u;
-        } else {
-            const u4 v = *(const u4 *)((const uint32_t *)a.scores + at);
-            k[0] = v.x;
-            k[1] = v.y;
-            k[2] = v.z;
-            k[3] = v.w;
-        }
+    const int64_t base = row * a.stride;
+    if (len < 4) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) k[t] = key_of(a, k[t]);
-    } else {
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) k[t] = j + t < len ? score_key(a, at + t) : 0u;
+            for (uint32_t t = 0; t < 4; ++t)
+                k[u][t] = j + u * apart + t < end ? score_key(a, base + j + u * apart + t) : 0u;
+        return;
     }
+    uint32_t at[U], down[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint32_t q = j + u * apart, last = len - 4;
+        at[u] = q < last ? q : last;
+        down[u] = q < end ? q - at[u] : 4u;
+    }
+    if (a.bf16) {
+        u2 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = *(const u2 *)((const uint16_t *)a.scores + base + at[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            k[u][0] = v[u].x << 16;
+            k[u][1] = v[u].x & 0xFFFF0000u;
+            k[u][2] = v[u].y << 16;
+            k[u][3] = v[u].y & 0xFFFF0000u;
+        }
+    } else {
+        u4 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = *(const u4 *)((const uint32_t *)a.scores + base + at[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            k[u][0] = v[u].x;
+            k[u][1] = v[u].y;
+            k[u][2] = v[u].z;
+            k[u][3] = v[u].w;
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) k[u][t] = key_of(a, k[u][t]);
+        const uint32_t d = down[u], k1 = k[u][1], k2 = k[u][2], k3 = k[u][3];
+        k[u][0] = d == 0 ? k[u][0] : d == 1 ? k1 : d == 2 ? k2 : d == 3 ? k3 : 0u;
+        k[u][1] = d == 0 ? k1 : d == 1 ? k2 : d == 2 ? k3 : 0u;
+        k[u][2] = d == 0 ? k2 : d == 1 ? k3 : 0u;
+        k[u][3] = d == 0 ? k3 : 0u;
+    }
+}
+__device__ __forceinline__ void load_keys(const DrawArgs &a, int64_t row, uint32_t j, uint32_t end, uint32_t len,
+                                          uint32_t k[4]) {
+    uint32_t q[1][4];
+    load_quads<1>(a, row, j, 0, end, len, q);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) k[t] = q[0][t];
 }
 
 // log2 of a positive float, in float64: with x = 2^e m, m in [sqrt(1/2),
@@ -132,20 +176,40 @@ __device__ __forceinline__ Scale scale_of(const DrawArgs &a, uint32_t top) {
     return s;
 }
 
-// q of a candidate. Adding 2^52 to a number from 0 to 2^52 rounds it to a whole
-// one, which the sum's bits then count.
+// q of N candidates, side by side: the chains of float64 operations are long.
+// Adding 2^52 to a number from 0 to 2^52 rounds it to a whole one, which the
+// sum's bits then count.
+template <int N>
+__device__ __forceinline__ void masses_of(const DrawArgs &a, const uint32_t key[N], const Scale &s, uint64_t q[N]) {
+    double v[N];
+#pragma unroll
+    for (int t = 0; t < N; ++t) v[t] = 0.0;
+    if (!s.best) {
+        double x[N];
+#pragma unroll
+        for (int t = 0; t < N; ++t) x[t] = key_score(a, key[t] ? key[t] : s.top);
+        if (a.form == kRatio) {
+#pragma unroll
+            for (int t = 0; t < N; ++t) v[t] = x[t] * s.at;
+        } else {
+            if (a.form == kPower) {
+#pragma unroll
+                for (int t = 0; t < N; ++t) x[t] = log2_of(x[t]);
+            }
+#pragma unroll
+            for (int t = 0; t < N; ++t) v[t] = exp2_of((x[t] - s.at) * a.rate, a.bits);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+        const uint64_t r = __builtin_bit_cast(uint64_t, v[t] + 0x1p52) - __builtin_bit_cast(uint64_t, 0x1p52);
+        q[t] = key[t] == 0 ? 0 : key[t] == s.top ? (uint64_t)1 << a.bits : r;
+    }
+}
 __device__ __forceinline__ uint64_t mass_of(const DrawArgs &a, uint32_t key, const Scale &s) {
-    if (key == s.top) return key ? (uint64_t)1 << a.bits : 0;
-    if (key == 0 || s.best) return 0;
-    const double x = key_score(a, key);
-    double v;
-    if (a.form == kRatio)
-        v = x * s.at;
-    else if (a.form == kPower)
-        v = exp2_of((log2_of(x) - s.at) * a.rate, a.bits);
-    else
-        v = exp2_of((x - s.at) * a.rate, a.bits);
-    return __builtin_bit_cast(uint64_t, v + 0x1p52) - __builtin_bit_cast(uint64_t, 0x1p52);
+    uint64_t q;
+    masses_of<1>(a, &key, s, &q);
+    return q;
 }
 
 // floor(m total / 2^53), m <= 2^53, total < 2^63
@@ -173,10 +237,10 @@ __device__ __forceinline__ uint32_t live(const uint32_t key[ITEMS]) {
     return n;
 }
 
-__device__ __forceinline__ int64_t row_length(const DrawArgs &a, int64_t row) {
-    if (!a.lengths) return a.n;
-    const int64_t l = a.lengths[row];
-    return l < 0 ? 0 : l > a.n ? a.n : l;
+__device__ __forceinline__ uint32_t row_length(const DrawArgs &a, int64_t row) {
+    if (!a.lengths) return (uint32_t)a.n;
+    const int32_t l = a.lengths[row];
+    return l < 0 ? 0u : l > a.n ? (uint32_t)a.n : (uint32_t)l;
 }
 
 __device__ __forceinline__ void write_draw(const DrawArgs &a, int64_t at, int64_t id, uint64_t q, uint64_t total) {
@@ -309,12 +373,12 @@ __global__ __launch_bounds__(NT) void k_draw_rows(DrawArgs a) {
     __shared__ uint64_t lds[NT / kWave + 2];
     uint64_t *s_out = lds + NT / kWave;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const int64_t len = row_length(a, row);
+        const uint32_t len = row_length(a, row);
         uint32_t key[ITEMS], top = 0, over = 0;  // over: ~key, for the least
         uint64_t q[ITEMS];
-        const int64_t j0 = (int64_t)threadIdx.x * ITEMS;
+        const uint32_t j0 = threadIdx.x * ITEMS;
 #pragma unroll
-        for (int t = 0; t < ITEMS; t += 4) load_keys(a, row, j0 + t, len, key + t);
+        for (int t = 0; t < ITEMS; t += 4) load_keys(a, row, j0 + t, len, len, key + t);
 #pragma unroll
         for (int t = 0; t < ITEMS; ++t) {
             top = umax_(top, key[t]);
@@ -323,7 +387,7 @@ __global__ __launch_bounds__(NT) void k_draw_rows(DrawArgs a) {
         top = group_max<NT>(top, lds);
         const Scale scale = scale_of(a, top);
 #pragma unroll
-        for (int t = 0; t < ITEMS; ++t) q[t] = mass_of(a, key[t], scale);
+        for (int t = 0; t < ITEMS; t += 4) masses_of<4>(a, key + t, scale, q + t);
         Kept kept{0, 0xFFFFFFFFu};
         if (a.form == kBest) {
             kept = Kept{top, 1};
@@ -431,8 +495,8 @@ __global__ __launch_bounds__(NT) void k_draw_rows(DrawArgs a) {
 constexpr uint32_t kThreads = 1024;
 constexpr uint32_t kParts = 4;
 constexpr uint32_t kSlice = 4 * kWave;
-constexpr int64_t kTile = 4 * kThreads;
 constexpr int64_t kPartTile = 4 * kBlock;
+constexpr int64_t kGranule = kParts * kSlice;  // a stretch is of whole slices of parts
 constexpr uint32_t kStretches = 256;  // of all rows, about; of a row, at most
 // A pass ends with an atomic add for every bin that a workgroup met, 20 to
 // 25 of them in a nanosecond on the whole chip: the first digit, which every
@@ -487,7 +551,7 @@ struct LongWork {
 LongWork long_layout(void *base, int64_t rows, int64_t n) {
     LongWork w;
     const int64_t most = rows >= (int64_t)kStretches ? 1 : (int64_t)kStretches / rows;
-    w.stretch = ((n + most - 1) / most + kTile - 1) / kTile * kTile;
+    w.stretch = ((n + most - 1) / most + kGranule - 1) / kGranule * kGranule;
     w.stretches = (uint32_t)((n + w.stretch - 1) / w.stretch);
     w.part = w.stretch / kParts;
     w.parts = (uint32_t)((n + w.part - 1) / w.part);
@@ -687,17 +751,36 @@ __device__ Digit end_mass(const DrawArgs &a, const LongWork &w, int64_t row, con
     return d;
 }
 
+// Every candidate's key of [i0, i1) of a row, over a workgroup of NT threads,
+// two quads on their way at a time; N keys a visit.
+template <int NT, int N, typename F>
+__device__ __forceinline__ void each_key(const DrawArgs &a, int64_t row, uint32_t i0, uint32_t i1, uint32_t len,
+                                         F visit) {
+    constexpr int kAhead = 2;
+    for (uint32_t t0 = i0; t0 < i1; t0 += kAhead * 4 * NT) {
+        uint32_t k[kAhead][4];
+        load_quads<kAhead>(a, row, t0 + threadIdx.x * 4, 4 * NT, i1, len, k);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (t0 + u * 4 * NT >= i1) break;
+#pragma unroll
+            for (int t = 0; t < 4; t += N) visit(k[u] + t);
+        }
+    }
+}
+
 struct Place {
-    int64_t row, i0, i1;  // the stretch (or part) of the row, cut to its length
-    uint32_t at;          // its number in the row
+    int64_t row;
+    uint32_t i0, i1, len;  // the stretch (or part) of the row, cut to its length
+    uint32_t at;           // its number in the row
 };
 __device__ __forceinline__ Place place_of(const DrawArgs &a, uint32_t pieces, int64_t length, uint64_t block) {
     Place p;
     p.row = (int64_t)(block / pieces);
     p.at = (uint32_t)(block % pieces);
-    const int64_t len = row_length(a, p.row);
-    p.i0 = (int64_t)p.at * length;
-    p.i1 = p.i0 + length < len ? p.i0 + length : len;
+    p.len = row_length(a, p.row);
+    p.i0 = p.at * (uint32_t)length;
+    p.i1 = p.len <= p.i0 ? p.i0 : p.len - p.i0 < (uint32_t)length ? p.len : p.i0 + (uint32_t)length;
     return p;
 }
 
@@ -712,15 +795,10 @@ __global__ __launch_bounds__(kThreads) void k_draw_ends(DrawArgs a, LongWork w, 
         if (a.top_p) w.masses[(size_t)p.row * bins + b] = 0;
     }
     uint32_t top = 0, over = 0;
-    for (int64_t i = p.i0 + threadIdx.x * 4; i < p.i1; i += kTile) {
-        uint32_t k[4];
-        load_keys(a, p.row, i, p.i1, k);
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            top = umax_(top, k[t]);
-            over = umax_(over, k[t] ? ~k[t] : 0u);
-        }
-    }
+    each_key<kThreads, 1>(a, p.row, p.i0, p.i1, p.len, [&](const uint32_t *k) {
+        top = umax_(top, *k);
+        over = umax_(over, *k ? ~*k : 0u);
+    });
     top = group_max<kThreads>(top, lds);
     over = group_max<kThreads>(over, lds);
     if (threadIdx.x == 0) w.ends[p.row * w.stretches + p.at] = make_uint2(top, over);
@@ -752,21 +830,35 @@ __global__ __launch_bounds__(kThreads) void k_draw_count(DrawArgs a, LongWork w,
     if (DIGIT > 0) before = end_count<DIGIT ? DIGIT - 1 : 0>(a, w, p.row, e, before, p.at == 0, lds);
     const uint32_t z0 = before.z;
     __syncthreads();
-    for (int64_t i = p.i0 + threadIdx.x * 4; i < p.i1; i += kTile) {
-        uint32_t k[4];
-        load_keys(a, p.row, i, p.i1, k);
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const uint32_t z = offset_of(k[t], e);
-            if (k[t] && same_before(z, z0, DIGIT)) atomicAdd(&s_hist[digit_of(z, DIGIT)], 1u);
-        }
-    }
+    each_key<kThreads, 1>(a, p.row, p.i0, p.i1, p.len, [&](const uint32_t *k) {
+        const uint32_t z = offset_of(*k, e);
+        if (*k && same_before(z, z0, DIGIT)) atomicAdd(&s_hist[digit_of(z, DIGIT)], 1u);
+    });
     __syncthreads();
     uint32_t *out = w.counts + (size_t)p.row * kBinsAll + bins_before(DIGIT) + (DIGIT ? 0u : p.at % w.copies * kBins0);
     for (uint32_t b = threadIdx.x; b < bins_of(DIGIT); b += kThreads)
         if (s_hist[b]) atomicAdd(&out[b], s_hist[b]);
     if (DIGIT == kDigits - 1 && last_of_row(w, p.row, p.at, 0, lds))
         end_count<DIGIT>(a, w, p.row, e, before, true, lds);
+}
+
+// Adds the masses of four candidates above `in` to a digit's bins, those that
+// have the digits of z0 before it.
+template <int DIGIT>
+__device__ __forceinline__ void add_masses(const DrawArgs &a, const uint32_t k[4], uint32_t in, uint32_t z0,
+                                           const Ends &e, const Scale &scale, unsigned long long *hist) {
+    uint32_t z[4], some = 0;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        z[t] = offset_of(k[t], e);
+        some |= (k[t] > in && same_before(z[t], z0, DIGIT) ? 1u : 0u) << t;
+    }
+    if (some == 0) return;
+    uint64_t q[4];
+    masses_of<4>(a, k, scale, q);
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+        if (some >> t & 1u && q[t]) atomicAdd(&hist[digit_of(z[t], DIGIT)], (unsigned long long)q[t]);
 }
 
 // Masses of a digit of the offsets that have top-p's earlier digits.
@@ -784,18 +876,9 @@ __global__ __launch_bounds__(kThreads) void k_draw_mass(DrawArgs a, LongWork w, 
     if (DIGIT > 0) before = end_mass<DIGIT ? DIGIT - 1 : 0>(a, w, p.row, in, e, scale, before, p.at == 0, lds);
     const uint32_t z0 = before.z;
     __syncthreads();
-    for (int64_t i = p.i0 + threadIdx.x * 4; i < p.i1; i += kTile) {
-        uint32_t k[4];
-        load_keys(a, p.row, i, p.i1, k);
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const uint32_t z = offset_of(k[t], e);
-            if (k[t] > in.key && same_before(z, z0, DIGIT)) {
-                const uint64_t q = mass_of(a, k[t], scale);
-                if (q) atomicAdd(&s_hist[digit_of(z, DIGIT)], (unsigned long long)q);
-            }
-        }
-    }
+    each_key<kThreads, 4>(a, p.row, p.i0, p.i1, p.len, [&](const uint32_t *k) {
+        add_masses<DIGIT>(a, k, in.key, z0, e, scale, s_hist);
+    });
     __syncthreads();
     unsigned long long *out = (unsigned long long *)(
         w.masses + (size_t)p.row * kBinsAll + bins_before(DIGIT) + (DIGIT ? 0u : p.at % w.copies * kBins0));
@@ -838,19 +921,32 @@ __global__ __launch_bounds__(kBlock) void k_draw_ties(DrawArgs a, LongWork w, ui
     row_kept(a, w, p.row, &kept, lds);
     if (!row_ranked(a, w, p.row)) return;
     uint32_t ties = 0;
-    for (int64_t i = p.i0 + threadIdx.x * 4; i < p.i1; i += kPartTile) {
-        uint32_t k[4];
-        load_keys(a, p.row, i, p.i1, k);
-        ties += ties_of(kept, k);
-    }
+    each_key<kBlock, 4>(a, p.row, p.i0, p.i1, p.len, [&](const uint32_t *k) { ties += ties_of(kept, k); });
     ties = group_sum<kBlock>(ties, lds);
     if (threadIdx.x == 0) w.ties[p.row * w.parts + p.at] = ties;
 }
 
-// q of a candidate by itself: what the filters leave of it if it stays.
-__device__ __forceinline__ uint64_t mass_left(const DrawArgs &a, const Scale &scale, uint32_t key) {
-    const uint64_t q = mass_of(a, key, scale);
-    return (double)q < a.least ? 0 : q;
+// What of four candidates' masses the filters leave: `before` equals of the
+// last key come earlier, which counts if they are ranked.
+__device__ __forceinline__ uint64_t masses_left(const DrawArgs &a, const Scale &scale, const Kept &kept, bool ranked,
+                                                const uint32_t k[4], uint32_t before, uint64_t q[4]) {
+    uint32_t some = 0;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        some |= k[t] && k[t] >= kept.key ? 1u : 0u;
+        q[t] = 0;
+    }
+    if (some == 0) return 0;
+    masses_of<4>(a, k, scale, q);
+    uint64_t sum = 0;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        bool stays = k[t] > kept.key;
+        if (k[t] == kept.key) stays = !ranked || before++ < kept.ties;
+        if (!stays || (double)q[t] < a.least) q[t] = 0;
+        sum += q[t];
+    }
+    return sum;
 }
 
 // Running masses of the quads of a slice, the slices of a part, and the parts'
@@ -870,29 +966,34 @@ __global__ __launch_bounds__(kBlock) void k_draw_run(DrawArgs a, LongWork w, uin
         place = group_sum<kBlock>(place, lds);
     }
     uint64_t run = 0;
-    const int64_t end = p.i0 + w.part < a.n ? p.i0 + w.part : a.n;
-    for (int64_t t0 = p.i0; t0 < end; t0 += kPartTile) {
-        const int64_t j = t0 + threadIdx.x * 4;
-        uint32_t k[4], before = 0, all;
-        load_keys(a, p.row, j, p.i1, k);
-        if (ranked) {
-            before = place + group_scan<kBlock>(ties_of(kept, k), lds, &all);
-            place += all;
-        }
-        uint64_t mine = 0, total;
+    const uint32_t n = (uint32_t)a.n, end = n - p.i0 < (uint32_t)w.part ? n : p.i0 + (uint32_t)w.part;
+    constexpr int kAhead = 2;
+    for (uint32_t t0 = p.i0; t0 < end; t0 += kAhead * (uint32_t)kPartTile) {
+        uint32_t keys[kAhead][4];
+        load_quads<kAhead>(a, p.row, t0 + threadIdx.x * 4, (uint32_t)kPartTile, p.i1, p.len, keys);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            bool stays = k[t] > kept.key;
-            if (CUT && k[t] == kept.key) stays = !ranked || before++ < kept.ties;
-            if (stays) mine += mass_left(a, scale, k[t]);
+        for (int u = 0; u < kAhead; ++u) {
+            const uint32_t tile = t0 + u * (uint32_t)kPartTile, j = tile + threadIdx.x * 4;
+            if (tile >= end) break;
+            const uint32_t *k = keys[u];
+            uint32_t before = 0, all;
+            if (ranked) {
+                before = place + group_scan<kBlock>(ties_of(kept, k), lds, &all);
+                place += all;
+            }
+            uint64_t q[4], total;
+            const uint64_t mine = masses_left(a, scale, kept, ranked, k, before, q);
+            const uint64_t upto = wave_scan(mine);  // in the slice
+            if (j < end) w.quad_run[p.row * w.quads + j / 4] = upto;
+            const uint64_t slice = run + group_scan<kBlock>(mine, lds, &total) + mine;
+            const uint32_t c = (tile - p.i0) / kSlice + threadIdx.x / kWave;
+            if (c < w.slices) {  // (a tile may pass the part's end)
+                const size_t at = block * w.slices + c;
+                if (lane % 8 == 7) w.oct_run[at * 8 + lane / 8] = upto;
+                if (lane == kWave - 1) w.slice_run[at] = slice;
+            }
+            run += total;
         }
-        const uint64_t upto = wave_scan(mine);  // in the slice
-        if (j < end) w.quad_run[p.row * w.quads + j / 4] = upto;
-        const uint64_t slice = run + group_scan<kBlock>(mine, lds, &total) + mine;
-        const size_t at = block * w.slices + (size_t)((t0 - p.i0) / kSlice) + threadIdx.x / kWave;
-        if (lane % 8 == 7) w.oct_run[at * 8 + lane / 8] = upto;
-        if (lane == kWave - 1) w.slice_run[at] = slice;
-        run += total;
     }
     if (threadIdx.x == 0) w.sums[p.row * w.parts + p.at] = run;
 }
@@ -985,25 +1086,28 @@ __global__ __launch_bounds__(kBlock) void k_draw_search(DrawArgs a, LongWork w, 
     if (quad == 0) quad_from = oct_from;
     r = in_slice - quad_from;
     quad += oct * 8;
-    const int64_t j = first + quad * 4;
+    const uint32_t j = (uint32_t)first + quad * 4, len = row_length(a, row);
     uint32_t k[4];
-    load_keys(a, row, j, row_length(a, row), k);
+    load_keys(a, row, j, len, len, k);
     uint64_t q[4], larger = 0, equal = 0;
+    masses_of<4>(a, k, scale, q);
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-        q[t] = k[t] > kept.key || (CUT && k[t] == kept.key) ? mass_left(a, scale, k[t]) : 0;
-        if (k[t] > kept.key) larger += q[t];
+        if (k[t] < kept.key || (double)q[t] < a.least) q[t] = 0;
+        if (k[t] > kept.key)
+            larger += q[t];
+        else
+            equal = equal > q[t] ? equal : q[t];
     }
-    if (CUT && kept.key) equal = mass_left(a, scale, kept.key);
     // how many of the equals stay: what is in the quad's mass
-    uint64_t staying = 0;
-    if (equal) staying = (quads[quad] - quad_from - larger) / equal;
+    uint64_t staying = ~(uint64_t)0;
+    if (CUT && equal) staying = (quads[quad] - quad_from - larger) / equal;
     uint32_t id = 0;
     uint64_t mass = 0, upto = 0;
     bool found = false;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-        if (CUT && k[t] == kept.key && (staying == 0 || staying-- == 0)) q[t] = 0;
+        if (k[t] == kept.key && (staying == 0 || staying-- == 0)) q[t] = 0;
         upto += q[t];
         if (!found && upto > r) {
             found = true;
@@ -1037,9 +1141,11 @@ hipError_t launch_draw(int64_t rows, int64_t n, const void *scores, int64_t stri
     a.uniform = uniform;
     a.ids = ids;
     a.prob = prob;
-    a.logits = p.logits != 0;
-    a.form = p.temperature == 0.0 ? kBest : a.logits ? kExp : p.temperature == 1.0 ? kRatio : kPower;
-    a.rate = a.form == kBest ? 0.0 : (a.logits ? 1.4426950408889634 : 1.0) / p.temperature;
+    const bool logits = p.logits != 0;
+    a.flip = logits ? ~0u : 0u;
+    a.floor = logits ? -__builtin_inff() : 0.0f;
+    a.form = p.temperature == 0.0 ? kBest : logits ? kExp : p.temperature == 1.0 ? kRatio : kPower;
+    a.rate = a.form == kBest ? 0.0 : (logits ? 1.4426950408889634 : 1.0) / p.temperature;
     int up = 0;
     while (((int64_t)1 << up) < n) ++up;
     a.bits = 62 - up < 52 ? 62 - up : 52;

@@ -377,7 +377,8 @@ def test_draw_rows(kind, rows, n, draws):
 
 
 @pytest.mark.parametrize("kind", ["weights", "logits", "ties", "tied_logits", "odd", "odd_logits"])
-@pytest.mark.parametrize("rows,n,draws", [(1, 16385, 50), (3, 20011, 7)])
+@pytest.mark.parametrize("rows,n,draws", [(1, 16385, 50), (3, 20011, 7), (1, 65536, 256), (1, 16385, 257),
+                                          (2, 20011, 300), (1, 65537, 9)])
 def test_draw_long_rows(kind, rows, n, draws):
     logits = kind.endswith("logits")
     r = np.random.default_rng(n + draws)
@@ -395,23 +396,24 @@ def test_draw_very_long_rows(settings):
     check_draw(scores_for("ties", 1, (1 << 21) + 5, r), 100, False, settings)
 
 
-@pytest.mark.parametrize("n", [70, 600, 5000, 17000])
-def test_draw_types_strides_and_lengths(n):
+@pytest.mark.parametrize("n,draws", [(70, 6), (600, 6), (5000, 6), (17000, 6), (17000, 260)])
+def test_draw_types_strides_and_lengths(n, draws):
     r = np.random.default_rng(n)
     for k, settings in enumerate(FILTERS):
-        check_draw(scores_for("logits", 5, n, r), 6, True, settings, seed=k, bf16=True, pad=k % 3)
-        check_draw(scores_for("weights", 5, n, r), 6, False, settings, seed=k, pad=1,
+        check_draw(scores_for("logits", 5, n, r), draws, True, settings, seed=k, bf16=True, pad=k % 3)
+        check_draw(scores_for("weights", 5, n, r), draws, False, settings, seed=k, pad=1,
                    lengths=[0, 1, n, n // 2, n + 9])
-        check_draw(scores_for("tied_logits", 3, n, r), 6, True, settings, seed=k, pad=5, lengths=[-3, n - 1, 2])
-    check_draw(np.zeros((2, n), np.float32), 6, False, dict(top_p=0.5))  # nothing to draw
-    check_draw(np.full((2, n), -np.inf, np.float32), 6, True, dict(top_k=3))
-    check_draw(np.full((2, n), 7.0, np.float32), 6, True, dict(top_k=3, top_p=0.5))
+        check_draw(scores_for("tied_logits", 3, n, r), draws, True, settings, seed=k, pad=5, lengths=[-3, n - 1, 2])
+    check_draw(np.zeros((2, n), np.float32), draws, False, dict(top_p=0.5))  # nothing to draw
+    check_draw(np.full((2, n), -np.inf, np.float32), draws, True, dict(top_k=3))
+    check_draw(np.full((2, n), 7.0, np.float32), draws, True, dict(top_k=3, top_p=0.5))
 
 
 def test_draw_many_rows():
     r = np.random.default_rng(1)
     check_draw(scores_for("weights", 2000, 33, r), 3, False, dict(top_k=5, top_p=0.9))
     check_draw(scores_for("weights", 40, 16385, r), 2, False, dict(top_p=0.9))
+    check_draw(scores_for("weights", 300, 16400, r), 300, False, dict(top_k=500, top_p=0.9))
 
 
 def test_draw_empty_shapes():
