@@ -21,7 +21,7 @@ namespace {
 // lanes; one a wave where there are too few to fill the chip otherwise.
 constexpr uint32_t kPack = 4;
 constexpr int64_t kPackMinGauss = 65536;
-constexpr uint32_t kXcdWaves = 4;
+constexpr uint32_t kXcdWaves = 64;
 // The rows of a Gaussian's queries: voxels of a grid; the plan's cells; voxels
 // of a jittered grid, every voxel with its query.
 enum { kWalkGrid = 0, kWalkPlan = 1, kWalkVoxels = 2 };
@@ -29,6 +29,9 @@ enum { kWalkGrid = 0, kWalkPlan = 1, kWalkVoxels = 2 };
 constexpr int64_t kVoxelsLeast = 4096;
 // waves of one launch (a launch has fewer than 2^32 threads)
 constexpr uint64_t kWavesMost = (uint64_t)1 << 25;
+
+// The hardware's root, good to an ulp: what it bounds has more slack than that.
+__device__ __forceinline__ float sqrt_hw(float x) { return __builtin_amdgcn_sqrtf(x); }
 
 // f of a query: its gain over I, 0 where the field is undefined.
 __device__ __forceinline__ float query_factor(const float *influence, const float *gain, int64_t t) {
@@ -95,11 +98,11 @@ __device__ __forceinline__ bool within_exact(const SharesExact &x, uint32_t gid,
 // of d = p - mu are rounded once, u's sums at most three times, so |du| <=
 // 5 2^-24 |U| |d| summed by components, at most sqrt(3) kappa |u| 5 2^-24 with
 // kappa the largest scale over the smallest; twice |u| |du| and the three
-// roundings of |u|^2 stay below 2^-19 kappa Q'.
+// roundings of |u|^2 make (10 sqrt(3) kappa + 3) 2^-24 Q', below 2^-19 kappa Q'.
 __device__ __forceinline__ float cutoff_margin(const SharesExact &x, uint32_t gid, float T) {
     const float *s = x.scale + 3 * (size_t)gid;
     const float hi = fmaxf(fmaxf(s[0], s[1]), s[2]), lo = fminf(fminf(s[0], s[1]), s[2]);
-    return hi / lo * 0x1p-19f * T;
+    return hi * __builtin_amdgcn_rcpf(lo) * 0x1p-19f * T;
 }
 
 struct SharesArgs {
@@ -134,7 +137,7 @@ __device__ __forceinline__ VoxelReach voxel_reach(const Record &r, const QueryPa
     const float hy = 0.5f * q.vsz[1], hz = 0.5f * q.vsz[2];
     const float e1 = fabsf(r.f2.x) * hy + fabsf(r.f2.y) * hz, e2 = fabsf(r.f2.z) * hz;
     VoxelReach v;
-    v.reach = __builtin_sqrtf(fmaf_(e1, e1, e2 * e2)) * (1.0f + 0x1p-10f);
+    v.reach = sqrt_hw(fmaf_(e1, e1, e2 * e2)) * (1.0f + 0x1p-10f);
     v.shift = (fabsf(r.f1.y) * hy + fabsf(r.f1.z) * hz) / fabsf(r.f1.x);
     return v;
 }
@@ -143,9 +146,9 @@ __device__ __forceinline__ VoxelReach voxel_reach(const Record &r, const QueryPa
 __device__ __forceinline__ void voxel_rows(const Record &r, const QueryParams &q, const GridParams &g,
                                            const BwdGeom &bg, uint32_t &y0, uint32_t &ny, uint32_t &z0,
                                            uint32_t &nz) {
-    const float rt = __builtin_sqrtf(bg.T2);
+    const float rt = sqrt_hw(bg.T2);
     const float t = r.f2.y / r.f2.z;
-    const float hy = rt * __builtin_sqrtf(fmaf_(t, t, 1.0f)) / r.f2.x, hz = rt / r.f2.z;
+    const float hy = rt * sqrt_hw(fmaf_(t, t, 1.0f)) / r.f2.x, hz = rt / r.f2.z;
     auto cut = [](float mu, float h, float lo, float iv, float slack, int32_t dim, uint32_t &first, uint32_t &n) {
         const float a = fmaxf(floorf((mu - h - lo) * iv - slack), 0.0f);
         const float c = fminf(floorf((mu + h - lo) * iv + slack), (float)(dim - 1));
@@ -164,12 +167,12 @@ __device__ __forceinline__ uint32_t voxel_row(const Record &r, const VoxelReach 
     const float dy = g.lo[1] + ((float)vy + 0.5f) * q.vsz[1] - r.f0.y;
     const float dz = g.lo[2] + ((float)vz + 0.5f) * q.vsz[2] - r.f0.z;
     const float e1 = fmaf_(r.f2.x, dy, r.f2.y * dz), e2 = r.f2.z * dz;
-    const float e = fmaxf(__builtin_sqrtf(fmaf_(e1, e1, e2 * e2)) * (1.0f - 0x1p-10f) - v.reach, 0.0f);
+    const float e = fmaxf(sqrt_hw(fmaf_(e1, e1, e2 * e2)) * (1.0f - 0x1p-10f) - v.reach, 0.0f);
     const float left = bg.T2 - e * e;
     first = 0;
     if (!(left >= 0.0f)) return 0;
     const float iu = __builtin_amdgcn_rcpf(r.f1.x);
-    const float w = __builtin_sqrtf(left) * iu * (1.0f + 0x1p-10f) + v.shift;
+    const float w = sqrt_hw(left) * iu * (1.0f + 0x1p-10f) + v.shift;
     const float c = r.f0.x - fmaf_(r.f1.y, dy, r.f1.z * dz) * iu;
     const float m = (fabsf(r.f0.x) + fabsf(c) + w) * 0x1p-20f;
     const float a = fmaxf(floorf((c - w - m - g.lo[0]) * bg.ivsz[0] - bg.vslack[0]), 0.0f);
@@ -181,13 +184,19 @@ __device__ __forceinline__ uint32_t voxel_row(const Record &r, const VoxelReach 
 
 // A wave takes `pack` Gaussians (consecutive in gorder). Their rows are listed
 // one Gaussian after the other and set up 64 at a time, a lane a row; the rows
-// with queries go to LDS. Then each Gaussian's rows are walked with its record
-// in scalars: 2^k lanes a row, the rows next to each other, so that short
-// rows share a step and a load reads whole stretches of memory.
+// with queries go to LDS, in up to kPieces pieces of 2^k queries. Then each
+// Gaussian's are walked with its record in scalars: 2^k lanes a piece, the
+// pieces next to each other, so that short rows share a step and a load reads
+// whole stretches of memory, and kAhead steps at a time, all their loads under
+// way before the first is used.
+constexpr uint32_t kAhead = 2;
+constexpr uint32_t kPieces = 4;
+constexpr uint32_t kEntries = kPieces * kWave + kAhead * 16;  // the last steps read past their rows
+
 template <int WALK>
 __global__ __launch_bounds__(kWave) void k_shares(SharesArgs a) {
-    __shared__ uint2 s_row[kWave];   // first query, queries
-    __shared__ uint4 s_grid[kWave];  // grids: first x, y and z
+    __shared__ uint2 s_row[kEntries];   // first query, queries
+    __shared__ uint4 s_grid[WALK == kWalkGrid ? kEntries : 1];  // grids: first x, y and z
     const uint32_t lane = threadIdx.x;
     const uint64_t first = (a.wave0 + xcd_group<kXcdWaves>(blockIdx.x, gridDim.x)) * a.pack;
     if (first >= (uint64_t)a.n_gauss) return;
@@ -264,12 +273,18 @@ __global__ __launch_bounds__(kWave) void k_shares(SharesArgs a) {
             if (WALK == kWalkGrid || voxels)
                 start = (uint32_t)a.q.dims[0] * (vy + (uint32_t)a.q.dims[1] * vz) + vx;
         }
-        const uint64_t some = __ballot(len > 0);
+        // queries of a piece: a power of two, kPieces of them the longest row
+        const uint32_t longest = wave_max_uniform(len);
+        const bool whole = longest > kPieces * kWave;  // rows that stay in one piece
+        const uint32_t shift = longest > 128u ? 6u : longest > 64u ? 5u : longest > 32u ? 4u : longest > 16u ? 3u : 2u;
+        const uint32_t wide = 1u << shift, mine = lane & (wide - 1), own = lane >> shift;
+        const uint32_t pieces = whole ? (len > 0 ? 1u : 0u) : (len + wide - 1) >> shift;
+        const uint32_t upto = wave_incl_sum(pieces);  // pieces of the batch's rows up to this one's
         __builtin_amdgcn_wave_barrier();
-        if (len > 0) {
-            const uint32_t at = (uint32_t)__popcll(some & (((uint64_t)1 << lane) - 1));
-            s_row[at] = make_uint2(start, len);
-            if (WALK == kWalkGrid) s_grid[at] = make_uint4(vx, __float_as_uint(py), __float_as_uint(pz), 0);
+        for (uint32_t k = 0; k < pieces; ++k) {
+            const uint32_t at = upto - pieces + k, from = k << shift;
+            s_row[at] = make_uint2(start + from, whole ? len : len - from);
+            if (WALK == kWalkGrid) s_grid[at] = make_uint4(vx + from, __float_as_uint(py), __float_as_uint(pz), 0);
         }
         __builtin_amdgcn_wave_barrier();
         const uint32_t nrows = Rw - rb < (uint32_t)kWave ? Rw - rb : (uint32_t)kWave;
@@ -284,44 +299,88 @@ __global__ __launch_bounds__(kWave) void k_shares(SharesArgs a) {
                 c = load_record_uniform(a.rec, cgid);
                 margin = readfirst_f(cutoff_margin(a.exact, cgid, T));
             }
-            // its rows in this batch, and those of them with queries
+            // its rows in this batch, and their pieces
             const uint32_t la = gend - gR > rb ? gend - gR - rb : 0u;
             const uint32_t lb = gend - rb < nrows ? gend - rb : nrows;
-            const uint64_t below_a = ((uint64_t)1 << la) - 1;
-            const uint64_t below_b = lb < (uint32_t)kWave ? ((uint64_t)1 << lb) - 1 : ~(uint64_t)0;
-            const uint32_t ra = (uint32_t)__popcll(some & below_a), rz = (uint32_t)__popcll(some & below_b);
-            if (ra == rz) continue;
-            // lanes of a row: the power of two from its longest row on
-            const uint32_t longest = wave_max_uniform(lane >= la && lane < lb ? len : 0u);
-            const uint32_t shift = longest > 32u ? 6u : longest > 16u ? 5u : longest > 8u ? 4u : 3u;
-            const uint32_t wide = 1u << shift, mine = lane & (wide - 1), own = lane >> shift;
-            for (uint32_t r0 = ra; r0 < rz; r0 += (uint32_t)kWave >> shift) {
-                const uint32_t row = r0 + own;
-                uint2 w = make_uint2(0, 0);
-                uint4 v = make_uint4(0, 0, 0, 0);
-                if (row < rz) {
-                    w = s_row[row];
-                    if (WALK == kWalkGrid) v = s_grid[row];
-                }
-                for (uint32_t e = mine; e < w.y; e += wide) {
-                    float px, py, pz, f;
+            const uint32_t ra = la ? __builtin_amdgcn_readlane(upto, la - 1) : 0u;
+            const uint32_t rz = lb ? __builtin_amdgcn_readlane(upto, lb - 1) : 0u;
+            // kAhead queries of a lane: query k[u] if on[u], at voxel x[u] of
+            // its row in grids
+            auto add = [&](const uint32_t k[kAhead], const bool on[kAhead], const uint4 v[kAhead]) {
+                float px[kAhead], py[kAhead], pz[kAhead], f[kAhead];
+#pragma unroll
+                for (uint32_t u = 0; u < kAhead; ++u) {
+                    const uint32_t q = on[u] ? k[u] : 0u;
                     if (WALK == kWalkGrid) {
-                        px = a.g.lo[0] + ((float)(v.x + e) + 0.5f) * a.q.vsz[0];
-                        py = __uint_as_float(v.y);
-                        pz = __uint_as_float(v.z);
-                        f = a.f[(size_t)w.x + e];
+                        f[u] = a.f[q];
                     } else {
-                        const size_t k = (size_t)w.x + e;
-                        const float4 t = a.pts[WALK == kWalkVoxels && !voxels ? (size_t)a.order[k] : k];
-                        px = t.x;
-                        py = t.y;
-                        pz = t.z;
-                        f = t.w;
+                        const float4 t = a.pts[WALK == kWalkVoxels && !voxels ? a.order[q] : q];
+                        px[u] = t.x;
+                        py[u] = t.y;
+                        pz[u] = t.z;
+                        f[u] = t.w;
                     }
-                    const float Q = record_q(c, px, py, pz);
-                    bool in = Q <= T;
-                    if (__builtin_fabsf(Q - T) <= margin) in = within_exact(a.exact, cgid, px, py, pz);
-                    if (in) acc = fmaf_(exp2_hw(-Q), f, acc);
+                }
+                bool in[kAhead], near[kAhead], any = false;
+                float e[kAhead];
+#pragma unroll
+                for (uint32_t u = 0; u < kAhead; ++u) {
+                    if (WALK == kWalkGrid) {
+                        px[u] = a.g.lo[0] + ((float)v[u].x + 0.5f) * a.q.vsz[0];
+                        py[u] = __uint_as_float(v[u].y);
+                        pz[u] = __uint_as_float(v[u].z);
+                    }
+                    const float Q = record_q(c, px[u], py[u], pz[u]);
+                    in[u] = on[u] && Q <= T;
+                    near[u] = on[u] && __builtin_fabsf(Q - T) <= margin;
+                    any = any || near[u];
+                    e[u] = exp2_hw(-Q) * f[u];
+                }
+                if (any) {
+#pragma unroll
+                    for (uint32_t u = 0; u < kAhead; ++u)
+                        if (near[u]) in[u] = within_exact(a.exact, cgid, px[u], py[u], pz[u]);
+                }
+#pragma unroll
+                for (uint32_t u = 0; u < kAhead; ++u) acc += in[u] ? e[u] : 0.0f;
+            };
+            if (!whole) {
+                const uint32_t rows = (uint32_t)kWave >> shift;  // of a step
+                for (uint32_t r0 = ra; r0 < rz; r0 += kAhead * rows) {
+                    uint32_t k[kAhead];
+                    bool on[kAhead];
+                    uint4 v[kAhead] = {};
+#pragma unroll
+                    for (uint32_t u = 0; u < kAhead; ++u) {
+                        const uint32_t row = r0 + u * rows + own;
+                        const uint2 w = s_row[row];
+                        on[u] = row < rz && mine < w.y;
+                        k[u] = w.x + mine;
+                        if (WALK == kWalkGrid) {
+                            v[u] = s_grid[row];
+                            v[u].x += mine;
+                        }
+                    }
+                    add(k, on, v);
+                }
+            } else {
+                for (uint32_t row = ra; row < rz; ++row) {
+                    const uint2 w = s_row[row];
+                    uint4 g = make_uint4(0, 0, 0, 0);
+                    if (WALK == kWalkGrid) g = s_grid[row];
+                    for (uint32_t e0 = 0; e0 < w.y; e0 += kAhead * kWave) {
+                        uint32_t k[kAhead];
+                        bool on[kAhead];
+                        uint4 v[kAhead];
+#pragma unroll
+                        for (uint32_t u = 0; u < kAhead; ++u) {
+                            const uint32_t e = e0 + u * kWave + lane;
+                            on[u] = e < w.y;
+                            k[u] = w.x + e;
+                            v[u] = make_uint4(g.x + e, g.y, g.z, 0);
+                        }
+                        add(k, on, v);
+                    }
                 }
             }
         }

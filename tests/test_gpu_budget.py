@@ -102,6 +102,10 @@ KINDS = {
     "voxels": dict(kind="voxels", cells=(5, 4, 3), dims=(17, 19, 13), n=1500),
     "jitter": dict(kind="jitter", cells=(4, 5, 3), dims=(13, 11, 9)),
     "jitter_wide": dict(kind="jitter", cells=(4, 5, 3), dims=(13, 11, 9), spread=0.8),
+    # from 4096 queries on jittered grids are walked by voxels, unless a
+    # position leaves its voxel
+    "jitter_voxels": dict(kind="jitter", cells=(4, 5, 3), dims=(21, 18, 17), lo=(-1.0, 0.5, 3.0), hi=(1.0, 1.5, 3.7)),
+    "jitter_stray": dict(kind="jitter", cells=(4, 5, 3), dims=(21, 18, 17), spread=0.8),
     "jitter_ids": dict(kind="jitter_ids", cells=(3, 3, 3), dims=(30, 31, 29), n=1777),
     "points": dict(kind="points", cells=(6, 6, 6), n=2003),
     "points_box": dict(kind="points", cells=(6, 3, 9), n=1201, lo=(-1.5, 2.0, -0.25), hi=(1.5, 4.0, 0.25)),
