@@ -397,11 +397,9 @@ __global__ __launch_bounds__(kBlock) void k_split_clear(int64_t n, const int32_t
     if (i >= 0 && i < n) copies[i] = 1u;
 }
 
-__global__ __launch_bounds__(kBlock) void k_split_rows(gs_params set, int64_t n, const int32_t *__restrict__ ids,
-                                                       int64_t count, int32_t *__restrict__ source,
-                                                       float *__restrict__ score, uint32_t *__restrict__ copies) {
-    const int64_t j = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (j >= count) return;
+// Row n + j, with the logit and the score that the Gaussian had, and its count.
+__device__ __forceinline__ void split_row(const gs_params &set, int64_t n, const int32_t *ids, int64_t j,
+                                          int32_t *source, float *score, uint32_t *copies) {
     const int64_t i = ids[j], d = n + j;
     Row r;
     float share = 0.0f;
@@ -422,16 +420,12 @@ __global__ __launch_bounds__(kBlock) void k_split_rows(gs_params set, int64_t n,
     if (source) source[d] = i >= 0 ? (int32_t)(-1 - i) : -1;
 }
 
-__global__ __launch_bounds__(kBlock) void k_split_weights(gs_params set, int64_t n, const int32_t *__restrict__ ids,
-                                                          int64_t count, float *__restrict__ score,
-                                                          const uint32_t *__restrict__ copies) {
-    const int64_t j = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    if (j >= count) return;
-    const int64_t i = ids[j], d = n + j;
-    if (i < 0 || i >= n) return;
-    // w / c with w = 1 / (1 + e^-l): -ln(c (1 + e^-l) - 1); far down, where
-    // e^-l is all of that, l - ln c
-    const double c = (double)copies[i], l = (double)set.weight_logit[d];
+// The shared weight of c copies: w / c with w = 1 / (1 + e^-l) is the logit -ln(c
+// (1 + e^-l) - 1); far down, where e^-l is all of that, l - ln c.
+__device__ __forceinline__ void split_weight(const gs_params &set, int64_t n, int64_t i, int64_t j, float *score,
+                                             uint32_t copies) {
+    const int64_t d = n + j;
+    const double c = (double)copies, l = (double)set.weight_logit[d];
     const double shared = l < -30.0 ? l - log(c) : -log((c - 1.0) + c * exp(-l));
     set.weight_logit[d] = (float)shared;
     set.weight_logit[i] = (float)shared;
@@ -440,6 +434,45 @@ __global__ __launch_bounds__(kBlock) void k_split_weights(gs_params set, int64_t
         score[d] = s;
         score[i] = s;
     }
+}
+
+__global__ __launch_bounds__(kBlock) void k_split_rows(gs_params set, int64_t n, const int32_t *__restrict__ ids,
+                                                       int64_t count, int32_t *__restrict__ source, float *score,
+                                                       uint32_t *__restrict__ copies) {
+    const int64_t j = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (j < count) split_row(set, n, ids, j, source, score, copies);
+}
+
+__global__ __launch_bounds__(kBlock) void k_split_weights(gs_params set, int64_t n, const int32_t *__restrict__ ids,
+                                                          int64_t count, float *score,
+                                                          const uint32_t *__restrict__ copies) {
+    const int64_t j = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (j >= count) return;
+    const int64_t i = ids[j];
+    if (i >= 0 && i < n) split_weight(set, n, i, j, score, copies[i]);
+}
+
+// Few copies: the three steps in one workgroup (819 copies: 14.9 us by three
+// launches, the host's time). A thread takes the same copies in every step, so
+// that only the counts pass between threads, by atomics.
+constexpr int64_t kSplitSmall = 2048;
+__global__ __launch_bounds__(kSmallThreads) void k_split_small(gs_params set, int64_t n, const int32_t *ids,
+                                                               int count, int32_t *source, float *score,
+                                                               uint32_t *copies) {
+    auto own = [&](int j) { return ids[j] >= 0 && ids[j] < n; };
+    for (int j = threadIdx.x; j < count; j += kSmallThreads)
+        if (own(j)) __hip_atomic_store(&copies[ids[j]], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // (what each wave has sent is carried out)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    for (int j = threadIdx.x; j < count; j += kSmallThreads) split_row(set, n, ids, j, source, score, copies);
+    // (what each wave has sent is carried out)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    for (int j = threadIdx.x; j < count; j += kSmallThreads)
+        if (own(j))
+            split_weight(set, n, ids[j], j, score,
+                         __hip_atomic_load(&copies[ids[j]], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
 
 struct EvictWork {
@@ -505,6 +538,12 @@ hipError_t launch_split(const gs_params &set, int64_t n, const int32_t *ids, int
     if (count <= 0) return hipSuccess;
     const dim3 nb = blocks_of(count), tb(kBlock);
     prof_begin("split", s);
+    if (count <= kSplitSmall) {
+        hipLaunchKernelGGL(k_split_small, dim3(1), dim3(kSmallThreads), 0, s, set, n, ids, (int)count, source, score,
+                           copies);
+        prof_end("split", s);
+        return hipGetLastError();
+    }
     if (n > 0 && count >= n / kClearAll) {
         hipLaunchKernelGGL(k_split_fill, blocks_of((n + 3) / 4), tb, 0, s, n, copies);
     } else {

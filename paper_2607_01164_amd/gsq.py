@@ -271,6 +271,20 @@ def _dev_f32(t: torch.Tensor, name: str, shape_tail=()) -> torch.Tensor:
     return t
 
 
+def _sound(arrays, rows: int, tails) -> bool:
+    """Whether all arrays are contiguous float32 device tensors of `rows` rows
+    (one test for the calls that are well formed; the others find their
+    message array by array)."""
+    for t, tail in zip(arrays, tails):
+        if not (t.dtype is torch.float32 and t.is_cuda and t.is_contiguous() and
+                t.shape == ((rows,) if tail is None else (rows, tail))):
+            return False
+    return True
+
+
+_TAILS = (3, 3, 4, None, None)  # mean, scale or log-scale, rotation, value, weight
+
+
 @dataclass
 class Gaussians:
     """Post-activation parameters on the device: mean [n,3], scale [n,3],
@@ -287,6 +301,9 @@ class Gaussians:
 
     def c(self) -> GsGaussians:
         n = self.n
+        if _sound((self.mean, self.scale, self.rot, self.value, self.weight), n, _TAILS):
+            return GsGaussians(n, self.mean.data_ptr(), self.scale.data_ptr(), self.rot.data_ptr(),
+                               self.value.data_ptr(), self.weight.data_ptr())
         _dev_f32(self.mean, "mean", (3,))
         _dev_f32(self.scale, "scale", (3,))
         _dev_f32(self.rot, "rot", (4,))
@@ -697,6 +714,9 @@ class ParamSet:
 
     def c(self) -> GsParams:
         r = self.rows
+        if _sound((self.mean, self.log_scale, self.rot, self.value_logit, self.weight_logit), r, _TAILS):
+            return GsParams(self.mean.data_ptr(), self.log_scale.data_ptr(), self.rot.data_ptr(),
+                            self.value_logit.data_ptr(), self.weight_logit.data_ptr())
         for t, nm, tail in ((self.mean, "mean", (3,)), (self.log_scale, "log_scale", (3,)), (self.rot, "rot", (4,)),
                             (self.value_logit, "value_logit", ()), (self.weight_logit, "weight_logit", ())):
             _dev_f32(t, nm, tail)
@@ -1030,7 +1050,7 @@ def gs_shares(gauss: Gaussians, index: Index, query: Query, plan: Optional[torch
     are left out); gain (None: 1) weighs the queries."""
     g = gauss.c()
     q = query.c()
-    nq = query.size()
+    nq = load_library().gs_query_size(ctypes.byref(q))
     _row_of(influence, "influence", torch.float32, nq)
     _row_of(gain, "gain", torch.float32, nq)
     _row_of(score, "score", torch.float32, gauss.n)
