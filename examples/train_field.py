@@ -8,9 +8,13 @@ losses, the sampler's and the activations' backward, then the global gradient
 norm (which opens the step, or skips it when a gradient is not finite) and one
 AdamW launch over the five parameter arrays, with the paper's learning rates.
 Every --densify-every iterations the field is pruned and grown, and the
-moments follow their Gaussians through the densification's source map. Moments
-are kept in 8 bits or in 32. Prints the loss and, at the end, the PSNR of the
-reconstructed volume."""
+moments follow their Gaussians through the densification's source map. With
+--rebalance-every the number of Gaussians is held instead: every iteration adds
+the attention weight that each Gaussian gets to its score, and every so many
+iterations a tenth with the least goes, Gaussians drawn by their score are
+copied in its place, and the copies share their weight. Moments are kept in 8
+bits or in 32. Prints the loss and, at the end, the PSNR of the reconstructed
+volume."""
 import argparse
 import math
 import os
@@ -24,6 +28,7 @@ import paper_2607_01164_amd as gs  # noqa: E402
 TAU, SCALE_CAP = 0.01, 0.04
 PRUNE_WEIGHT, NEW_WEIGHT = 0.005, 0.01
 FN_EPS, FN_LAMBDA = 0.1, 1.0
+SCORE_DECAY, MOVED, APART = 0.9, 0.1, 0.5  # of a score an iteration; share moved; copies' distance in scales
 # arrays of the free parameters: width, learning rate
 ARRAYS = (("mean", 3, 1.6e-4), ("log_scale", 3, 1e-3), ("rot", 4, 1e-4), ("value_logit", 1, 2.5e-3),
           ("weight_logit", 1, 2.5e-2))
@@ -92,6 +97,7 @@ class Trainer:
         self.act_value, self.weight = torch.empty(rows, **f), torch.empty(rows, **f)
         self.all_grads = gs.Grads.empty(rows, device)
         self.source = torch.empty(rows, dtype=torch.int32, device=device)
+        self.scores = [torch.zeros(rows, **f) for _ in range(2)]
         p = self.sets[0]
         p.mean[:n].uniform_(0.0, 1.0, generator=self.gen)
         self.new_log_scale = math.log(0.7 / n ** (1.0 / 3.0))
@@ -127,9 +133,12 @@ class Trainer:
             self.index = gs.Index(self.grid, self.scale.shape[0], int(1.3 * self.index.n_pairs), self.device)
             gs.gs_build_index(self.gauss, self.grid, TAU, self.index)
 
-    def step(self):
-        """One iteration; nothing of it but the index's pair count is waited for."""
+    def step(self, attend=False):
+        """One iteration; nothing of it but the index's pair count is waited
+        for. attend: whether the scores take the batch's attention weight."""
         self.gradients()
+        if attend:
+            self.attend()
         self.update()
 
     def gradients(self):
@@ -160,6 +169,32 @@ class Trainer:
         self.n, self.now = n, new
         self.layout()
 
+    def attend(self):
+        """Between a step's gradients and its update, which changes the
+        Gaussians that were sampled: the attention weight of its batch."""
+        work = gs.alloc_shares_work(self.index, self.query, self.device)
+        gs.gs_shares(self.gauss, self.index, self.query, self.plan, self.influence, self.scores[self.now][:self.n],
+                     work, decay=SCORE_DECAY)
+
+    def rebalance(self):
+        """Moves the Gaussians of the least score to where the most attention
+        is; their number stays, and moments follow. Nothing is waited for."""
+        old, new, n = self.now, 1 - self.now, self.n
+        p, score = self.sets[new], self.scores[new]
+        keep = gs.gs_evict(self.sets[old], n, self.scores[old], n - int(MOVED * n), p, self.source,
+                           gs.alloc_evict_work(n, self.device), score_out=score)
+        moved = n - keep
+        ids = torch.empty(moved, dtype=torch.int32, device=self.device)
+        uniform = torch.rand(moved, dtype=torch.float64, generator=self.gen, device=self.device)
+        gs.gs_draw(score[:keep], uniform, ids, gs.alloc_draw_work(1, keep, moved, self.device))
+        gs.gs_split(p, keep, ids, self.source, gs.alloc_split_work(keep, self.device), score=score)
+        # copies at one place would learn the same
+        p.mean[keep:n] += APART * torch.exp(p.log_scale[keep:n]) * torch.randn(moved, 3, generator=self.gen,
+                                                                               device=self.device)
+        gs.gs_adamw_carry(self.carries[old], n, self.source, n)
+        self.now = new
+        self.layout()
+
     def loss(self):
         return gs.read_loss_terms(self.terms)["total"]
 
@@ -172,11 +207,13 @@ class Trainer:
         return -10.0 * math.log10(float(err))
 
 
-def train(t, steps, densify_every=100, report=None):
+def train(t, steps, densify_every=100, report=None, rebalance_every=0):
     """`steps` iterations of a Trainer; returns [(step, Gaussians, loss)]."""
     seen = []
     for k in range(1, steps + 1):
-        t.step()
+        t.step(attend=rebalance_every > 0)
+        if rebalance_every and k % rebalance_every == 0 and k < steps:
+            t.rebalance()
         if densify_every and k % densify_every == 0 and k < steps:
             t.densify(t.sets[0].rows // 10)
         if k % 50 == 0 or k in (1, steps):
@@ -193,10 +230,12 @@ def main():
     ap.add_argument("--steps", type=int, default=600)
     ap.add_argument("--moments", type=int, choices=(8, 32), default=8, help="bits of the optimiser's moments")
     ap.add_argument("--densify-every", type=int, default=100)
+    ap.add_argument("--rebalance-every", type=int, default=0,
+                    help="hold the number of Gaussians and move a tenth of them this often (no densification then)")
     a = ap.parse_args()
     t = Trainer(a.gaussians, a.dims, gs.GS_MOMENTS_MXFP8 if a.moments == 8 else gs.GS_MOMENTS_F32)
-    train(t, a.steps, a.densify_every,
-          lambda k, n, x: print(f"step {k:5d}  {n:8d} Gaussians  loss {x:.5f}", flush=True))
+    train(t, a.steps, 0 if a.rebalance_every else a.densify_every,
+          lambda k, n, x: print(f"step {k:5d}  {n:8d} Gaussians  loss {x:.5f}", flush=True), a.rebalance_every)
     c = gs.read_adam_control(t.control)
     print(f"{c['step']} steps, {c['skipped']} skipped, last gradient norm {c['norm']:.3g}, PSNR {t.psnr():.2f} dB")
 

@@ -585,6 +585,48 @@ def test_a_budget_round():
     assert torch.isfinite(kept).all()
 
 
+@pytest.mark.parametrize("form", ["f32", "mxfp8"])
+def test_training_under_a_budget(form):
+    """examples/train_field.py with --rebalance-every: scores follow the
+    batches, the moved Gaussians the definition, and the number stays."""
+    from examples.train_field import APART, MOVED, SCORE_DECAY, TAU as TRAIN_TAU, Trainer, train
+    t = Trainer(moments=gs.GS_MOMENTS_F32 if form == "f32" else gs.GS_MOMENTS_MXFP8, n=1000, dims=32)
+    n = t.n
+    score = np.zeros(n)
+    for _ in range(3):
+        t.gradients()
+        got = gs.Gaussians(*(getattr(t.gauss, k).clone() for k in ("mean", "scale", "rot", "value", "weight")))
+        t.attend()
+        t.update()
+        g = synth.Gaussians(*(getattr(got, k).cpu().numpy() for k in ("mean", "scale", "rot", "value", "weight")))
+        points = voxel_positions(t.dims, np.arange(32 ** 3), t.offsets.cpu().numpy(), (0, 0, 0), (1, 1, 1))
+        score, tol = bo.shares(g, points, t.influence.cpu().numpy(), None, score, SCORE_DECAY)
+        seen = t.scores[t.now][:n].cpu().numpy()
+        assert (np.abs(seen - score) <= tol).all()
+        score = seen
+    before = {k: getattr(t.sets[t.now], k)[:n].cpu().numpy() for k in ARRAYS}
+    score = t.scores[t.now][:n].cpu().numpy()
+    keep = n - int(MOVED * n)
+    t.rebalance()
+    assert t.n == n
+    at = bo.evict(score, keep)
+    source = t.source[:n].cpu().numpy()
+    assert np.array_equal(source[:keep], at)
+    ids = -1 - source[keep:]
+    assert (ids >= 0).all() and (ids < keep).all()
+    after = {k: getattr(t.sets[t.now], k)[:n].cpu().numpy() for k in ARRAYS}
+    for k in ("mean", "log_scale", "rot", "value_logit"):
+        assert np.array_equal(after[k][:keep], before[k][at])
+    for k in ("log_scale", "rot", "value_logit"):
+        assert np.array_equal(after[k][keep:], after[k][ids])
+    far = np.abs(after["mean"][keep:] - after["mean"][ids]) / np.exp(after["log_scale"][ids])
+    assert far.max() < 8 * APART and far.min() < APART
+    assert np.array_equal(after["weight_logit"][keep:], after["weight_logit"][ids])
+    seen = train(t, 12, 0, rebalance_every=5)
+    assert seen[-1][1] == n and all(np.isfinite(x) for _, _, x in seen)
+    assert TRAIN_TAU == TAU
+
+
 @pytest.mark.parametrize("n_long", [3000, 40000])
 def test_budget_calls_in_a_graph(n_long):
     """All four calls captured on a side stream and replayed, with eager work
