@@ -37,14 +37,17 @@ size_t gs_shares_work_bytes(const gs_index *index, const gs_query *query);
  * elements to 0 to leave queries out. Queries outside the domain count for
  * nothing, whatever their influence. gain may hold any finite numbers (the
  * error of a sample, say). With gain null the new weights of all Gaussians add
- * up to the number of defined queries. For VOXELS, POINTS and JITTER queries
+ * up to the number of defined queries, up to rounding and to the pairs at the
+ * cutoff (below). For VOXELS, POINTS and JITTER queries
  * plan must be the one that gs_sample (or gs_plan_queries and
  * gs_sample_planned) filled for this index and query; influence is read from
  * the caller's array, not from the plan. gauss must be the Gaussians that the
  * index was built from, unchanged. decay = 0 overwrites score without reading
  * it (0 <= decay, finite).
  * The sums are float32, in an order that the inputs alone fix. Pairs whose Q
- * is so near the cutoff that float32 cannot tell are decided in float64.
+ * is so near the cutoff that float32 cannot tell are decided in float64 from
+ * gauss (the sampler decides them in float32: of a pair that the two take
+ * differently, tau w_i / I is missing in the sum or too much).
  */
 gs_status gs_shares(const gs_gaussians *gauss, const gs_index *index, const gs_query *query, const void *plan,
                     size_t plan_bytes, const float *influence, const float *gain, float decay, float *score,

@@ -129,12 +129,13 @@ struct SharesArgs {
 // voxels holds points of the slab [y, y + 1] x [z, z + 1]. With e the part of
 // u = U d that depends on y and z alone, |e| over the slab is at least its value
 // at the slab's centre less `reach`, the largest |e| of half a voxel; so is Q
-// >= |e|^2. In x the row's centre moves by at most `shift` over the slab.
+// >= |e|^2. In x the row's centre moves by at most `shift` over the slab. (The
+// slab is widened by what rounding moves a position.)
 struct VoxelReach {
     float reach, shift;
 };
-__device__ __forceinline__ VoxelReach voxel_reach(const Record &r, const QueryParams &q) {
-    const float hy = 0.5f * q.vsz[1], hz = 0.5f * q.vsz[2];
+__device__ __forceinline__ VoxelReach voxel_reach(const Record &r, const QueryParams &q, const BwdGeom &bg) {
+    const float hy = (0.5f + bg.vslack[1]) * q.vsz[1], hz = (0.5f + bg.vslack[2]) * q.vsz[2];
     const float e1 = fabsf(r.f2.x) * hy + fabsf(r.f2.y) * hz, e2 = fabsf(r.f2.z) * hz;
     VoxelReach v;
     v.reach = sqrt_hw(fmaf_(e1, e1, e2 * e2)) * (1.0f + 0x1p-10f);
@@ -267,7 +268,7 @@ __global__ __launch_bounds__(kWave) void k_shares(SharesArgs a) {
             if (WALK == kWalkGrid)
                 len = grid_row(r, x0, nx, vy, vz, a.q, a.g, a.bg, vx, py, pz);
             else if (voxels)
-                len = voxel_row(r, voxel_reach(r, a.q), vy, vz, a.q, a.g, a.bg, vx);
+                len = voxel_row(r, voxel_reach(r, a.q, a.bg), vy, vz, a.q, a.g, a.bg, vx);
             else
                 len = plan_row(r, x0, nx, vy, vz, a.g, a.bg, a.point_off, start);
             if (WALK == kWalkGrid || voxels)

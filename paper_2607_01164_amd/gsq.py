@@ -1015,9 +1015,12 @@ def _work_size(b: int, what: str) -> int:
 
 
 def _one_device(dev: int, **tensors) -> None:
+    """All tensors on one device, the current one: kernels run there."""
     for name, t in tensors.items():
         if t is not None and t.get_device() != dev:
             raise ValueError(f"{name} must be on the same device as the others")
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on device {dev}, which is not the current one")
 
 
 def _row_of(t: Optional[torch.Tensor], name: str, dtype, n: int) -> None:

@@ -105,6 +105,7 @@ KINDS = {
     # from 4096 queries on jittered grids are walked by voxels, unless a
     # position leaves its voxel
     "jitter_voxels": dict(kind="jitter", cells=(4, 5, 3), dims=(21, 18, 17), lo=(-1.0, 0.5, 3.0), hi=(1.0, 1.5, 3.7)),
+    "jitter_long": dict(kind="jitter", cells=(1, 64, 2), dims=(2, 30011, 3), lo=(-4.0, 10.0, 0.0), hi=(-3.9, 11.0, 0.1)),
     "jitter_stray": dict(kind="jitter", cells=(4, 5, 3), dims=(21, 18, 17), spread=0.8),
     "jitter_ids": dict(kind="jitter_ids", cells=(3, 3, 3), dims=(30, 31, 29), n=1777),
     "points": dict(kind="points", cells=(6, 6, 6), n=2003),
