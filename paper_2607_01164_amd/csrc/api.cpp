@@ -1210,7 +1210,7 @@ static const int64_t kGaussMost = (int64_t)1 << 31;
 size_t gs_shares_work_bytes(const gs_index *index, const gs_query *query) {
     std::string why;
     if (!index || index->n_pairs < 0 || !query_valid(query, &why)) return (size_t)-1;
-    return shares_layout(nullptr, query_count(query), query->kind == GS_QUERY_GRID).bytes;
+    return shares_layout(nullptr, index->n_gauss, query_count(query), query->kind == GS_QUERY_GRID).bytes;
 }
 
 gs_status gs_shares(const gs_gaussians *gauss, const gs_index *index, const gs_query *query, const void *plan,
@@ -1227,7 +1227,7 @@ gs_status gs_shares(const gs_gaussians *gauss, const gs_index *index, const gs_q
     const GridParams gp = grid_params(&index->grid);
     const QueryParams qp = query_params(query, &index->grid);
     const bool grid = query->kind == GS_QUERY_GRID;
-    const SharesWork sw = shares_layout(work, nq, grid);
+    const SharesWork sw = shares_layout(work, n, nq, grid);
     if (!work || work_bytes < sw.bytes || !aligned(work))
         return fail(GS_ERR_WORKSPACE, "gs_shares: workspace needs %zu bytes, 256-byte aligned (got %zu)", sw.bytes,
                     work_bytes);

@@ -12,9 +12,10 @@ struct SharesWork {
     float4 *pts;      // ordered queries, in the plan's or the voxels' order: position and f
     float *f;         // grids: f of every voxel
     uint32_t *stray;  // jittered grids: whether a position lies outside its voxel
+    uint32_t *teams;  // Gaussians left to teams of waves: the lists' counts, then the lists
     size_t bytes;
 };
-SharesWork shares_layout(void *work, int64_t nq, bool grid);
+SharesWork shares_layout(void *work, int64_t n_gauss, int64_t nq, bool grid);
 // The Gaussians as the caller holds them, for the pairs near the cutoff.
 struct SharesExact {
     const float *mean, *scale, *rot;

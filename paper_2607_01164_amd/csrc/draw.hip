@@ -14,7 +14,6 @@
 // masses stay in registers, the running mass goes to LDS, where the draws
 // search it. Longer rows are cut into stretches over many workgroups, with a
 // launch for each pass, and the running mass in the workspace.
-#include <type_traits>
 
 #include "budget.h"
 

@@ -1,15 +1,18 @@
 // The attention weight that every Gaussian gets from a batch of queries
 // (include/gs_budget.h): score_i <- decay score_i + w_i sum_t f_t G_i(p_t).
 //
-// A lane takes a row of a Gaussian's queries: for grids a row of voxels at
-// fixed (y, z), for ordered queries a row of cells, a run of the plan's order,
-// both cut to the cutoff ellipsoid as the backward cuts them. Along a row of
-// voxels only u0 = U00 dx + c changes, so a pair costs a subtraction, two
-// FMAs, the test, one v_exp_f32 and an FMA; there is no search for the row of
-// an element, which costs more than the pair itself (the backward's walk, a
-// lane an element, has to do it for its longer pairs). A wave takes the rows
-// of a few Gaussians, 64 at a time, and adds each Gaussian's lanes with a
-// segmented scan: no atomics, an order fixed by the inputs.
+// A Gaussian's queries come in rows: of voxels at fixed (y, z) in grids, of the
+// plan's cells for ordered queries, both cut to the cutoff ellipsoid as the
+// backward cuts them. A wave takes the rows of a few Gaussians, cuts them into
+// pieces of one width and walks them with the Gaussian's record in scalars, so
+// that a query costs its load and the 24 or so instructions of a pair; lanes
+// are added at a Gaussian's end: no atomics, an order fixed by the inputs. The
+// bound is the arithmetic over the pairs of the rows, of which the cutoff
+// keeps a fourth to a third: a 128^3 jittered grid and 131072 Gaussians, 123
+// million pairs, 174 us with the vector units busy for 74 of 100 cycles. (A
+// lane a row, each with its own record: 583 us.)
+#include <type_traits>
+
 #include "budget.h"
 
 #pragma clang fp contract(off)
@@ -18,15 +21,31 @@ namespace gs {
 namespace {
 
 // Gaussians of a wave (consecutive in gorder), so that their rows fill its
-// lanes; one a wave where there are too few to fill the chip otherwise.
+// lanes; fewer where there would be fewer waves than the chip holds (60011
+// Gaussians, a jittered 100^3 grid: one a wave 90 us, four 80).
 constexpr uint32_t kPack = 4;
-constexpr int64_t kPackMinGauss = 65536;
+constexpr int64_t kPackWaves = 8192;
+// Waves of an XCD that follow each other, so that neighbours read the same
+// queries through one L2 (a jittered 128^3 grid, 131072 Gaussians: 4 waves 195
+// us, 64 174 us, 512 181 us).
 constexpr uint32_t kXcdWaves = 64;
 // The rows of a Gaussian's queries: voxels of a grid; the plan's cells; voxels
 // of a jittered grid, every voxel with its query.
 enum { kWalkGrid = 0, kWalkPlan = 1, kWalkVoxels = 2 };
 // queries from which a jittered grid is walked by voxels
 constexpr int64_t kVoxelsLeast = 4096;
+// A Gaussian of more than kStepsMost steps in its first 64 rows, or of more than
+// kRowsMost rows, keeps its wave long after the others are done. Where there
+// are queries for such ones, they are left to the launch that follows, a
+// workgroup of kTeam waves each. (One Gaussian that reaches all of 2 M points
+// or voxels: 5.0 to 10 ms -> 0.73 to 1.5 ms; 9001 Gaussians, 300007 crowded
+// points: 114 -> 93 us; without such ones the launch costs 3 us.) They go
+// to kTeamLists lists: counts in one place wait for each other.
+constexpr uint32_t kStepsMost = 256, kRowsMost = 1024;
+constexpr uint32_t kTeam = 8;
+constexpr int64_t kTeamQueries = 65536;
+constexpr uint32_t kTeamBlocks = 512, kTeamLists = 64;
+
 // waves of one launch (a launch has fewer than 2^32 threads)
 constexpr uint64_t kWavesMost = (uint64_t)1 << 25;
 
@@ -41,8 +60,10 @@ __device__ __forceinline__ float query_factor(const float *influence, const floa
 }
 
 __global__ __launch_bounds__(kBlock) void k_shares_stage_grid(int64_t n, const float *__restrict__ influence,
-                                                              const float *__restrict__ gain, float *__restrict__ f) {
+                                                              const float *__restrict__ gain, float *__restrict__ f,
+                                                              uint32_t *__restrict__ teams) {
     const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (i < kTeamLists) teams[i] = 0;
     if (i < n) f[i] = query_factor(influence, gain, i);
 }
 
@@ -50,8 +71,10 @@ __global__ __launch_bounds__(kBlock) void k_shares_stage_plan(int64_t n, const u
                                                               const float4 *__restrict__ pos,
                                                               const float *__restrict__ influence,
                                                               const float *__restrict__ gain,
-                                                              float4 *__restrict__ pts) {
+                                                              float4 *__restrict__ pts,
+                                                              uint32_t *__restrict__ teams) {
     const int64_t k = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (k < kTeamLists) teams[k] = 0;
     if (k >= n) return;
     const float4 p = pos[k];
     pts[k] = make_float4(p.x, p.y, p.z, query_factor(influence, gain, order[k]));
@@ -64,8 +87,10 @@ __global__ __launch_bounds__(kBlock) void k_shares_stage_voxels(QueryParams q, G
                                                                 const float *__restrict__ influence,
                                                                 const float *__restrict__ gain,
                                                                 float4 *__restrict__ pts,
-                                                                uint32_t *__restrict__ stray) {
+                                                                uint32_t *__restrict__ stray,
+                                                                uint32_t *__restrict__ teams) {
     const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+    if (i < kTeamLists) teams[i] = 0;
     if (i >= q.n) return;
     float p[3];
     bool valid, in = true, home = true;
@@ -121,6 +146,8 @@ struct SharesArgs {
     SharesExact exact;
     float T, decay;
     float *score;
+    uint32_t *teams;  // Gaussians left to teams: the lists' counts, then the lists (null: none are left)
+    uint32_t team_room;
     uint32_t pack;
     uint64_t wave0;  // the launch's first wave
 };
@@ -194,21 +221,20 @@ constexpr uint32_t kAhead = 2;
 constexpr uint32_t kPieces = 4;
 constexpr uint32_t kEntries = kPieces * kWave + kAhead * 16;  // the last steps read past their rows
 
-template <int WALK>
-__global__ __launch_bounds__(kWave) void k_shares(SharesArgs a) {
-    __shared__ uint2 s_row[kEntries];   // first query, queries
-    __shared__ uint4 s_grid[WALK == kWalkGrid ? kEntries : 1];  // grids: first x, y and z
-    const uint32_t lane = threadIdx.x;
-    const uint64_t first = (a.wave0 + xcd_group<kXcdWaves>(blockIdx.x, gridDim.x)) * a.pack;
-    if (first >= (uint64_t)a.n_gauss) return;
-    const uint32_t nk = (uint64_t)a.n_gauss - first < a.pack ? (uint32_t)((uint64_t)a.n_gauss - first) : a.pack;
+// The sums of a wave's Gaussians, lane i < nk Gaussian i's (mgid). part of
+// parts: of the steps, or of the rows where there are many, this wave takes its
+// share. LEAVE: Gaussians of too many steps are left out, in `left` by bit.
+template <int WALK, bool LEAVE>
+__device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32_t nk, uint32_t part, uint32_t parts,
+                                      uint32_t &left, uint2 *s_row, uint4 *s_grid) {
+    const uint32_t lane = threadIdx.x % kWave;
     const float T = a.T;
     // positions that leave their voxels: the plan's rows, through its order
     const bool voxels = WALK == kWalkVoxels && *a.stray == 0;
+    left = 0;
     // lane i < nk describes Gaussian i of the wave: its rows
-    uint32_t mgid = 0, mR = 0, mnx = 0, mny = 1, mx = 0, my = 0, mz = 0;
+    uint32_t mR = 0, mnx = 0, mny = 1, mx = 0, my = 0, mz = 0;
     if (lane < nk) {
-        mgid = a.gorder[first + lane];
         const CellBox b = a.box[mgid];
         if (b.hi.x >= b.lo.x && a.q.n > 0) {
             if (WALK == kWalkGrid) {
@@ -239,6 +265,7 @@ __global__ __launch_bounds__(kWave) void k_shares(SharesArgs a) {
     float mtot = 0.0f;  // lane i < nk: Gaussian i's sum
     float acc = 0.0f;   // of the Gaussian being walked
     uint32_t cur = ~0u, cgid = 0;
+    bool skip = false;
     Record c = {};
     float margin = 0.0f;
     auto finish = [&]() {
@@ -248,7 +275,10 @@ __global__ __launch_bounds__(kWave) void k_shares(SharesArgs a) {
         if (lane == cur) mtot = t;
         acc = 0.0f;
     };
-    for (uint32_t rb = 0; rb < Rw; rb += kWave) {
+    const bool by_rows = Rw > kWave;
+    const uint32_t rb0 = by_rows ? part * kWave : 0u, rb_step = by_rows ? parts * kWave : (uint32_t)kWave;
+    const uint32_t sub = by_rows ? 0u : part, subs = by_rows ? 1u : parts;
+    for (uint32_t rb = rb0; rb < Rw; rb += rb_step) {
         // lane l sets up row rb + l of the wave's list, of Gaussian i (the
         // permutes run with every lane)
         const uint32_t gr = rb + lane;
@@ -288,23 +318,31 @@ __global__ __launch_bounds__(kWave) void k_shares(SharesArgs a) {
             if (WALK == kWalkGrid) s_grid[at] = make_uint4(vx + from, __float_as_uint(py), __float_as_uint(pz), 0);
         }
         __builtin_amdgcn_wave_barrier();
+        const uint32_t limit = whole ? 0u : kStepsMost << (6u - shift);  // pieces of so many steps
         const uint32_t nrows = Rw - rb < (uint32_t)kWave ? Rw - rb : (uint32_t)kWave;
         const uint32_t ia = __builtin_amdgcn_readlane(i, 0), ib = __builtin_amdgcn_readlane(i, nrows - 1);
         for (uint32_t gi = ia; gi <= ib; ++gi) {
             const uint32_t gend = __builtin_amdgcn_readlane(mRend, gi), gR = __builtin_amdgcn_readlane(mR, gi);
             if (gR == 0) continue;
-            if (gi != cur) {
-                if (cur != ~0u) finish();
-                cur = gi;
-                cgid = __builtin_amdgcn_readlane(mgid, gi);
-                c = load_record_uniform(a.rec, cgid);
-                margin = readfirst_f(cutoff_margin(a.exact, cgid, T));
-            }
             // its rows in this batch, and their pieces
             const uint32_t la = gend - gR > rb ? gend - gR - rb : 0u;
             const uint32_t lb = gend - rb < nrows ? gend - rb : nrows;
             const uint32_t ra = la ? __builtin_amdgcn_readlane(upto, la - 1) : 0u;
             const uint32_t rz = lb ? __builtin_amdgcn_readlane(upto, lb - 1) : 0u;
+            if (gi != cur) {
+                if (cur != ~0u) finish();
+                cur = gi;
+                skip = LEAVE && (gR > kRowsMost || rz - ra > limit);
+                if (LEAVE && skip && gR <= kRowsMost && whole) {
+                    const uint32_t all = wave_incl_sum(lane >= la && lane < lb ? len : 0u);
+                    skip = __builtin_amdgcn_readlane(all, kWave - 1) / kWave > kStepsMost;
+                }
+                left |= skip ? 1u << gi : 0u;
+                cgid = __builtin_amdgcn_readlane(mgid, gi);
+                c = load_record_uniform(a.rec, cgid);
+                margin = readfirst_f(cutoff_margin(a.exact, cgid, T));
+            }
+            if (LEAVE && skip) continue;
             // kAhead queries of a lane: query k[u] if on[u], at voxel x[u] of
             // its row in grids
             auto add = [&](const uint32_t k[kAhead], const bool on[kAhead], const uint4 v[kAhead]) {
@@ -347,7 +385,7 @@ __global__ __launch_bounds__(kWave) void k_shares(SharesArgs a) {
             };
             if (!whole) {
                 const uint32_t rows = (uint32_t)kWave >> shift;  // of a step
-                for (uint32_t r0 = ra; r0 < rz; r0 += kAhead * rows) {
+                for (uint32_t r0 = ra + sub * kAhead * rows; r0 < rz; r0 += subs * kAhead * rows) {
                     uint32_t k[kAhead];
                     bool on[kAhead];
                     uint4 v[kAhead] = {};
@@ -369,7 +407,7 @@ __global__ __launch_bounds__(kWave) void k_shares(SharesArgs a) {
                     const uint2 w = s_row[row];
                     uint4 g = make_uint4(0, 0, 0, 0);
                     if (WALK == kWalkGrid) g = s_grid[row];
-                    for (uint32_t e0 = 0; e0 < w.y; e0 += kAhead * kWave) {
+                    for (uint32_t e0 = sub * kAhead * kWave; e0 < w.y; e0 += subs * kAhead * kWave) {
                         uint32_t k[kAhead];
                         bool on[kAhead];
                         uint4 v[kAhead];
@@ -387,11 +425,59 @@ __global__ __launch_bounds__(kWave) void k_shares(SharesArgs a) {
         }
     }
     if (cur != ~0u) finish();
-    if (lane < nk) {
-        const float add = a.rec[mgid].f0.w * mtot;
-        a.score[mgid] = a.decay > 0.0f ? fmaf_(a.decay, a.score[mgid], add) : add;
+    return mtot;
+}
+
+__device__ __forceinline__ void add_score(const SharesArgs &a, uint32_t gid, float sum) {
+    const float add = a.rec[gid].f0.w * sum;
+    a.score[gid] = a.decay > 0.0f ? fmaf_(a.decay, a.score[gid], add) : add;
+}
+
+template <int WALK, bool LEAVE>
+__global__ __launch_bounds__(kWave) void k_shares(SharesArgs a) {
+    __shared__ uint2 s_row[kEntries];   // first query, queries
+    __shared__ uint4 s_grid[WALK == kWalkGrid ? kEntries : 1];  // grids: first x, y and z
+    const uint32_t lane = threadIdx.x;
+    const uint64_t first = (a.wave0 + xcd_group<kXcdWaves>(blockIdx.x, gridDim.x)) * a.pack;
+    if (first >= (uint64_t)a.n_gauss) return;
+    const uint32_t nk = (uint64_t)a.n_gauss - first < a.pack ? (uint32_t)((uint64_t)a.n_gauss - first) : a.pack;
+    const uint32_t gid = lane < nk ? a.gorder[first + lane] : 0u;
+    uint32_t left;
+    const float sum = walk<WALK, LEAVE>(a, gid, nk, 0, 1, left, s_row, s_grid);
+    if (lane >= nk) return;
+    if (LEAVE && (left >> lane & 1u)) {
+        const uint32_t list = (uint32_t)((a.wave0 + blockIdx.x) % kTeamLists);
+        a.teams[kTeamLists + (size_t)list * a.team_room + atomicAdd(&a.teams[list], 1u)] = gid;
+    } else
+        add_score(a, gid, sum);
+}
+
+// The Gaussians that k_shares left, a workgroup each.
+template <int WALK>
+__global__ __launch_bounds__(kTeam * kWave) void k_shares_team(SharesArgs a) {
+    __shared__ uint2 s_row[kTeam][kEntries];
+    __shared__ uint4 s_grid[WALK == kWalkGrid ? kTeam : 1][WALK == kWalkGrid ? kEntries : 1];
+    __shared__ float s_sum[kTeam];
+    const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const uint32_t list = blockIdx.x % kTeamLists, count = a.teams[list];
+    for (uint32_t i = blockIdx.x / kTeamLists; i < count; i += gridDim.x / kTeamLists) {
+        const uint32_t gid = a.teams[kTeamLists + (size_t)list * a.team_room + i];
+        uint32_t left;
+        const float sum = walk<WALK, false>(a, gid, 1, wave, kTeam, left, s_row[wave],
+                                            s_grid[WALK == kWalkGrid ? wave : 0]);
+        if (lane == 0) s_sum[wave] = sum;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            float all = 0.0f;
+#pragma unroll
+            for (uint32_t w = 0; w < kTeam; ++w) all += s_sum[w];
+            add_score(a, gid, all);
+        }
+        __syncthreads();
     }
 }
+
+bool has_teams(int64_t nq) { return nq >= kTeamQueries; }
 
 size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -399,14 +485,17 @@ size_t al256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 bool walks_voxels(const QueryParams &q) { return q.kind == 3 && !q.voxel_ids && q.n >= kVoxelsLeast; }
 
-SharesWork shares_layout(void *work, int64_t nq, bool grid) {
+SharesWork shares_layout(void *work, int64_t n_gauss, int64_t nq, bool grid) {
     SharesWork w;
     const size_t m = (size_t)(nq > 0 ? nq : 1);
-    w.stray = (uint32_t *)work;
-    char *rest = work ? (char *)work + 256 : nullptr;
-    w.pts = grid ? nullptr : (float4 *)rest;
-    w.f = grid ? (float *)rest : nullptr;
-    w.bytes = 256 + al256(m * (grid ? sizeof(float) : sizeof(float4)));
+    char *b = (char *)work;
+    w.stray = (uint32_t *)b;
+    w.teams = b ? (uint32_t *)(b + 256) : nullptr;
+    const size_t room = has_teams(nq) ? (size_t)n_gauss + kTeamLists * kPack : 0;
+    const size_t head = 256 + al256(sizeof(uint32_t) * (kTeamLists + room));
+    w.pts = grid || !b ? nullptr : (float4 *)(b + head);
+    w.f = grid && b ? (float *)(b + head) : nullptr;
+    w.bytes = head + al256(m * (grid ? sizeof(float) : sizeof(float4)));
     return w;
 }
 
@@ -416,19 +505,20 @@ hipError_t launch_shares(const QueryParams &q, const GridParams &g, const BwdGeo
                          const float *influence, const float *gain, float decay, float *score,
                          const SharesWork &w, hipStream_t s) {
     if (n_gauss <= 0) return hipSuccess;
-    const int walk = q.kind == 0 ? kWalkGrid : walks_voxels(q) ? kWalkVoxels : kWalkPlan;
+    const int kind = q.kind == 0 ? kWalkGrid : walks_voxels(q) ? kWalkVoxels : kWalkPlan;
     hipError_t e;
     if (q.n > 0) {
         const dim3 nb((uint32_t)((q.n + kBlock - 1) / kBlock));
         prof_begin("shares_stage", s);
-        if (walk == kWalkGrid) {
-            hipLaunchKernelGGL(k_shares_stage_grid, nb, dim3(kBlock), 0, s, q.n, influence, gain, w.f);
-        } else if (walk == kWalkVoxels) {
+        if (kind == kWalkGrid) {
+            hipLaunchKernelGGL(k_shares_stage_grid, nb, dim3(kBlock), 0, s, q.n, influence, gain, w.f, w.teams);
+        } else if (kind == kWalkVoxels) {
             if ((e = fill_u32(w.stray, 0u, 1, s)) != hipSuccess) return e;
-            hipLaunchKernelGGL(k_shares_stage_voxels, nb, dim3(kBlock), 0, s, q, g, influence, gain, w.pts, w.stray);
+            hipLaunchKernelGGL(k_shares_stage_voxels, nb, dim3(kBlock), 0, s, q, g, influence, gain, w.pts, w.stray,
+                               w.teams);
         } else {
             hipLaunchKernelGGL(k_shares_stage_plan, nb, dim3(kBlock), 0, s, q.n, order, plan_pos, influence, gain,
-                               w.pts);
+                               w.pts, w.teams);
         }
         prof_end("shares_stage", s);
         if ((e = hipGetLastError()) != hipSuccess) return e;
@@ -451,21 +541,44 @@ hipError_t launch_shares(const QueryParams &q, const GridParams &g, const BwdGeo
     a.decay = decay;
     a.score = score;
     // a wave's rows are counted in 32 bits
-    const int64_t rows = walk == kWalkPlan ? (int64_t)g.cells[1] * g.cells[2] : (int64_t)q.dims[1] * q.dims[2];
-    a.pack = n_gauss < kPackMinGauss || rows > ((int64_t)1 << 31) / kPack ? 1u : kPack;
+    const int64_t rows = kind == kWalkPlan ? (int64_t)g.cells[1] * g.cells[2] : (int64_t)q.dims[1] * q.dims[2];
+    const int64_t most = n_gauss / kPackWaves < (int64_t)kPack ? n_gauss / kPackWaves : (int64_t)kPack;
+    a.pack = most < 1 || rows > ((int64_t)1 << 31) / kPack ? 1u : (uint32_t)most;
     const uint64_t waves = ((uint64_t)n_gauss + a.pack - 1) / a.pack;
+    a.teams = has_teams(q.n) ? w.teams : nullptr;
+    a.team_room = (uint32_t)((waves + kTeamLists - 1) / kTeamLists * a.pack);
     prof_begin("shares", s);
     for (a.wave0 = 0; a.wave0 < waves; a.wave0 += kWavesMost) {
         const uint64_t left = waves - a.wave0;
         const dim3 wb((uint32_t)(left < kWavesMost ? left : kWavesMost));
-        if (walk == kWalkGrid)
-            hipLaunchKernelGGL(k_shares<kWalkGrid>, wb, dim3(kWave), 0, s, a);
-        else if (walk == kWalkVoxels)
-            hipLaunchKernelGGL(k_shares<kWalkVoxels>, wb, dim3(kWave), 0, s, a);
+        auto launch = [&](auto walk, auto leave) {
+            hipLaunchKernelGGL((k_shares<decltype(walk)::value, decltype(leave)::value>), wb, dim3(kWave), 0, s, a);
+        };
+        auto each = [&](auto leave) {
+            if (kind == kWalkGrid)
+                launch(std::integral_constant<int, kWalkGrid>(), leave);
+            else if (kind == kWalkVoxels)
+                launch(std::integral_constant<int, kWalkVoxels>(), leave);
+            else
+                launch(std::integral_constant<int, kWalkPlan>(), leave);
+        };
+        if (a.teams)
+            each(std::true_type());
         else
-            hipLaunchKernelGGL(k_shares<kWalkPlan>, wb, dim3(kWave), 0, s, a);
+            each(std::false_type());
     }
     prof_end("shares", s);
+    if (a.teams) {
+        const dim3 tb(kTeamBlocks), tt(kTeam * kWave);
+        prof_begin("shares_team", s);
+        if (kind == kWalkGrid)
+            hipLaunchKernelGGL(k_shares_team<kWalkGrid>, tb, tt, 0, s, a);
+        else if (kind == kWalkVoxels)
+            hipLaunchKernelGGL(k_shares_team<kWalkVoxels>, tb, tt, 0, s, a);
+        else
+            hipLaunchKernelGGL(k_shares_team<kWalkPlan>, tb, tt, 0, s, a);
+        prof_end("shares_team", s);
+    }
     return hipGetLastError();
 }
 

@@ -154,6 +154,28 @@ def test_shares_many_gaussians_and_long_rows(kind):
     assert abs(out.astype(np.float64).sum() - total) <= 2e-5 * len(b.points)
 
 
+@pytest.mark.parametrize("kind", ["grid", "jitter", "jitter_stray", "points", "voxels"])
+def test_shares_of_gaussians_with_most_of_the_queries(kind):
+    """A few Gaussians over the whole domain among small ones, whose queries or
+    rows are too many for one wave; queries crowded in a few cells."""
+    r = np.random.default_rng(7)
+    n = 90
+    g = synth.random_gaussians(13, n, log_mu=math.log(0.02), log_sd=0.5)
+    g.scale[::9] *= 12
+    g.scale[5] = (0.5, 0.4, 0.6)
+    if kind == "points":
+        crowd = 0.5 + 0.02 * r.standard_normal((60000, 3))
+        b = Batch(g, "points", (9, 9, 9), points=np.concatenate([crowd, r.random((10001, 3))]))
+    elif kind == "voxels":
+        b = Batch(g, "voxels", (9, 9, 9), (50, 51, 52), n=70001)
+    else:
+        b = Batch(g, kind.split("_")[0], (8, 8, 8), (48, 48, 48), spread=0.7 if kind == "jitter_stray" else 0.0)
+    b.check()
+    b.check(gain=r.standard_normal(len(b.points)).astype(np.float32), score=r.random(n).astype(np.float32), decay=0.5)
+    a = b.shares(torch.empty(n, device=DEV))
+    assert all(torch.equal(a, b.shares(torch.empty(n, device=DEV))) for _ in range(3))
+
+
 def test_shares_left_out_queries():
     """Influence set to 0 by the caller, or not a number: left out; a decay
     without queries."""
