@@ -1209,7 +1209,7 @@ static const int64_t kGaussMost = (int64_t)1 << 31;
 
 size_t gs_shares_work_bytes(const gs_index *index, const gs_query *query) {
     std::string why;
-    if (!index || index->n_pairs < 0 || !query_valid(query, &why)) return (size_t)-1;
+    if (!index || index->n_pairs < 0 || index->n_gauss < 0 || !query_valid(query, &why)) return (size_t)-1;
     return shares_layout(nullptr, index->n_gauss, query_count(query), query->kind == GS_QUERY_GRID).bytes;
 }
 
@@ -1241,8 +1241,9 @@ gs_status gs_shares(const gs_gaussians *gauss, const gs_index *index, const gs_q
     const IndexWork w = index_layout(index->work, n, &index->grid, index->capacity);
     const float T = cutoff_T(index->tau);
     const SharesExact exact{gauss->mean, gauss->scale, gauss->rot, 2.0 * std::log(1.0 / (double)index->tau)};
-    GS_TRY(launch_shares(qp, gp, bwd_geom(gp, qp, T, query->kind == GS_QUERY_GRID || query->kind == GS_QUERY_JITTER), w.rec, w.box, w.gorder, n, p.order, p.point_off, p.res.pos, T,
-                         exact, influence, gain, decay, score, sw, stream),
+    const BwdGeom bg = bwd_geom(gp, qp, T, grid || query->kind == GS_QUERY_JITTER);
+    GS_TRY(launch_shares(qp, gp, bg, w.rec, w.box, w.gorder, n, p.order, p.point_off, p.res.pos, T, exact, influence,
+                         gain, decay, score, sw, stream),
            "gs_shares");
     return GS_OK;
 }

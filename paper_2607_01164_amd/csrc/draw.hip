@@ -12,8 +12,12 @@
 //
 // A row that fits the registers and LDS of a workgroup is one launch: keys and
 // masses stay in registers, the running mass goes to LDS, where the draws
-// search it. Longer rows are cut into stretches over many workgroups, with a
-// launch for each pass, and the running mass in the workspace.
+// search it. Longer rows are cut into stretches over many workgroups. Where
+// few candidates stay, every workgroup lists its stretch's best, and the lists
+// are drawn from like a short row; otherwise every pass is a launch, and the
+// running mass goes to the workspace.
+
+#include <type_traits>
 
 #include "budget.h"
 
@@ -363,8 +367,53 @@ __device__ __forceinline__ uint32_t pass_bin(const unsigned long long *hist, uin
     return (uint32_t)out[0];
 }
 
+// The digits of a workgroup's keys: of key - least, from the one that holds the
+// spread's highest bit (at `first`) on.
+struct Digits {
+    uint32_t least;
+    int first;
+    // whether the digits above `shift` of a candidate's offset are those of z
+    __device__ __forceinline__ bool reach(uint32_t k, uint32_t z, int shift) const {
+        return k != 0 && (shift >= 24 || ((k - least) >> (shift + 8)) == z);
+    }
+    __device__ __forceinline__ uint32_t at(uint32_t k, int shift) const { return (k - least) >> shift & 255u; }
+};
+__device__ __forceinline__ Digits digits_of(uint32_t top, uint32_t least) {
+    const uint32_t spread = top ? top - least : 0u;
+    return Digits{least, spread ? (31 - __builtin_clz(spread)) / 8 * 8 : 0};
+}
+
+// The first top_k of a workgroup's candidates; all of them if they are no more.
 template <int NT, int ITEMS>
-__global__ __launch_bounds__(NT) void k_draw_rows(DrawArgs a) {
+__device__ __forceinline__ Kept top_kept(const uint32_t key[ITEMS], uint32_t top_k, const Digits &dg,
+                                         unsigned long long *s_hist, uint64_t *lds, uint64_t *s_out) {
+    if (group_sum<NT>(live<ITEMS>(key), lds) <= top_k) return Kept{0, 0xFFFFFFFFu};
+    uint64_t need = top_k;
+    uint32_t z = 0;
+    for (int shift = dg.first; shift >= 0; shift -= 8) {
+        __syncthreads();
+        for (uint32_t b = threadIdx.x; b < kSmallBins; b += NT) s_hist[b] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < ITEMS; ++t)
+            if (dg.reach(key[t], z, shift)) atomicAdd((uint32_t *)&s_hist[dg.at(key[t], shift)], 1u);
+        uint64_t above;
+        z = z << 8 | pass_bin<NT>(s_hist, need - 1, &above, s_out);
+        need -= above;
+    }
+    return Kept{dg.least + z, (uint32_t)need};
+}
+
+// Lists of candidates that stand for the rows: keys (0: none) and numbers.
+struct Lists {
+    uint32_t *key, *id;  // [rows][stride]
+    int64_t stretch;     // candidates of a row's stretch
+    uint32_t stride, stretches, want;  // want: entries of a stretch's list
+};
+
+// Draws from rows of a workgroup. LIST: the rows are lists, a.n entries each.
+template <int NT, int ITEMS, bool LIST>
+__global__ __launch_bounds__(NT) void k_draw_rows(DrawArgs a, Lists lists) {
     // a thread's entries are followed by an empty one, so that threads do not
     // meet in a bank
     __shared__ uint64_t s_run[NT * (ITEMS + 1)];
@@ -372,12 +421,24 @@ __global__ __launch_bounds__(NT) void k_draw_rows(DrawArgs a) {
     __shared__ uint64_t lds[NT / kWave + 2];
     uint64_t *s_out = lds + NT / kWave;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const uint32_t len = row_length(a, row);
         uint32_t key[ITEMS], top = 0, over = 0;  // over: ~key, for the least
         uint64_t q[ITEMS];
         const uint32_t j0 = threadIdx.x * ITEMS;
+        if (LIST) {
 #pragma unroll
-        for (int t = 0; t < ITEMS; t += 4) load_keys(a, row, j0 + t, len, len, key + t);
+            for (int t = 0; t < ITEMS; t += 4) {
+                const uint32_t j = j0 + t, last = lists.stride - 4;
+                const uint4 v = *(const uint4 *)(lists.key + row * lists.stride + (j < last ? j : last));
+                key[t] = j <= last ? v.x : 0u;
+                key[t + 1] = j <= last ? v.y : 0u;
+                key[t + 2] = j <= last ? v.z : 0u;
+                key[t + 3] = j <= last ? v.w : 0u;
+            }
+        } else {
+            const uint32_t len = row_length(a, row);
+#pragma unroll
+            for (int t = 0; t < ITEMS; t += 4) load_keys(a, row, j0 + t, len, len, key + t);
+        }
 #pragma unroll
         for (int t = 0; t < ITEMS; ++t) {
             top = umax_(top, key[t]);
@@ -391,31 +452,8 @@ __global__ __launch_bounds__(NT) void k_draw_rows(DrawArgs a) {
         if (a.form == kBest) {
             kept = Kept{top, 1};
         } else if (a.top_k < (uint32_t)a.n || a.top_p) {
-            const uint32_t least = ~group_max<NT>(over, lds);  // 2^32 - 1: no candidate
-            const uint32_t spread = top ? top - least : 0u;
-            const int first = spread ? (31 - __builtin_clz(spread)) / 8 * 8 : 0;
-            // the digits above `shift` of a candidate's offset are those of z
-            auto in_reach = [&](uint32_t k, uint32_t z, int shift) {
-                return k != 0 && (shift >= 24 || ((k - least) >> (shift + 8)) == z);
-            };
-            // (with no more than top_k candidates all of them stay)
-            if (a.top_k < (uint32_t)a.n && a.top_k < group_sum<NT>(live<ITEMS>(key), lds)) {
-                uint64_t need = a.top_k;
-                uint32_t z = 0;
-                for (int shift = first; shift >= 0; shift -= 8) {
-                    __syncthreads();
-                    for (uint32_t b = threadIdx.x; b < kSmallBins; b += NT) s_hist[b] = 0;
-                    __syncthreads();
-#pragma unroll
-                    for (int t = 0; t < ITEMS; ++t)
-                        if (in_reach(key[t], z, shift))
-                            atomicAdd((uint32_t *)&s_hist[(key[t] - least) >> shift & 255u], 1u);
-                    uint64_t above;
-                    z = z << 8 | pass_bin<NT>(s_hist, need - 1, &above, s_out);
-                    need -= above;
-                }
-                kept = Kept{least + z, (uint32_t)need};
-            }
+            const Digits dg = digits_of(top, ~group_max<NT>(over, lds));
+            if (a.top_k < (uint32_t)a.n) kept = top_kept<NT, ITEMS>(key, a.top_k, dg, s_hist, lds, s_out);
             if (a.top_p) {
                 // masses of what top-k left: the equals at its end count as
                 // far as they were taken
@@ -426,21 +464,21 @@ __global__ __launch_bounds__(NT) void k_draw_rows(DrawArgs a) {
                 sum = group_sum<NT>(sum, lds) + qk;
                 uint64_t most = share_of(a.share, sum);
                 uint32_t z = 0;
-                for (int shift = first; shift >= 0; shift -= 8) {
+                for (int shift = dg.first; shift >= 0; shift -= 8) {
                     __syncthreads();
                     for (uint32_t b = threadIdx.x; b < kSmallBins; b += NT) s_hist[b] = 0;
                     __syncthreads();
 #pragma unroll
                     for (int t = 0; t < ITEMS; ++t)
-                        if (key[t] > kept.key && q[t] && in_reach(key[t], z, shift))
-                            atomicAdd(&s_hist[(key[t] - least) >> shift & 255u], (unsigned long long)q[t]);
-                    if (qk && threadIdx.x == 0 && in_reach(kept.key, z, shift))
-                        atomicAdd(&s_hist[(kept.key - least) >> shift & 255u], (unsigned long long)qk);
+                        if (key[t] > kept.key && q[t] && dg.reach(key[t], z, shift))
+                            atomicAdd(&s_hist[dg.at(key[t], shift)], (unsigned long long)q[t]);
+                    if (qk && threadIdx.x == 0 && dg.reach(kept.key, z, shift))
+                        atomicAdd(&s_hist[dg.at(kept.key, shift)], (unsigned long long)qk);
                     uint64_t above;
                     z = z << 8 | pass_bin<NT>(s_hist, most, &above, s_out);
                     most -= above;
                 }
-                const uint32_t k = top ? least + z : 0u;
+                const uint32_t k = top ? dg.least + z : 0u;
                 const uint64_t qp = mass_of(a, k, scale);
                 uint64_t ties = qp ? most / qp + 1 : 0;
                 if (k == kept.key && ties > kept.ties) ties = kept.ties;
@@ -479,11 +517,58 @@ __global__ __launch_bounds__(NT) void k_draw_rows(DrawArgs a) {
             if (total == 0) {
                 write_draw(a, at, -1, 0, 1);
             } else {
-                write_draw(a, at, lo, run_at(lo) - (lo ? run_at(lo - 1) : 0), total);
+                const uint32_t id = LIST ? lists.id[row * lists.stride + lo] : lo;
+                write_draw(a, at, id, run_at(lo) - (lo ? run_at(lo - 1) : 0), total);
             }
         }
         __syncthreads();
     }
+}
+
+// ---- lists of a long row's best --------------------------------------------
+
+// A stretch of a row: its first `want` candidates in the order of the scores,
+// listed in the order of the row. The first `want` of the row are among those
+// of its stretches.
+constexpr int kListThreads = 1024, kListItems = 16;
+__global__ __launch_bounds__(kListThreads) void k_draw_list(DrawArgs a, Lists w, uint64_t block0) {
+    __shared__ unsigned long long s_hist[kSmallBins];
+    __shared__ uint64_t lds[kListThreads / kWave + 2];
+    const uint64_t block = block0 + blockIdx.x;
+    const int64_t row = (int64_t)(block / w.stretches);
+    const uint32_t at = (uint32_t)(block % w.stretches), len = row_length(a, row);
+    const uint32_t i0 = at * (uint32_t)w.stretch, j0 = i0 + threadIdx.x * kListItems;
+    const uint32_t i1 = len <= i0 ? i0 : len - i0 < (uint32_t)w.stretch ? len : i0 + (uint32_t)w.stretch;
+    uint32_t key[kListItems], top = 0, over = 0;
+#pragma unroll
+    for (int t = 0; t < kListItems; t += 4) load_keys(a, row, j0 + t, i1, len, key + t);
+#pragma unroll
+    for (int t = 0; t < kListItems; ++t) {
+        top = umax_(top, key[t]);
+        over = umax_(over, key[t] ? ~key[t] : 0u);
+    }
+    top = group_max<kListThreads>(top, lds);
+    const Digits dg = digits_of(top, ~group_max<kListThreads>(over, lds));
+    const Kept kept = top_kept<kListThreads, kListItems>(key, w.want, dg, s_hist, lds, lds + kListThreads / kWave);
+    uint32_t mine = 0, total;  // larger: low half, equal: high half
+#pragma unroll
+    for (int t = 0; t < kListItems; ++t)
+        mine += key[t] > kept.key ? 1u : key[t] && key[t] == kept.key ? 0x10000u : 0u;
+    uint32_t run = group_scan<kListThreads>(mine, lds, &total);
+    const size_t first = (size_t)row * w.stride + (size_t)at * w.want;
+#pragma unroll
+    for (int t = 0; t < kListItems; ++t) {
+        const bool up = key[t] > kept.key, tie = key[t] && key[t] == kept.key;
+        const uint32_t equals = run >> 16, place = (run & 0xFFFFu) + (equals < kept.ties ? equals : kept.ties);
+        if (up || (tie && equals < kept.ties)) {
+            w.key[first + place] = key[t];
+            w.id[first + place] = j0 + t;
+        }
+        run += up ? 1u : tie ? 0x10000u : 0u;
+    }
+    const uint32_t ties = total >> 16, count = (total & 0xFFFFu) + (ties < kept.ties ? ties : kept.ties);
+    const uint32_t end = at + 1 == w.stretches ? w.stride - at * w.want : w.want;
+    for (uint32_t e = count + threadIdx.x; e < end; e += kListThreads) w.key[first + e] = 0;
 }
 
 // ---- rows over many workgroups --------------------------------------------
@@ -1118,12 +1203,18 @@ __global__ __launch_bounds__(kBlock) void k_draw_search(DrawArgs a, LongWork w, 
 }
 
 constexpr int64_t kRowSmall = 512, kRowMiddle = 4096, kRowLarge = 16384;
+// Lists of a row's best are drawn from where all of its stretches' fit in a row
+// of a workgroup.
+constexpr int64_t kListRow = kRowLarge, kListStretch = kListThreads * kListItems;
+size_t list_bytes(int64_t rows) { return 2 * al256(4 * (size_t)rows * kListRow); }
 constexpr uint64_t kBlocksMost = (uint64_t)1 << 21;  // workgroups of a launch (fewer than 2^32 threads)
 
 }  // namespace
 
 size_t draw_work_bytes(int64_t rows, int64_t n, int64_t) {
-    return n <= kRowLarge || rows == 0 ? 256 : long_layout(nullptr, rows, n).bytes;
+    if (n <= kRowLarge || rows == 0) return 256;
+    const size_t passes = long_layout(nullptr, rows, n).bytes, lists = list_bytes(rows);
+    return passes > lists ? passes : lists;
 }
 
 hipError_t launch_draw(int64_t rows, int64_t n, const void *scores, int64_t stride, const int32_t *lengths,
@@ -1153,24 +1244,44 @@ hipError_t launch_draw(int64_t rows, int64_t n, const void *scores, int64_t stri
     a.share = (uint64_t)(p.top_p * 0x1p53);
     a.top_k = p.top_k > 0 && p.top_k < n && a.form != kBest ? (uint32_t)p.top_k : 0xFFFFFFFFu;
     a.bf16 = p.type == GS_SCORE_BF16;
-    if (n <= kRowLarge) {
-        const uint32_t most = n <= kRowSmall ? 1u << 20 : 1u << 16;
+    auto draw_rows = [&](const DrawArgs &d, const Lists &l, auto list) {
+        constexpr bool LIST = decltype(list)::value;
+        const uint32_t most = d.n <= kRowSmall ? 1u << 20 : 1u << 16;
         const dim3 nb(rows < (int64_t)most ? (uint32_t)rows : most);
         prof_begin("draw_rows", s);
-        if (n <= kRowSmall)
-            hipLaunchKernelGGL((k_draw_rows<64, 8>), nb, dim3(64), 0, s, a);
-        else if (n <= kRowMiddle)
-            hipLaunchKernelGGL((k_draw_rows<256, 16>), nb, dim3(256), 0, s, a);
+        if (d.n <= kRowSmall)
+            hipLaunchKernelGGL((k_draw_rows<64, 8, LIST>), nb, dim3(64), 0, s, d, l);
+        else if (d.n <= kRowMiddle)
+            hipLaunchKernelGGL((k_draw_rows<256, 16, LIST>), nb, dim3(256), 0, s, d, l);
         else
-            hipLaunchKernelGGL((k_draw_rows<1024, 16>), nb, dim3(1024), 0, s, a);
+            hipLaunchKernelGGL((k_draw_rows<1024, 16, LIST>), nb, dim3(1024), 0, s, d, l);
         prof_end("draw_rows", s);
         return hipGetLastError();
-    }
-    const LongWork w = long_layout(work, rows, n);
+    };
+    if (n <= kRowLarge) return draw_rows(a, Lists{}, std::false_type());
     auto over = [](uint64_t blocks, auto launch) {
         for (uint64_t b = 0; b < blocks; b += kBlocksMost)
             launch(dim3((uint32_t)(blocks - b < kBlocksMost ? blocks - b : kBlocksMost)), b);
     };
+    const int64_t stretches = (n + kListStretch - 1) / kListStretch, want = a.form == kBest ? 1 : a.top_k;
+    if (stretches * want <= kListRow) {
+        Lists l;
+        l.stretches = (uint32_t)stretches;
+        l.stretch = ((n + stretches - 1) / stretches + 3) / 4 * 4;
+        l.want = (uint32_t)want;
+        l.stride = (uint32_t)(stretches * want + 3) / 4 * 4;
+        l.key = (uint32_t *)work;
+        l.id = (uint32_t *)((char *)work + list_bytes(rows) / 2);
+        prof_begin("draw_list", s);
+        over((uint64_t)rows * l.stretches, [&](dim3 nb, uint64_t b) {
+            hipLaunchKernelGGL(k_draw_list, nb, dim3(kListThreads), 0, s, a, l, b);
+        });
+        prof_end("draw_list", s);
+        DrawArgs d = a;
+        d.n = stretches * want;
+        return draw_rows(d, l, std::true_type());
+    }
+    const LongWork w = long_layout(work, rows, n);
     const uint64_t blocks = (uint64_t)rows * w.stretches, parts = (uint64_t)rows * w.parts;
     const dim3 tb(kThreads), pb(kBlock);
     prof_begin("draw_filter", s);

@@ -275,10 +275,13 @@ __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32
         if (lane == cur) mtot = t;
         acc = 0.0f;
     };
-    const bool by_rows = Rw > kWave;
-    const uint32_t rb0 = by_rows ? part * kWave : 0u, rb_step = by_rows ? parts * kWave : (uint32_t)kWave;
-    const uint32_t sub = by_rows ? 0u : part, subs = by_rows ? 1u : parts;
-    for (uint32_t rb = rb0; rb < Rw; rb += rb_step) {
+    // the parts share the batches of 64 rows; where those are fewer, several
+    // parts share a batch's steps
+    const uint32_t batches = Rw / kWave + (Rw % kWave ? 1u : 0u);
+    const uint32_t groups = batches < parts ? (batches ? batches : 1u) : parts;
+    const uint32_t sub = part / groups, subs = parts / groups;
+    const uint32_t rb0 = sub < subs ? part % groups * kWave : Rw;
+    for (uint32_t rb = rb0; rb < Rw; rb += groups * kWave) {
         // lane l sets up row rb + l of the wave's list, of Gaussian i (the
         // permutes run with every lane)
         const uint32_t gr = rb + lane;

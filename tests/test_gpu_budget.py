@@ -423,6 +423,33 @@ def test_draw_very_long_rows(settings):
     check_draw(scores_for("ties", 1, (1 << 21) + 5, r), 100, False, settings)
 
 
+@pytest.mark.parametrize("kind", ["weights", "tied_logits", "odd_logits", "infinite"])
+@pytest.mark.parametrize("n,top_k", [(16385, 1), (16385, 8192), (16385, 8193), (50021, 200), (49155, 4096),
+                                     (49155, 4097), (200003, 1260), (200003, 1261), (200003, 130), (999983, 17)])
+def test_draw_few_of_long_rows(kind, n, top_k):
+    """A stretch of 16384 candidates lists its first top_k, and a row is drawn
+    from its lists where they hold 16384 together; equals across stretches."""
+    logits = kind != "weights"
+    x = scores_for(kind, 2, n, np.random.default_rng(n + top_k))
+    for k, settings in enumerate([dict(), dict(top_p=0.8, temperature=0.7), dict(top_p=0.5, min_p=0.1)]):
+        check_draw(x, 40, logits, dict(settings, top_k=top_k), seed=k, lengths=[n, n - 16383] if k == 1 else None)
+    check_draw(x, 3, logits, dict(temperature=0.0, top_k=top_k))
+    check_draw(x, 5, logits, dict(top_k=top_k), bf16=True, pad=3)
+
+
+def test_draw_best_of_a_huge_row():
+    n = (1 << 28) + 7
+    x = torch.zeros(n, device=DEV)
+    ids = torch.empty(2, dtype=torch.int32, device=DEV)
+    prob = torch.empty(2, device=DEV)
+    u = torch.tensor([0.0, 0.99], dtype=torch.float64, device=DEV)
+    work = gs.alloc_draw_work(1, n, 2, DEV)
+    for at in (0, 16384, (1 << 28) + 2):
+        x[at:at + 3] = 1.0 + at
+        gs.gs_draw(x, u, ids, work, prob=prob, temperature=0.0)
+        assert ids.tolist() == [at, at] and prob.tolist() == [1.0, 1.0]
+
+
 @pytest.mark.parametrize("n,draws", [(70, 6), (600, 6), (5000, 6), (17000, 6), (17000, 260)])
 def test_draw_types_strides_and_lengths(n, draws):
     r = np.random.default_rng(n)
