@@ -368,26 +368,44 @@ __device__ __forceinline__ uint32_t pass_bin(const unsigned long long *hist, uin
 }
 
 // The digits of a workgroup's keys: of key - least, from the one that holds the
-// spread's highest bit (at `first`) on.
+// spread's highest bit (at `first`) on. Keys below `least` have none.
 struct Digits {
     uint32_t least;
     int first;
     // whether the digits above `shift` of a candidate's offset are those of z
     __device__ __forceinline__ bool reach(uint32_t k, uint32_t z, int shift) const {
-        return k != 0 && (shift >= 24 || ((k - least) >> (shift + 8)) == z);
+        return k >= least && (shift >= 24 || ((k - least) >> (shift + 8)) == z);
     }
     __device__ __forceinline__ uint32_t at(uint32_t k, int shift) const { return (k - least) >> shift & 255u; }
 };
 __device__ __forceinline__ Digits digits_of(uint32_t top, uint32_t least) {
-    const uint32_t spread = top ? top - least : 0u;
+    const uint32_t spread = top > least ? top - least : 0u;
     return Digits{least, spread ? (31 - __builtin_clz(spread)) / 8 * 8 : 0};
 }
 
+// A key that at least `want` <= NT candidates of a workgroup reach, given each
+// thread's largest: want / waves of a wave's lanes reach what its top 16 bits
+// are found to be, bit by bit, and every wave that of the least one.
+template <int NT>
+__device__ __forceinline__ uint32_t reached_by(uint32_t mine, uint32_t want, uint64_t *lds) {
+    const uint32_t share = (want + NT / kWave - 1) / (NT / kWave);
+    uint32_t t = 0;
+    for (uint32_t bit = 1u << 31; bit >= 1u << 16; bit >>= 1)
+        if ((uint32_t)__popcll(__ballot(mine >= (t | bit))) >= share) t |= bit;
+    return ~group_max<NT>(~t, lds);
+}
+
 // The first top_k of a workgroup's candidates; all of them if they are no more.
+// top, least: the keys' largest and least; mine: the thread's largest. (Where
+// top_k <= NT, the few candidates that can be among them are found first:
+// scores have few exponents, and adds of all of them to the first digit's bins
+// wait for each other, stretches of 16384 logits, 200 of them: 19 -> 14 us.)
 template <int NT, int ITEMS>
-__device__ __forceinline__ Kept top_kept(const uint32_t key[ITEMS], uint32_t top_k, const Digits &dg,
-                                         unsigned long long *s_hist, uint64_t *lds, uint64_t *s_out) {
+__device__ __forceinline__ Kept top_kept(const uint32_t key[ITEMS], uint32_t mine, uint32_t top_k, uint32_t top,
+                                         uint32_t least, unsigned long long *s_hist, uint64_t *lds, uint64_t *s_out) {
     if (group_sum<NT>(live<ITEMS>(key), lds) <= top_k) return Kept{0, 0xFFFFFFFFu};
+    if (top_k <= NT) least = umax_(least, reached_by<NT>(mine, top_k, lds));
+    const Digits dg = digits_of(top, least);
     uint64_t need = top_k;
     uint32_t z = 0;
     for (int shift = dg.first; shift >= 0; shift -= 8) {
@@ -401,30 +419,136 @@ __device__ __forceinline__ Kept top_kept(const uint32_t key[ITEMS], uint32_t top
         z = z << 8 | pass_bin<NT>(s_hist, need - 1, &above, s_out);
         need -= above;
     }
-    return Kept{dg.least + z, (uint32_t)need};
+    return Kept{least + z, (uint32_t)need};
+}
+
+// The places of a workgroup's kept candidates in their order: put(t, place) for
+// each of them. Returns how many.
+template <int NT, int ITEMS, typename F>
+__device__ __forceinline__ uint32_t place_kept(const uint32_t key[ITEMS], const Kept &kept, uint64_t *lds, F put) {
+    uint32_t mine = 0, total;  // larger: low half, equal: high half
+#pragma unroll
+    for (int t = 0; t < ITEMS; ++t)
+        mine += key[t] > kept.key ? 1u : key[t] && key[t] == kept.key ? 0x10000u : 0u;
+    uint32_t run = group_scan<NT>(mine, lds, &total);
+#pragma unroll
+    for (int t = 0; t < ITEMS; ++t) {
+        const bool up = key[t] > kept.key, tie = key[t] && key[t] == kept.key;
+        const uint32_t equals = run >> 16, place = (run & 0xFFFFu) + (equals < kept.ties ? equals : kept.ties);
+        if (up || (tie && equals < kept.ties)) put(t, place);
+        run += up ? 1u : tie ? 0x10000u : 0u;
+    }
+    const uint32_t ties = total >> 16;
+    return (total & 0xFFFFu) + (ties < kept.ties ? ties : kept.ties);
 }
 
 // Lists of candidates that stand for the rows: keys (0: none) and numbers.
 struct Lists {
     uint32_t *key, *id;  // [rows][stride]
-    int64_t stretch;     // candidates of a row's stretch
     uint32_t stride, stretches, want;  // want: entries of a stretch's list
 };
 
-// Draws from rows of a workgroup. LIST: the rows are lists, a.n entries each.
-template <int NT, int ITEMS, bool LIST>
-__global__ __launch_bounds__(NT) void k_draw_rows(DrawArgs a, Lists lists) {
+// Draws from a row whose candidates the threads of a workgroup hold, in order,
+// after top-k has kept `kept` of them; id(j): the j-th candidate's number. s_run:
+// LDS, NT (ITEMS + 1) entries.
+template <int NT, int ITEMS, typename F>
+__device__ __forceinline__ void draw_from(const DrawArgs &a, int64_t row, const uint32_t key[ITEMS], Kept kept,
+                                          uint32_t top, uint32_t least, uint64_t *s_run, unsigned long long *s_hist,
+                                          uint64_t *lds, uint64_t *s_out, F id) {
+    uint64_t q[ITEMS];
+    const Scale scale = scale_of(a, top);
+    constexpr int kSide = ITEMS < 4 ? ITEMS : 4;
+#pragma unroll
+    for (int t = 0; t < ITEMS; t += kSide) masses_of<kSide>(a, key + t, scale, q + t);
+    if (a.top_p) {
+        // masses of what top-k left: the equals at its end count as far as
+        // they were taken
+        const Digits dg = digits_of(top, umax_(least, kept.key));
+        const uint64_t qk = kept.key ? mass_of(a, kept.key, scale) * kept.ties : 0;
+        uint64_t sum = 0;
+#pragma unroll
+        for (int t = 0; t < ITEMS; ++t) sum += key[t] > kept.key ? q[t] : 0;
+        sum = group_sum<NT>(sum, lds) + qk;
+        uint64_t most = share_of(a.share, sum);
+        uint32_t z = 0;
+        for (int shift = dg.first; shift >= 0; shift -= 8) {
+            __syncthreads();
+            for (uint32_t b = threadIdx.x; b < kSmallBins; b += NT) s_hist[b] = 0;
+            __syncthreads();
+#pragma unroll
+            for (int t = 0; t < ITEMS; ++t)
+                if (key[t] > kept.key && q[t] && dg.reach(key[t], z, shift))
+                    atomicAdd(&s_hist[dg.at(key[t], shift)], (unsigned long long)q[t]);
+            if (qk && threadIdx.x == 0 && dg.reach(kept.key, z, shift))
+                atomicAdd(&s_hist[dg.at(kept.key, shift)], (unsigned long long)qk);
+            uint64_t above;
+            z = z << 8 | pass_bin<NT>(s_hist, most, &above, s_out);
+            most -= above;
+        }
+        const uint32_t k = top ? dg.least + z : 0u;
+        const uint64_t qp = mass_of(a, k, scale);
+        uint64_t ties = qp ? most / qp + 1 : 0;
+        if (k == kept.key && ties > kept.ties) ties = kept.ties;
+        kept = Kept{k, ties < 0xFFFFFFFFu ? (uint32_t)ties : 0xFFFFFFFFu};
+    }
+    if (kept.key) {  // equals of the last key in earlier threads
+        uint32_t mine = 0, all;
+#pragma unroll
+        for (int t = 0; t < ITEMS; ++t) mine += key[t] == kept.key ? 1u : 0u;
+        uint32_t place = group_scan<NT>(mine, lds, &all);
+#pragma unroll
+        for (int t = 0; t < ITEMS; ++t) {
+            if (key[t] < kept.key) q[t] = 0;
+            if (key[t] == kept.key && place++ >= kept.ties) q[t] = 0;
+        }
+    }
+    uint64_t run = 0, total;
+#pragma unroll
+    for (int t = 0; t < ITEMS; ++t) {
+        if ((double)q[t] < a.least) q[t] = 0;
+        run += q[t];
+    }
+    run = group_scan<NT>(run, lds, &total);
     // a thread's entries are followed by an empty one, so that threads do not
     // meet in a bank
-    __shared__ uint64_t s_run[NT * (ITEMS + 1)];
+    constexpr int kApart = ITEMS > 1 ? ITEMS + 1 : 1;
+#pragma unroll
+    for (int t = 0; t < ITEMS; ++t) s_run[threadIdx.x * kApart + t] = run += q[t];
+    __syncthreads();
+    auto run_at = [&](uint32_t j) { return s_run[ITEMS > 1 ? j + j / ITEMS : j]; };
+    for (int64_t d = threadIdx.x; d < a.draws; d += NT) {
+        const int64_t at = row * a.draws + d;
+        const uint64_t r = share_of(uniform_bits(a.uniform[at]), total);
+        uint32_t lo = 0;  // candidates with at most r up to them
+#pragma unroll
+        for (uint32_t step = NT * ITEMS / 2; step > 0; step /= 2)
+            if (run_at(lo + step - 1) <= r) lo += step;
+        if (total == 0)
+            write_draw(a, at, -1, 0, 1);
+        else
+            write_draw(a, at, id(lo), run_at(lo) - (lo ? run_at(lo - 1) : 0), total);
+    }
+    __syncthreads();
+}
+
+// Draws from rows of a workgroup. kList: the rows are lists, a.n entries each,
+// of which a.top_k <= NT stay. kFew: a.top_k <= NT stay of a row; they are put
+// side by side before anything is done about their masses.
+enum { kAll = 0, kFew = 1, kList = 2 };
+constexpr int waves_of(int NT) { return NT == kBlock ? 3 : 4; }  // of a SIMD: registers are held to that
+template <int NT, int ITEMS, int FORM>
+__global__ __launch_bounds__(NT, waves_of(NT)) void k_draw_rows(DrawArgs a, Lists lists) {
+    constexpr int kHeld = FORM == kAll ? ITEMS : 1;  // candidates of a thread that masses are formed of
+    __shared__ uint64_t s_run[NT * (kHeld + 1)];
     __shared__ unsigned long long s_hist[kSmallBins];
     __shared__ uint64_t lds[NT / kWave + 2];
     uint64_t *s_out = lds + NT / kWave;
+    uint32_t *s_key = (uint32_t *)(s_run + NT), *s_id = s_key + NT;  // behind the running masses of one each
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        uint32_t key[ITEMS], top = 0, over = 0;  // over: ~key, for the least
-        uint64_t q[ITEMS];
+        uint32_t key[ITEMS], mine = 0, over = 0;  // the largest, and ~key, for the least
         const uint32_t j0 = threadIdx.x * ITEMS;
-        if (LIST) {
+        const uint32_t *list_id = FORM == kList ? lists.id + row * lists.stride : nullptr;
+        if (FORM == kList) {
 #pragma unroll
             for (int t = 0; t < ITEMS; t += 4) {
                 const uint32_t j = j0 + t, last = lists.stride - 4;
@@ -441,87 +565,30 @@ __global__ __launch_bounds__(NT) void k_draw_rows(DrawArgs a, Lists lists) {
         }
 #pragma unroll
         for (int t = 0; t < ITEMS; ++t) {
-            top = umax_(top, key[t]);
+            mine = umax_(mine, key[t]);
             over = umax_(over, key[t] ? ~key[t] : 0u);
         }
-        top = group_max<NT>(top, lds);
-        const Scale scale = scale_of(a, top);
-#pragma unroll
-        for (int t = 0; t < ITEMS; t += 4) masses_of<4>(a, key + t, scale, q + t);
+        const uint32_t top = group_max<NT>(mine, lds);
+        const bool filters = a.top_k < (uint32_t)a.n || a.top_p;
+        const uint32_t least = filters ? ~group_max<NT>(over, lds) : 0u;
         Kept kept{0, 0xFFFFFFFFu};
-        if (a.form == kBest) {
+        if (a.form == kBest)
             kept = Kept{top, 1};
-        } else if (a.top_k < (uint32_t)a.n || a.top_p) {
-            const Digits dg = digits_of(top, ~group_max<NT>(over, lds));
-            if (a.top_k < (uint32_t)a.n) kept = top_kept<NT, ITEMS>(key, a.top_k, dg, s_hist, lds, s_out);
-            if (a.top_p) {
-                // masses of what top-k left: the equals at its end count as
-                // far as they were taken
-                const uint64_t qk = kept.key ? mass_of(a, kept.key, scale) * kept.ties : 0;
-                uint64_t sum = 0;
-#pragma unroll
-                for (int t = 0; t < ITEMS; ++t) sum += key[t] > kept.key ? q[t] : 0;
-                sum = group_sum<NT>(sum, lds) + qk;
-                uint64_t most = share_of(a.share, sum);
-                uint32_t z = 0;
-                for (int shift = dg.first; shift >= 0; shift -= 8) {
-                    __syncthreads();
-                    for (uint32_t b = threadIdx.x; b < kSmallBins; b += NT) s_hist[b] = 0;
-                    __syncthreads();
-#pragma unroll
-                    for (int t = 0; t < ITEMS; ++t)
-                        if (key[t] > kept.key && q[t] && dg.reach(key[t], z, shift))
-                            atomicAdd(&s_hist[dg.at(key[t], shift)], (unsigned long long)q[t]);
-                    if (qk && threadIdx.x == 0 && dg.reach(kept.key, z, shift))
-                        atomicAdd(&s_hist[dg.at(kept.key, shift)], (unsigned long long)qk);
-                    uint64_t above;
-                    z = z << 8 | pass_bin<NT>(s_hist, most, &above, s_out);
-                    most -= above;
-                }
-                const uint32_t k = top ? dg.least + z : 0u;
-                const uint64_t qp = mass_of(a, k, scale);
-                uint64_t ties = qp ? most / qp + 1 : 0;
-                if (k == kept.key && ties > kept.ties) ties = kept.ties;
-                kept = Kept{k, ties < 0xFFFFFFFFu ? (uint32_t)ties : 0xFFFFFFFFu};
-            }
+        else if (a.top_k < (uint32_t)a.n)
+            kept = top_kept<NT, ITEMS>(key, mine, a.top_k, top, least, s_hist, lds, s_out);
+        if (FORM == kAll) {
+            draw_from<NT, kHeld>(a, row, key, kept, top, least, s_run, s_hist, lds, s_out,
+                                 [&](uint32_t j) { return j; });
+            continue;
         }
-        if (kept.key) {  // equals of the last key in earlier threads
-            uint32_t mine = 0, all;
-#pragma unroll
-            for (int t = 0; t < ITEMS; ++t) mine += key[t] == kept.key ? 1u : 0u;
-            uint32_t place = group_scan<NT>(mine, lds, &all);
-#pragma unroll
-            for (int t = 0; t < ITEMS; ++t) {
-                if (key[t] < kept.key) q[t] = 0;
-                if (key[t] == kept.key && place++ >= kept.ties) q[t] = 0;
-            }
-        }
-        uint64_t run = 0, total;
-#pragma unroll
-        for (int t = 0; t < ITEMS; ++t) {
-            if ((double)q[t] < a.least) q[t] = 0;
-            run += q[t];
-        }
-        run = group_scan<NT>(run, lds, &total);
-#pragma unroll
-        for (int t = 0; t < ITEMS; ++t) s_run[threadIdx.x * (ITEMS + 1) + t] = run += q[t];
+        const uint32_t count = place_kept<NT, ITEMS>(key, kept, lds, [&](int t, uint32_t place) {
+            s_key[place] = key[t];
+            s_id[place] = FORM == kList ? list_id[j0 + t] : j0 + t;
+        });
         __syncthreads();
-        auto run_at = [&](uint32_t j) { return s_run[j + j / ITEMS]; };
-        for (int64_t d = threadIdx.x; d < a.draws; d += NT) {
-            const int64_t at = row * a.draws + d;
-            const uint64_t r = share_of(uniform_bits(a.uniform[at]), total);
-            uint32_t lo = 0;  // candidates with at most r up to them
-#pragma unroll
-            for (uint32_t step = NT * ITEMS / 2; step > 0; step /= 2)
-                if (run_at(lo + step - 1) <= r) lo += step;
-            if (total == 0) {
-                write_draw(a, at, -1, 0, 1);
-            } else {
-                const uint32_t id = LIST ? lists.id[row * lists.stride + lo] : lo;
-                write_draw(a, at, id, run_at(lo) - (lo ? run_at(lo - 1) : 0), total);
-            }
-        }
-        __syncthreads();
+        const uint32_t held[kHeld] = {threadIdx.x < count ? s_key[threadIdx.x] : 0u};
+        draw_from<NT, kHeld>(a, row, held, Kept{0, 0xFFFFFFFFu}, top, umax_(least, kept.key), s_run, s_hist, lds,
+                             s_out, [&](uint32_t j) { return s_id[j]; });
     }
 }
 
@@ -531,42 +598,31 @@ __global__ __launch_bounds__(NT) void k_draw_rows(DrawArgs a, Lists lists) {
 // listed in the order of the row. The first `want` of the row are among those
 // of its stretches.
 constexpr int kListThreads = 1024, kListItems = 16;
+constexpr uint32_t kListStretch = kListThreads * kListItems;
 __global__ __launch_bounds__(kListThreads) void k_draw_list(DrawArgs a, Lists w, uint64_t block0) {
     __shared__ unsigned long long s_hist[kSmallBins];
     __shared__ uint64_t lds[kListThreads / kWave + 2];
     const uint64_t block = block0 + blockIdx.x;
     const int64_t row = (int64_t)(block / w.stretches);
     const uint32_t at = (uint32_t)(block % w.stretches), len = row_length(a, row);
-    const uint32_t i0 = at * (uint32_t)w.stretch, j0 = i0 + threadIdx.x * kListItems;
-    const uint32_t i1 = len <= i0 ? i0 : len - i0 < (uint32_t)w.stretch ? len : i0 + (uint32_t)w.stretch;
-    uint32_t key[kListItems], top = 0, over = 0;
+    const uint32_t i0 = at * kListStretch, j0 = i0 + threadIdx.x * kListItems;
+    const uint32_t i1 = len <= i0 ? i0 : len - i0 < kListStretch ? len : i0 + kListStretch;
+    uint32_t key[kListItems], mine = 0, over = 0;
 #pragma unroll
     for (int t = 0; t < kListItems; t += 4) load_keys(a, row, j0 + t, i1, len, key + t);
 #pragma unroll
     for (int t = 0; t < kListItems; ++t) {
-        top = umax_(top, key[t]);
+        mine = umax_(mine, key[t]);
         over = umax_(over, key[t] ? ~key[t] : 0u);
     }
-    top = group_max<kListThreads>(top, lds);
-    const Digits dg = digits_of(top, ~group_max<kListThreads>(over, lds));
-    const Kept kept = top_kept<kListThreads, kListItems>(key, w.want, dg, s_hist, lds, lds + kListThreads / kWave);
-    uint32_t mine = 0, total;  // larger: low half, equal: high half
-#pragma unroll
-    for (int t = 0; t < kListItems; ++t)
-        mine += key[t] > kept.key ? 1u : key[t] && key[t] == kept.key ? 0x10000u : 0u;
-    uint32_t run = group_scan<kListThreads>(mine, lds, &total);
+    const uint32_t top = group_max<kListThreads>(mine, lds), least = ~group_max<kListThreads>(over, lds);
+    const Kept kept = top_kept<kListThreads, kListItems>(key, mine, w.want, top, least, s_hist, lds,
+                                                         lds + kListThreads / kWave);
     const size_t first = (size_t)row * w.stride + (size_t)at * w.want;
-#pragma unroll
-    for (int t = 0; t < kListItems; ++t) {
-        const bool up = key[t] > kept.key, tie = key[t] && key[t] == kept.key;
-        const uint32_t equals = run >> 16, place = (run & 0xFFFFu) + (equals < kept.ties ? equals : kept.ties);
-        if (up || (tie && equals < kept.ties)) {
-            w.key[first + place] = key[t];
-            w.id[first + place] = j0 + t;
-        }
-        run += up ? 1u : tie ? 0x10000u : 0u;
-    }
-    const uint32_t ties = total >> 16, count = (total & 0xFFFFu) + (ties < kept.ties ? ties : kept.ties);
+    const uint32_t count = place_kept<kListThreads, kListItems>(key, kept, lds, [&](int t, uint32_t place) {
+        w.key[first + place] = key[t];
+        w.id[first + place] = j0 + t;
+    });
     const uint32_t end = at + 1 == w.stretches ? w.stride - at * w.want : w.want;
     for (uint32_t e = count + threadIdx.x; e < end; e += kListThreads) w.key[first + e] = 0;
 }
@@ -1203,9 +1259,9 @@ __global__ __launch_bounds__(kBlock) void k_draw_search(DrawArgs a, LongWork w, 
 }
 
 constexpr int64_t kRowSmall = 512, kRowMiddle = 4096, kRowLarge = 16384;
-// Lists of a row's best are drawn from where all of its stretches' fit in a row
-// of a workgroup.
-constexpr int64_t kListRow = kRowLarge, kListStretch = kListThreads * kListItems;
+// Lists of a row's best are drawn from where they have no more entries than a
+// workgroup has threads, and all of a row's fit into a workgroup.
+constexpr int64_t kListRow = kRowLarge;
 size_t list_bytes(int64_t rows) { return 2 * al256(4 * (size_t)rows * kListRow); }
 constexpr uint64_t kBlocksMost = (uint64_t)1 << 21;  // workgroups of a launch (fewer than 2^32 threads)
 
@@ -1244,30 +1300,42 @@ hipError_t launch_draw(int64_t rows, int64_t n, const void *scores, int64_t stri
     a.share = (uint64_t)(p.top_p * 0x1p53);
     a.top_k = p.top_k > 0 && p.top_k < n && a.form != kBest ? (uint32_t)p.top_k : 0xFFFFFFFFu;
     a.bf16 = p.type == GS_SCORE_BF16;
-    auto draw_rows = [&](const DrawArgs &d, const Lists &l, auto list) {
-        constexpr bool LIST = decltype(list)::value;
-        const uint32_t most = d.n <= kRowSmall ? 1u << 20 : 1u << 16;
-        const dim3 nb(rows < (int64_t)most ? (uint32_t)rows : most);
+    const int64_t want = a.form == kBest ? 1 : a.top_k;
+    auto rows_by = [&](auto threads, auto items, auto form, const DrawArgs &d, const Lists &l) {
+        constexpr int NT = decltype(threads)::value;
+        const int64_t most = (int64_t)1 << (NT == 64 ? 20 : 16);
         prof_begin("draw_rows", s);
-        if (d.n <= kRowSmall)
-            hipLaunchKernelGGL((k_draw_rows<64, 8, LIST>), nb, dim3(64), 0, s, d, l);
-        else if (d.n <= kRowMiddle)
-            hipLaunchKernelGGL((k_draw_rows<256, 16, LIST>), nb, dim3(256), 0, s, d, l);
-        else
-            hipLaunchKernelGGL((k_draw_rows<1024, 16, LIST>), nb, dim3(1024), 0, s, d, l);
+        hipLaunchKernelGGL((k_draw_rows<NT, decltype(items)::value, decltype(form)::value>),
+                           dim3((uint32_t)(rows < most ? rows : most)), dim3(NT), 0, s, d, l);
         prof_end("draw_rows", s);
         return hipGetLastError();
     };
-    if (n <= kRowLarge) return draw_rows(a, Lists{}, std::false_type());
+    using I4 = std::integral_constant<int, 4>;
+    using I8 = std::integral_constant<int, 8>;
+    using I16 = std::integral_constant<int, 16>;
+    using T64 = std::integral_constant<int, 64>;
+    using T256 = std::integral_constant<int, 256>;
+    using T1024 = std::integral_constant<int, 1024>;
+    using All = std::integral_constant<int, kAll>;
+    using Few = std::integral_constant<int, kFew>;
+    using List = std::integral_constant<int, kList>;
+    if (n <= kRowLarge) {
+        if (want >= n) a.top_k = 0xFFFFFFFFu;
+        else a.top_k = (uint32_t)want;
+        if (n <= kRowSmall)
+            return want <= 64 && want < n ? rows_by(T64(), I8(), Few(), a, Lists{}) : rows_by(T64(), I8(), All(), a, Lists{});
+        if (n <= kRowMiddle)
+            return want <= 256 ? rows_by(T256(), I16(), Few(), a, Lists{}) : rows_by(T256(), I16(), All(), a, Lists{});
+        return want <= 1024 ? rows_by(T1024(), I16(), Few(), a, Lists{}) : rows_by(T1024(), I16(), All(), a, Lists{});
+    }
     auto over = [](uint64_t blocks, auto launch) {
         for (uint64_t b = 0; b < blocks; b += kBlocksMost)
             launch(dim3((uint32_t)(blocks - b < kBlocksMost ? blocks - b : kBlocksMost)), b);
     };
-    const int64_t stretches = (n + kListStretch - 1) / kListStretch, want = a.form == kBest ? 1 : a.top_k;
-    if (stretches * want <= kListRow) {
+    const int64_t stretches = (n + kListStretch - 1) / kListStretch;
+    if (want <= kListThreads && stretches * want <= kListRow) {
         Lists l;
         l.stretches = (uint32_t)stretches;
-        l.stretch = ((n + stretches - 1) / stretches + 3) / 4 * 4;
         l.want = (uint32_t)want;
         l.stride = (uint32_t)(stretches * want + 3) / 4 * 4;
         l.key = (uint32_t *)work;
@@ -1279,7 +1347,10 @@ hipError_t launch_draw(int64_t rows, int64_t n, const void *scores, int64_t stri
         prof_end("draw_list", s);
         DrawArgs d = a;
         d.n = stretches * want;
-        return draw_rows(d, l, std::true_type());
+        d.top_k = (uint32_t)want;
+        if (d.n <= 1024 && want <= 256) return rows_by(T256(), I4(), List(), d, l);
+        if (d.n <= 4096) return rows_by(T1024(), I4(), List(), d, l);
+        return rows_by(T1024(), I16(), List(), d, l);
     }
     const LongWork w = long_layout(work, rows, n);
     const uint64_t blocks = (uint64_t)rows * w.stretches, parts = (uint64_t)rows * w.parts;

@@ -437,6 +437,24 @@ def test_draw_few_of_long_rows(kind, n, top_k):
     check_draw(x, 5, logits, dict(top_k=top_k), bf16=True, pad=3)
 
 
+@pytest.mark.parametrize("order", ["none", "rising", "falling", "late"])
+@pytest.mark.parametrize("n,ks", [(500, (63, 64, 65, 499, 500)), (4000, (200, 256, 257)), (16000, (1, 1024, 1025)),
+                                  (40000, (64, 1024, 1025, 5461))])
+def test_draw_top_k_around_a_workgroup(order, n, ks):
+    """As many candidates as a workgroup's threads, one less and one more;
+    sorted rows, and rows whose candidates stand in the last threads."""
+    r = np.random.default_rng(n)
+    x = scores_for("logits", 2, n, r)
+    if order == "late":
+        x[:, : n - n // 7] = -np.inf
+    elif order != "none":
+        x = np.sort(x, axis=1)[:, :: 1 if order == "rising" else -1].copy()
+    for k in ks:
+        check_draw(x, 30, True, dict(top_k=k), seed=k)
+        check_draw(x, 30, True, dict(top_k=k, top_p=0.7, min_p=0.01, temperature=1.5), seed=k)
+        check_draw(np.round(x), 30, True, dict(top_k=k, top_p=0.9, temperature=2.0), seed=k)
+
+
 def test_draw_best_of_a_huge_row():
     n = (1 << 28) + 7
     x = torch.zeros(n, device=DEV)
