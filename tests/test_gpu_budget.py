@@ -424,11 +424,11 @@ def test_draw_very_long_rows(settings):
 
 
 @pytest.mark.parametrize("kind", ["weights", "tied_logits", "odd_logits", "infinite"])
-@pytest.mark.parametrize("n,top_k", [(16385, 1), (16385, 8192), (16385, 8193), (50021, 200), (49155, 4096),
-                                     (49155, 4097), (200003, 1260), (200003, 1261), (200003, 130), (999983, 17)])
+@pytest.mark.parametrize("n,top_k", [(16385, 1), (16385, 1024), (16385, 8193), (50021, 200), (50021, 1024),
+                                     (50021, 1025), (278529, 910), (278529, 911), (200003, 130), (999983, 17)])
 def test_draw_few_of_long_rows(kind, n, top_k):
-    """A stretch of 16384 candidates lists its first top_k, and a row is drawn
-    from its lists where they hold 16384 together; equals across stretches."""
+    """A stretch of 16384 candidates lists its first top_k <= 1024, and a row is
+    drawn from its lists where they hold 16384 together; equals across stretches."""
     logits = kind != "weights"
     x = scores_for(kind, 2, n, np.random.default_rng(n + top_k))
     for k, settings in enumerate([dict(), dict(top_p=0.8, temperature=0.7), dict(top_p=0.5, min_p=0.1)]):
