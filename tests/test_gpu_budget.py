@@ -751,3 +751,52 @@ def test_budget_calls_in_a_graph(n_long):
     calls(stream=side)  # named, not current
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, outs()))
+
+
+def test_large_budget_calls_in_a_graph():
+    """The same with sets, rows and Gaussians that take several launches."""
+    n, keep = 40000, 30000
+    g = synth.random_gaussians(43, n, log_mu=math.log(0.01))
+    g.scale[11] = (0.5, 0.4, 0.6)
+    batches = {"points": Batch(g, "points", (16, 16, 16), n=70001, seed=1),
+               "jitter": Batch(g, "jitter", (16, 16, 16), (42, 43, 44), seed=2),
+               "grid": Batch(g, "grid", (16, 16, 16), (48, 48, 48), seed=3)}
+    p, q = param_set(n, 3), gs.ParamSet.empty(n, DEV)
+    score = {k: torch.zeros(n, device=DEV) for k in batches}
+    source, kept = torch.empty(n, dtype=torch.int32, device=DEV), torch.empty(n, device=DEV)
+    pinned = torch.zeros(n, dtype=torch.uint8, device=DEV)
+    pinned[::37] = 1
+    uniform = torch.rand(n - keep, dtype=torch.float64, device=DEV)
+    ids, few = (torch.empty(n - keep, dtype=torch.int32, device=DEV) for _ in range(2))
+    best = torch.empty(1, dtype=torch.int32, device=DEV)
+    works = (gs.alloc_evict_work(n, DEV), gs.alloc_draw_work(1, keep, n - keep, DEV), gs.alloc_split_work(keep, DEV))
+
+    def calls():
+        for k, b in batches.items():
+            b.shares(score[k], decay=0.5)
+        gs.gs_evict(p, n, score["points"], keep, q, source, works[0], pinned=pinned, score_out=kept)
+        gs.gs_draw(kept[:keep], uniform, ids, works[1], top_k=20000, top_p=0.8)
+        gs.gs_draw(kept[:keep], uniform, few, works[1], top_k=100, top_p=0.8, temperature=0.5)
+        gs.gs_draw(kept[:keep], uniform[:1], best, works[1], temperature=0.0)
+        gs.gs_split(q, keep, ids, source, works[2], score=kept)
+
+    outs = lambda: [x.clone() for x in (*score.values(), kept, source, ids, few, best, q.mean, q.weight_logit)]  # noqa: E731
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for turn in range(4):
+        uniform.copy_(torch.rand_like(uniform))
+        start = {k: torch.rand(n, device=DEV) for k in score}
+        for k in score:
+            score[k].copy_(start[k])
+        calls()
+        want = outs()
+        for x in (kept, source, ids, few, best, q.mean, q.weight_logit):
+            x.fill_(1)
+        for k in score:
+            score[k].copy_(start[k])
+        torch.cuda.synchronize()
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(want, outs())), turn
+        if turn == 1:
+            torch.cuda.synchronize()
