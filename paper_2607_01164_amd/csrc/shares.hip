@@ -9,7 +9,7 @@
 // are added at a Gaussian's end: no atomics, an order fixed by the inputs. The
 // bound is the arithmetic over the pairs of the rows, of which the cutoff
 // keeps a fourth to a third: a 128^3 jittered grid and 131072 Gaussians, 123
-// million pairs, 174 us with the vector units busy for 74 of 100 cycles. (A
+// million pairs, 168 us with the vector units busy for 74 of 100 cycles. (A
 // lane a row, each with its own record: 583 us.)
 #include <type_traits>
 
@@ -234,6 +234,7 @@ __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32
     left = 0;
     // lane i < nk describes Gaussian i of the wave: its rows
     uint32_t mR = 0, mnx = 0, mny = 1, mx = 0, my = 0, mz = 0;
+    VoxelReach mreach{0.0f, 0.0f};
     if (lane < nk) {
         const CellBox b = a.box[mgid];
         if (b.hi.x >= b.lo.x && a.q.n > 0) {
@@ -246,9 +247,11 @@ __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32
                 mz = r.z0;
                 mR = r.ny * r.nz;
             } else if (voxels) {
+                const Record r = a.rec[mgid];
                 uint32_t nz;
-                voxel_rows(a.rec[mgid], a.q, a.g, a.bg, my, mny, mz, nz);
+                voxel_rows(r, a.q, a.g, a.bg, my, mny, mz, nz);
                 mR = mny * nz;
+                mreach = voxel_reach(r, a.q, a.bg);
             } else {
                 mx = (uint32_t)b.lo.x;
                 mnx = (uint32_t)(b.hi.x - b.lo.x + 1);
@@ -291,6 +294,11 @@ __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32
         auto perm = [&](uint32_t v) { return (uint32_t)__builtin_amdgcn_ds_bpermute((int)src, (int)v); };
         const uint32_t gid = perm(mgid), end = perm(mRend), R = perm(mR), nx = perm(mnx), ny = perm(mny);
         const uint32_t x0 = perm(mx), y0 = perm(my), z0 = perm(mz);
+        VoxelReach reach{0.0f, 0.0f};
+        if (voxels) {
+            reach.reach = __uint_as_float(perm(__float_as_uint(mreach.reach)));
+            reach.shift = __uint_as_float(perm(__float_as_uint(mreach.shift)));
+        }
         uint32_t start = 0, len = 0, vx = 0;
         float py = 0.0f, pz = 0.0f;
         if (gr < Rw) {
@@ -301,7 +309,7 @@ __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32
             if (WALK == kWalkGrid)
                 len = grid_row(r, x0, nx, vy, vz, a.q, a.g, a.bg, vx, py, pz);
             else if (voxels)
-                len = voxel_row(r, voxel_reach(r, a.q, a.bg), vy, vz, a.q, a.g, a.bg, vx);
+                len = voxel_row(r, reach, vy, vz, a.q, a.g, a.bg, vx);
             else
                 len = plan_row(r, x0, nx, vy, vz, a.g, a.bg, a.point_off, start);
             if (WALK == kWalkGrid || voxels)
