@@ -367,20 +367,25 @@ __device__ __forceinline__ uint32_t pass_bin(const unsigned long long *hist, uin
     return (uint32_t)out[0];
 }
 
-// The digits of a workgroup's keys: of key - least, from the one that holds the
-// spread's highest bit (at `first`) on. Keys below `least` have none.
+// The digits of a workgroup's keys: of key - least, moved up so that the spread
+// fills 32 bits and the first digit its bins (few of them would be met by most
+// candidates, which wait for each other there). Keys below `least` have none.
 struct Digits {
     uint32_t least;
-    int first;
+    int lift;
+    // whether the digit at `shift` tells anything
+    __device__ __forceinline__ bool more(int shift) const { return shift + 8 > lift; }
     // whether the digits above `shift` of a candidate's offset are those of z
     __device__ __forceinline__ bool reach(uint32_t k, uint32_t z, int shift) const {
-        return k >= least && (shift >= 24 || ((k - least) >> (shift + 8)) == z);
+        return k >= least && (shift >= 24 || ((k - least) << lift >> (shift + 8)) == z);
     }
-    __device__ __forceinline__ uint32_t at(uint32_t k, int shift) const { return (k - least) >> shift & 255u; }
+    __device__ __forceinline__ uint32_t at(uint32_t k, int shift) const { return (k - least) << lift >> shift & 255u; }
+    // the key of the digits z down to the one at `shift`
+    __device__ __forceinline__ uint32_t key(uint32_t z, int shift) const { return least + (z << shift >> lift); }
 };
 __device__ __forceinline__ Digits digits_of(uint32_t top, uint32_t least) {
     const uint32_t spread = top > least ? top - least : 0u;
-    return Digits{least, spread ? (31 - __builtin_clz(spread)) / 8 * 8 : 0};
+    return Digits{least, __builtin_clz(spread | 1u)};
 }
 
 // A key that at least `want` <= NT candidates of a workgroup reach, given each
@@ -408,7 +413,8 @@ __device__ __forceinline__ Kept top_kept(const uint32_t key[ITEMS], uint32_t min
     const Digits dg = digits_of(top, least);
     uint64_t need = top_k;
     uint32_t z = 0;
-    for (int shift = dg.first; shift >= 0; shift -= 8) {
+    int shift = 24;
+    for (; dg.more(shift); shift -= 8) {
         __syncthreads();
         for (uint32_t b = threadIdx.x; b < kSmallBins; b += NT) s_hist[b] = 0;
         __syncthreads();
@@ -419,7 +425,7 @@ __device__ __forceinline__ Kept top_kept(const uint32_t key[ITEMS], uint32_t min
         z = z << 8 | pass_bin<NT>(s_hist, need - 1, &above, s_out);
         need -= above;
     }
-    return Kept{least + z, (uint32_t)need};
+    return Kept{dg.key(z, shift + 8), (uint32_t)need};
 }
 
 // The places of a workgroup's kept candidates in their order: put(t, place) for
@@ -471,7 +477,8 @@ __device__ __forceinline__ void draw_from(const DrawArgs &a, int64_t row, const 
         sum = group_sum<NT>(sum, lds) + qk;
         uint64_t most = share_of(a.share, sum);
         uint32_t z = 0;
-        for (int shift = dg.first; shift >= 0; shift -= 8) {
+        int shift = 24;
+        for (; dg.more(shift); shift -= 8) {
             __syncthreads();
             for (uint32_t b = threadIdx.x; b < kSmallBins; b += NT) s_hist[b] = 0;
             __syncthreads();
@@ -485,7 +492,7 @@ __device__ __forceinline__ void draw_from(const DrawArgs &a, int64_t row, const 
             z = z << 8 | pass_bin<NT>(s_hist, most, &above, s_out);
             most -= above;
         }
-        const uint32_t k = top ? dg.least + z : 0u;
+        const uint32_t k = top ? dg.key(z, shift + 8) : 0u;
         const uint64_t qp = mass_of(a, k, scale);
         uint64_t ties = qp ? most / qp + 1 : 0;
         if (k == kept.key && ties > kept.ties) ties = kept.ties;
