@@ -5,7 +5,9 @@
 // (pinned, then the score's bits made monotone), whose budget-th largest value
 // three counting passes over the scores find digit by digit; what lies above
 // it stays, and as many of its equals, by index, as the budget leaves. Bound
-// by the rows of the kept ones, read and written once.
+// by the rows of the kept ones, read and written once: half of 2 M Gaussians
+// moves 173 MB (lines of which half is kept) in 36 us, after five launches of 5
+// to 8 us for the scores and counts; smaller sets by their six launches.
 #include <type_traits>
 
 #include "budget.h"
@@ -373,7 +375,9 @@ __global__ __launch_bounds__(kBlock) void k_evict_rows(int64_t keep, gs_params i
 // Copies. Counting the draws of a Gaussian touches only those drawn: their
 // counts are cleared, then raised by integer atomics (any order gives the
 // same), then every copy works out the shared weight from the logit that it
-// took along; the copies of one Gaussian write the same number to it.
+// took along; the copies of one Gaussian write the same number to it. Bound by
+// the random lines that rows are read from: 419430 copies out of 2 M Gaussians
+// read 314 MB for their 20 MB in 53 us, the shared weights take 18.
 // Below one draw in so many Gaussians only the drawn ones' counts are cleared
 // (2 M Gaussians: all of them 4 us, 419430 draws' one by one 10 us).
 constexpr int64_t kClearAll = 16;
