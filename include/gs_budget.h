@@ -43,7 +43,7 @@ size_t gs_shares_work_bytes(const gs_index *index, const gs_query *query);
  * gs_sample_planned) filled for this index and query; influence is read from
  * the caller's array, not from the plan. gauss must be the Gaussians that the
  * index was built from, unchanged. decay = 0 overwrites score without reading
- * it (0 <= decay, finite).
+ * it (0 <= decay, finite). score overlaps no input.
  * The sums are float32, in an order that the inputs alone fix. Pairs whose Q
  * is so near the cutoff that float32 cannot tell are decided in float64 from
  * gauss (the sampler decides them in float32: of a pair that the two take
@@ -112,7 +112,8 @@ size_t gs_draw_work_bytes(int64_t rows, int64_t n, int64_t draws);
  * and prob (null: not wanted) q_j / M. All sums are exact, so the draws do
  * not depend on how the work is cut. temperature 0 draws the first of the
  * largest scores, with prob 1. A row in which nothing can be drawn (no
- * candidates, or none with mass) gives id -1 and prob 0.
+ * candidates, or none with mass) gives id -1 and prob 0. ids and prob overlap
+ * no input.
  * 0 <= rows, n < 2^31, 0 <= draws < 2^31, rows n and rows draws below 2^40.
  */
 gs_status gs_draw(int64_t rows, int64_t n, const void *scores, int64_t stride, const int32_t *lengths,
@@ -135,7 +136,7 @@ size_t gs_split_work_bytes(int64_t n);
  * An id outside [0, n) makes a Gaussian that contributes nothing: its mean is
  * NaN, its log-scale 0, its rotation (1, 0, 0, 0), its value logit 0, its
  * weight logit -infinity, its score 0, and source is -1 - id (-1 for a negative
- * id). n + count < 2^31. ids, source and score overlap none of the set.
+ * id). n + count < 2^31. ids, source, score and the set do not overlap.
  */
 gs_status gs_split(const gs_params *set, int64_t n, const int32_t *ids, int64_t count, int32_t *source, float *score,
                    void *work, size_t work_bytes, hipStream_t stream);

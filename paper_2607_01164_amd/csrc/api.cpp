@@ -582,6 +582,24 @@ gs_status check_adamw(const char *who, const gs_adamw_plan *plan, const gs_adamw
     return GS_OK;
 }
 
+// Memory that a call reads or writes.
+struct Span {
+    const void *p;
+    size_t bytes;
+};
+bool overlap(const Span &a, const Span &b) {
+    return a.p && b.p && a.bytes && b.bytes && (uintptr_t)a.p < (uintptr_t)b.p + b.bytes &&
+           (uintptr_t)b.p < (uintptr_t)a.p + a.bytes;
+}
+template <size_t N, size_t M>
+bool overlap(const Span (&a)[N], const Span (&b)[M]) {
+    for (const Span &x : a)
+        for (const Span &y : b)
+            if (overlap(x, y)) return true;
+    return false;
+}
+Span floats(const float *p, int64_t n) { return Span{p, sizeof(float) * (size_t)n}; }
+
 }  // namespace
 
 extern "C" {
@@ -1238,6 +1256,10 @@ gs_status gs_shares(const gs_gaussians *gauss, const gs_index *index, const gs_q
             return fail(GS_ERR_WORKSPACE, "gs_shares: plan needs %zu bytes (got %zu)", need, plan_bytes);
         p = plan_layout(const_cast<void *>(plan), nq, gp.ncells);
     }
+    const Span read[] = {floats(gauss->mean, 3 * n), floats(gauss->scale, 3 * n), floats(gauss->rot, 4 * n),
+                         floats(influence, nq), floats(gain, nq)};
+    const Span written[] = {floats(score, n)};
+    if (overlap(read, written)) return fail(GS_ERR_INVALID_ARGUMENT, "gs_shares: score overlaps an input");
     const IndexWork w = index_layout(index->work, n, &index->grid, index->capacity);
     const float T = cutoff_T(index->tau);
     const SharesExact exact{gauss->mean, gauss->scale, gauss->rot, 2.0 * std::log(1.0 / (double)index->tau)};
@@ -1267,6 +1289,13 @@ gs_status gs_evict(const gs_params *in, int64_t n, const float *score, const uin
     if (!work || work_bytes < need || !aligned(work))
         return fail(GS_ERR_WORKSPACE, "gs_evict: workspace needs %zu bytes, 256-byte aligned (got %zu)", need,
                     work_bytes);
+    const Span read[] = {floats(in->mean, 3 * n), floats(in->log_scale, 3 * n), floats(in->rot, 4 * n),
+                         floats(in->value_logit, n), floats(in->weight_logit, n), floats(score, n),
+                         Span{pinned, (size_t)n}};
+    const Span written[] = {floats(out->mean, 3 * keep), floats(out->log_scale, 3 * keep), floats(out->rot, 4 * keep),
+                            floats(out->value_logit, keep), floats(out->weight_logit, keep),
+                            Span{source, sizeof(int32_t) * (size_t)keep}, floats(score_out, keep)};
+    if (overlap(read, written)) return fail(GS_ERR_INVALID_ARGUMENT, "gs_evict: an output overlaps an input");
     GS_TRY(launch_evict(*in, n, score, pinned, keep, *out, source, score_out, work, stream), "gs_evict");
     return GS_OK;
 }
@@ -1303,6 +1332,11 @@ gs_status gs_draw(int64_t rows, int64_t n, const void *scores, int64_t stride, c
     if (!work || work_bytes < need || !aligned(work))
         return fail(GS_ERR_WORKSPACE, "gs_draw: workspace needs %zu bytes, 256-byte aligned (got %zu)", need,
                     work_bytes);
+    const size_t size = p.type == GS_SCORE_BF16 ? 2 : 4, total = (size_t)rows * (size_t)draws;
+    const Span read[] = {Span{scores, size * (size_t)((rows - 1) * stride + n)}, Span{uniform, sizeof(double) * total},
+                         Span{lengths, sizeof(int32_t) * (size_t)rows}};
+    const Span written[] = {Span{ids, sizeof(int32_t) * total}, Span{prob, sizeof(float) * total}};
+    if (overlap(read, written)) return fail(GS_ERR_INVALID_ARGUMENT, "gs_draw: an output overlaps an input");
     GS_TRY(launch_draw(rows, n, scores, stride, lengths, p, draws, uniform, ids, prob, work, stream), "gs_draw");
     return GS_OK;
 }
@@ -1321,6 +1355,13 @@ gs_status gs_split(const gs_params *set, int64_t n, const int32_t *ids, int64_t 
     if (!work || work_bytes < need || !aligned(work))
         return fail(GS_ERR_WORKSPACE, "gs_split: workspace needs %zu bytes, 256-byte aligned (got %zu)", need,
                     work_bytes);
+    const int64_t all = n + count;
+    const Span rows[] = {floats(set->mean, 3 * all), floats(set->log_scale, 3 * all), floats(set->rot, 4 * all),
+                         floats(set->value_logit, all), floats(set->weight_logit, all)};
+    const Span read[] = {Span{ids, sizeof(int32_t) * (size_t)count}};
+    const Span written[] = {Span{source, sizeof(int32_t) * (size_t)all}, floats(score, all)};
+    if (overlap(rows, read) || overlap(rows, written) || overlap(read, written) || overlap(written[0], written[1]))
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_split: ids, source, score and the set overlap");
     GS_TRY(launch_split(*set, n, ids, count, source, score, (uint32_t *)work, stream), "gs_split");
     return GS_OK;
 }

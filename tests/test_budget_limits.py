@@ -165,3 +165,52 @@ def test_binding_refuses_host_tensors():
         gs.gs_split(p, 5, i, None, w)
     with pytest.raises(ValueError, match="ids"):
         gs.gs_split(p, 4, i, None, w)
+
+
+def apart(first, step=1 << 16):
+    """Addresses that no array here reaches from one to the next."""
+    return [first + k * step for k in range(5)]
+
+
+def test_overlapping_arrays_are_refused():
+    """Outputs on inputs, at their ends too: the kernels read rows after others
+    have written."""
+    L, byref = gs.load_library(), ctypes.byref
+    i, o = gsq.GsParams(*apart(1 << 20)), gsq.GsParams(*apart(1 << 24))
+    far = [1 << 26, (1 << 26) + 4096, (1 << 26) + 8192]  # score, source, score_out
+
+    def evict_at(out=o, score=far[0], pinned=None, source=far[1], score_out=far[2]):
+        return err(L.gs_evict(byref(i), 10, score, pinned, 5, byref(out), source, score_out, FAKE, BIG, None))
+
+    for args in (dict(out=i), dict(source=far[0]), dict(score_out=far[0] + 36), dict(score_out=far[0] - 16),
+                 dict(pinned=far[1] + 19), dict(source=i.rot + 156), dict(source=i.weight_logit - 16)):
+        st, msg = evict_at(**args)
+        assert st == 1 and "overlaps" in msg, args
+
+    p = gsq.GsDrawParams(1.0, 1.0, 0.0, 0, 0, gs.GS_SCORE_BF16)
+
+    def draw_at(scores=1 << 20, lengths=None, uniform=1 << 22, ids=1 << 24, prob=1 << 26):
+        return err(L.gs_draw(3, 100, scores, 120, lengths, byref(p), 4, uniform, ids, prob, FAKE, BIG, None))
+
+    for args in (dict(ids=(1 << 20) + 676), dict(ids=(1 << 20) - 44), dict(prob=(1 << 22) + 92), dict(uniform=1 << 24),
+                 dict(lengths=(1 << 26) + 44)):
+        st, msg = draw_at(**args)
+        assert st == 1 and "overlaps" in msg, args
+
+    def split_at(ids=far[0], source=far[1], score=far[2]):
+        return err(L.gs_split(byref(o), 10, ids, 6, source, score, FAKE, BIG, None))
+
+    for args in (dict(ids=far[1] + 40), dict(ids=far[1] + 60), dict(ids=far[2]), dict(source=far[2] + 60),
+                 dict(ids=o.mean + 188), dict(source=o.value_logit), dict(score=o.weight_logit + 60)):
+        st, msg = split_at(**args)
+        assert st == 1 and "overlap" in msg, args
+
+    g = gsq.GsGaussians(10, *apart(1 << 20))
+    ix, q = index(), query()
+
+    def shares_at(influence=1 << 24, gain=1 << 25, score=1 << 26):
+        return err(L.gs_shares(byref(g), byref(ix), byref(q), FAKE, BIG, influence, gain, 0.0, score, FAKE, BIG, None))
+
+    for args in (dict(score=(1 << 24) + 396), dict(score=(1 << 25) - 36), dict(score=g.mean + 116), dict(score=g.rot)):
+        st, msg = shares_at(**args)
+        assert st == 1 and "overlaps" in msg, args
