@@ -113,7 +113,9 @@ size_t gs_draw_work_bytes(int64_t rows, int64_t n, int64_t draws);
  * not depend on how the work is cut. temperature 0 draws the first of the
  * largest scores, with prob 1. A row in which nothing can be drawn (no
  * candidates, or none with mass) gives id -1 and prob 0. ids and prob overlap
- * no input.
+ * no input. Numbers in rising order draw ids in rising order, which reads
+ * memory line by line, here and where gs_split copies what was drawn (419430
+ * of 2 M Gaussians: 65 -> 55 us and 78 -> 37).
  * 0 <= rows, n < 2^31, 0 <= draws < 2^31, rows n and rows draws below 2^40.
  */
 gs_status gs_draw(int64_t rows, int64_t n, const void *scores, int64_t stride, const int32_t *lengths,

@@ -1114,7 +1114,8 @@ def gs_draw(scores: torch.Tensor, uniform: torch.Tensor, ids: torch.Tensor, work
     scores [rows, n] or [n], float32 or bfloat16, weights (or logits), with
     candidates of a row next to each other and any distance between rows;
     uniform [rows, draws] or [draws], float64 in [0, 1). Writes ids (int32, -1:
-    nothing to draw) and the candidates' probabilities."""
+    nothing to draw) and the candidates' probabilities. Rising numbers give
+    rising ids, which are drawn and copied faster."""
     if scores.dim() == 1:
         rows, n, stride = 1, scores.numel(), scores.numel()
         draws = uniform.numel()
