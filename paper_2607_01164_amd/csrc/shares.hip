@@ -9,7 +9,7 @@
 // are added at a Gaussian's end: no atomics, an order fixed by the inputs. The
 // bound is the arithmetic over the pairs of the rows, of which the cutoff
 // keeps a fourth to a third: a 128^3 jittered grid and 131072 Gaussians, 123
-// million pairs, 168 us with the vector units busy for 74 of 100 cycles. (A
+// million pairs, 156 us. (A
 // lane a row, each with its own record: 583 us.)
 #include <type_traits>
 
@@ -152,6 +152,12 @@ struct SharesArgs {
     uint64_t wave0;  // the launch's first wave
 };
 
+// A grid's voxel: its number in x, its centre's y and z.
+struct Voxel {
+    uint32_t x;
+    float y, z;
+};
+
 // The voxels of a jittered grid that a Gaussian can reach: a row (y, z) of
 // voxels holds points of the slab [y, y + 1] x [z, z + 1]. With e the part of
 // u = U d that depends on y and z alone, |e| over the slab is at least its value
@@ -226,7 +232,7 @@ constexpr uint32_t kEntries = kPieces * kWave + kAhead * 16;  // the last steps 
 // share. LEAVE: Gaussians of too many steps are left out, in `left` by bit.
 template <int WALK, bool LEAVE>
 __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32_t nk, uint32_t part, uint32_t parts,
-                                      uint32_t &left, uint2 *s_row, uint4 *s_grid) {
+                                      uint32_t &left, uint2 *s_row, float2 *s_yz, uint32_t *s_x) {
     const uint32_t lane = threadIdx.x % kWave;
     const float T = a.T;
     // positions that leave their voxels: the plan's rows, through its order
@@ -326,7 +332,10 @@ __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32
         for (uint32_t k = 0; k < pieces; ++k) {
             const uint32_t at = upto - pieces + k, from = k << shift;
             s_row[at] = make_uint2(start + from, whole ? len : len - from);
-            if (WALK == kWalkGrid) s_grid[at] = make_uint4(vx + from, __float_as_uint(py), __float_as_uint(pz), 0);
+            if (WALK == kWalkGrid) {
+                s_yz[at] = make_float2(py, pz);
+                s_x[at] = vx + from;
+            }
         }
         __builtin_amdgcn_wave_barrier();
         const uint32_t limit = whole ? 0u : kStepsMost << (6u - shift);  // pieces of so many steps
@@ -356,7 +365,7 @@ __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32
             if (LEAVE && skip) continue;
             // kAhead queries of a lane: query k[u] if on[u], at voxel x[u] of
             // its row in grids
-            auto add = [&](const uint32_t k[kAhead], const bool on[kAhead], const uint4 v[kAhead]) {
+            auto add = [&](const uint32_t k[kAhead], const bool on[kAhead], const Voxel v[kAhead]) {
                 float px[kAhead], py[kAhead], pz[kAhead], f[kAhead];
 #pragma unroll
                 for (uint32_t u = 0; u < kAhead; ++u) {
@@ -377,8 +386,8 @@ __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32
                 for (uint32_t u = 0; u < kAhead; ++u) {
                     if (WALK == kWalkGrid) {
                         px[u] = a.g.lo[0] + ((float)v[u].x + 0.5f) * a.q.vsz[0];
-                        py[u] = __uint_as_float(v[u].y);
-                        pz[u] = __uint_as_float(v[u].z);
+                        py[u] = v[u].y;
+                        pz[u] = v[u].z;
                     }
                     const float Q = record_q(c, px[u], py[u], pz[u]);
                     in[u] = on[u] && Q <= T;
@@ -399,7 +408,7 @@ __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32
                 for (uint32_t r0 = ra + sub * kAhead * rows; r0 < rz; r0 += subs * kAhead * rows) {
                     uint32_t k[kAhead];
                     bool on[kAhead];
-                    uint4 v[kAhead] = {};
+                    Voxel v[kAhead] = {};
 #pragma unroll
                     for (uint32_t u = 0; u < kAhead; ++u) {
                         const uint32_t row = r0 + u * rows + own;
@@ -407,8 +416,8 @@ __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32
                         on[u] = row < rz && mine < w.y;
                         k[u] = w.x + mine;
                         if (WALK == kWalkGrid) {
-                            v[u] = s_grid[row];
-                            v[u].x += mine;
+                            const float2 yz = s_yz[row];
+                            v[u] = Voxel{s_x[row] + mine, yz.x, yz.y};
                         }
                     }
                     add(k, on, v);
@@ -416,18 +425,22 @@ __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32
             } else {
                 for (uint32_t row = ra; row < rz; ++row) {
                     const uint2 w = s_row[row];
-                    uint4 g = make_uint4(0, 0, 0, 0);
-                    if (WALK == kWalkGrid) g = s_grid[row];
+                    uint32_t x0 = 0;
+                    float2 yz = make_float2(0.0f, 0.0f);
+                    if (WALK == kWalkGrid) {
+                        x0 = s_x[row];
+                        yz = s_yz[row];
+                    }
                     for (uint32_t e0 = sub * kAhead * kWave; e0 < w.y; e0 += subs * kAhead * kWave) {
                         uint32_t k[kAhead];
                         bool on[kAhead];
-                        uint4 v[kAhead];
+                        Voxel v[kAhead];
 #pragma unroll
                         for (uint32_t u = 0; u < kAhead; ++u) {
                             const uint32_t e = e0 + u * kWave + lane;
                             on[u] = e < w.y;
                             k[u] = w.x + e;
-                            v[u] = make_uint4(g.x + e, g.y, g.z, 0);
+                            v[u] = Voxel{x0 + e, yz.x, yz.y};
                         }
                         add(k, on, v);
                     }
@@ -444,17 +457,22 @@ __device__ __forceinline__ void add_score(const SharesArgs &a, uint32_t gid, flo
     a.score[gid] = a.decay > 0.0f ? fmaf_(a.decay, a.score[gid], add) : add;
 }
 
+// Waves of a SIMD, to which registers are held: waits for loads and LDS are
+// filled by other waves (6, then 7 or 8 of them: a jittered 128^3 grid 167 -> 156
+// us, 2 M points 172 -> 155; grids lose by it, 120 -> 124 us).
+constexpr int waves_of(int walk) { return walk == kWalkPlan ? 8 : walk == kWalkVoxels ? 7 : 6; }
 template <int WALK, bool LEAVE>
-__global__ __launch_bounds__(kWave) void k_shares(SharesArgs a) {
+__global__ __launch_bounds__(kWave, waves_of(WALK)) void k_shares(SharesArgs a) {
     __shared__ uint2 s_row[kEntries];   // first query, queries
-    __shared__ uint4 s_grid[WALK == kWalkGrid ? kEntries : 1];  // grids: first x, y and z
+    __shared__ float2 s_yz[WALK == kWalkGrid ? kEntries : 1];   // grids: y and z, first voxel in x
+    __shared__ uint32_t s_x[WALK == kWalkGrid ? kEntries : 1];
     const uint32_t lane = threadIdx.x;
     const uint64_t first = (a.wave0 + xcd_group<kXcdWaves>(blockIdx.x, gridDim.x)) * a.pack;
     if (first >= (uint64_t)a.n_gauss) return;
     const uint32_t nk = (uint64_t)a.n_gauss - first < a.pack ? (uint32_t)((uint64_t)a.n_gauss - first) : a.pack;
     const uint32_t gid = lane < nk ? a.gorder[first + lane] : 0u;
     uint32_t left;
-    const float sum = walk<WALK, LEAVE>(a, gid, nk, 0, 1, left, s_row, s_grid);
+    const float sum = walk<WALK, LEAVE>(a, gid, nk, 0, 1, left, s_row, s_yz, s_x);
     if (lane >= nk) return;
     if (LEAVE && (left >> lane & 1u)) {
         const uint32_t list = (uint32_t)((a.wave0 + blockIdx.x) % kTeamLists);
@@ -467,7 +485,8 @@ __global__ __launch_bounds__(kWave) void k_shares(SharesArgs a) {
 template <int WALK>
 __global__ __launch_bounds__(kTeam * kWave) void k_shares_team(SharesArgs a) {
     __shared__ uint2 s_row[kTeam][kEntries];
-    __shared__ uint4 s_grid[WALK == kWalkGrid ? kTeam : 1][WALK == kWalkGrid ? kEntries : 1];
+    __shared__ float2 s_yz[WALK == kWalkGrid ? kTeam : 1][WALK == kWalkGrid ? kEntries : 1];
+    __shared__ uint32_t s_x[WALK == kWalkGrid ? kTeam : 1][WALK == kWalkGrid ? kEntries : 1];
     __shared__ float s_sum[kTeam];
     const uint32_t lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const uint32_t list = blockIdx.x % kTeamLists, count = a.teams[list];
@@ -475,7 +494,7 @@ __global__ __launch_bounds__(kTeam * kWave) void k_shares_team(SharesArgs a) {
         const uint32_t gid = a.teams[kTeamLists + (size_t)list * a.team_room + i];
         uint32_t left;
         const float sum = walk<WALK, false>(a, gid, 1, wave, kTeam, left, s_row[wave],
-                                            s_grid[WALK == kWalkGrid ? wave : 0]);
+                                            s_yz[WALK == kWalkGrid ? wave : 0], s_x[WALK == kWalkGrid ? wave : 0]);
         if (lane == 0) s_sum[wave] = sum;
         __syncthreads();
         if (threadIdx.x == 0) {
