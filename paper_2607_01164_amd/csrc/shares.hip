@@ -9,7 +9,7 @@
 // are added at a Gaussian's end: no atomics, an order fixed by the inputs. The
 // bound is the arithmetic over the pairs of the rows, of which the cutoff
 // keeps a fourth to a third: a 128^3 jittered grid and 131072 Gaussians, 123
-// million pairs, 156 us. (A
+// million pairs, 151 us. (A
 // lane a row, each with its own record: 583 us.)
 #include <type_traits>
 
@@ -21,14 +21,15 @@ namespace gs {
 namespace {
 
 // Gaussians of a wave (consecutive in gorder), so that their rows fill its
-// lanes; fewer where there would be fewer waves than the chip holds (60011
-// Gaussians, a jittered 100^3 grid: one a wave 90 us, four 80).
+// lanes; fewer where there would be fewer waves than the chip holds (20011
+// Gaussians and 100003 points: two a wave 23 us, one 25; 30011 on a 64^3 grid:
+// three 29 us, one 33).
 constexpr uint32_t kPack = 4;
 constexpr int64_t kPackWaves = 8192;
 // Waves of an XCD that follow each other, so that neighbours read the same
-// queries through one L2 (a jittered 128^3 grid, 131072 Gaussians: 4 waves 195
-// us, 64 174 us, 512 181 us).
-constexpr uint32_t kXcdWaves = 64;
+// queries through one L2 (a jittered 128^3 grid, 131072 Gaussians, all of the
+// call: 4 waves some 195 us, 64 166, 128 160, 256 166, 512 172).
+constexpr uint32_t kXcdWaves = 128;
 // The rows of a Gaussian's queries: voxels of a grid; the plan's cells; voxels
 // of a jittered grid, every voxel with its query.
 enum { kWalkGrid = 0, kWalkPlan = 1, kWalkVoxels = 2 };
