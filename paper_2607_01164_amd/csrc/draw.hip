@@ -165,9 +165,9 @@ __device__ __forceinline__ double exp2_of(double z, int more) {
     return __builtin_amdgcn_ldexp(p, (int)n + more);
 }
 
-// What turns a row's keys into masses, given its largest key. (Formed without
-// a division or a library call a candidate: they cost more than the candidate
-// itself.)
+// What turns a row's keys into masses, given its largest key. (No library call
+// a candidate, and no division but the logarithm's: they cost more than the
+// candidate itself.)
 struct Scale {
     uint32_t top;
     double at;  // kRatio: 2^k / max, kPower: log2 max, kExp: max
@@ -1338,13 +1338,12 @@ hipError_t launch_draw(int64_t rows, int64_t n, const void *scores, int64_t stri
     using Few = std::integral_constant<int, kFew>;
     using List = std::integral_constant<int, kList>;
     if (n <= kRowLarge) {
-        if (want >= n) a.top_k = 0xFFFFFFFFu;
-        else a.top_k = (uint32_t)want;
-        if (n <= kRowSmall)
-            return want <= 64 && want < n ? rows_by(T64(), I8(), Few(), a, Lists{}) : rows_by(T64(), I8(), All(), a, Lists{});
-        if (n <= kRowMiddle)
-            return want <= 256 ? rows_by(T256(), I16(), Few(), a, Lists{}) : rows_by(T256(), I16(), All(), a, Lists{});
-        return want <= 1024 ? rows_by(T1024(), I16(), Few(), a, Lists{}) : rows_by(T1024(), I16(), All(), a, Lists{});
+        a.top_k = want < n ? (uint32_t)want : 0xFFFFFFFFu;
+        auto by = [&](auto threads, auto items) {
+            if (a.top_k <= (uint32_t)decltype(threads)::value) return rows_by(threads, items, Few(), a, Lists{});
+            return rows_by(threads, items, All(), a, Lists{});
+        };
+        return n <= kRowSmall ? by(T64(), I8()) : n <= kRowMiddle ? by(T256(), I16()) : by(T1024(), I16());
     }
     auto over = [](uint64_t blocks, auto launch) {
         for (uint64_t b = 0; b < blocks; b += kBlocksMost)
@@ -1392,10 +1391,14 @@ hipError_t launch_draw(int64_t rows, int64_t n, const void *scores, int64_t stri
     const uint64_t groups = ((uint64_t)draws + kBlock - 1) / kBlock, draw_blocks = (uint64_t)rows * groups;
     if (cut) {
         over(parts, [&](dim3 nb, uint64_t b) { hipLaunchKernelGGL(k_draw_run<true>, nb, pb, 0, s, a, w, b); });
-        over(draw_blocks, [&](dim3 nb, uint64_t b) { hipLaunchKernelGGL(k_draw_search<true>, nb, pb, 0, s, a, w, groups, b); });
+        over(draw_blocks, [&](dim3 nb, uint64_t b) {
+            hipLaunchKernelGGL(k_draw_search<true>, nb, pb, 0, s, a, w, groups, b);
+        });
     } else {
         over(parts, [&](dim3 nb, uint64_t b) { hipLaunchKernelGGL(k_draw_run<false>, nb, pb, 0, s, a, w, b); });
-        over(draw_blocks, [&](dim3 nb, uint64_t b) { hipLaunchKernelGGL(k_draw_search<false>, nb, pb, 0, s, a, w, groups, b); });
+        over(draw_blocks, [&](dim3 nb, uint64_t b) {
+            hipLaunchKernelGGL(k_draw_search<false>, nb, pb, 0, s, a, w, groups, b);
+        });
     }
     prof_end("draw_pick", s);
     return hipGetLastError();

@@ -176,9 +176,10 @@ __device__ Cut cut_after(const uint32_t *hist, Cut *cuts, uint32_t keep, uint32_
 
 // Counts of a digit over the Gaussians that have the cut's earlier digits.
 template <int DIGIT>
-__global__ __launch_bounds__(kCountThreads) void k_evict_count(int64_t n, int64_t stretch, const float *__restrict__ score,
-                                                        const uint8_t *__restrict__ pinned, uint32_t keep,
-                                                        uint32_t *hist, Cut *cuts) {
+__global__ __launch_bounds__(kCountThreads) void k_evict_count(int64_t n, int64_t stretch,
+                                                               const float *__restrict__ score,
+                                                               const uint8_t *__restrict__ pinned, uint32_t keep,
+                                                               uint32_t *hist, Cut *cuts) {
     constexpr uint32_t kBins = bins_of(DIGIT);
     __shared__ uint32_t s_hist[kBins];
     __shared__ uint32_t lds[kCountThreads / kWave + 2];
@@ -191,7 +192,8 @@ __global__ __launch_bounds__(kCountThreads) void k_evict_count(int64_t n, int64_
         Key k[kEach];
         const uint32_t m = load_keys(score, pinned, t0 + threadIdx.x * kEach, i1, k);
 #pragma unroll
-        for (uint32_t t = 0; t < kEach; ++t) hist_add(s_hist, digit_of<DIGIT>(k[t]), t < m && has_digits<DIGIT>(k[t], cut));
+        for (uint32_t t = 0; t < kEach; ++t)
+            hist_add(s_hist, digit_of<DIGIT>(k[t]), t < m && has_digits<DIGIT>(k[t], cut));
     }
     __syncthreads();
     uint32_t *out = hist + blockIdx.x % kCopies * kBinsAll + bins_before(DIGIT);
@@ -334,7 +336,8 @@ __global__ __launch_bounds__(kSmallThreads) void k_evict_small(int n, const floa
         for (int t = 0; t < kTiles; ++t) {
             if (t * (int)(kSmallThreads * kEach) >= n) continue;
 #pragma unroll
-            for (uint32_t j = 0; j < kEach; ++j) hist_add(s_hist, digit_of<D>(k[t][j]), j < m[t] && has_digits<D>(k[t][j], cut));
+            for (uint32_t j = 0; j < kEach; ++j)
+                hist_add(s_hist, digit_of<D>(k[t][j]), j < m[t] && has_digits<D>(k[t][j], cut));
         }
         __syncthreads();
         cut = next_digit<kSmallThreads, D, 1>(cut, s_hist, lds);
