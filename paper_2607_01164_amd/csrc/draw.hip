@@ -274,11 +274,20 @@ __device__ __forceinline__ uint64_t wave_scan(uint64_t x) {
     return x;
 }
 __device__ __forceinline__ uint32_t wave_scan(uint32_t x) { return wave_incl_sum(x); }
-__device__ __forceinline__ uint64_t last_lane(uint64_t x) {
-    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(x >> 32), kWave - 1) << 32 |
-           (uint32_t)__builtin_amdgcn_readlane((uint32_t)x, kWave - 1);
+// The same over the first 16 lanes.
+__device__ __forceinline__ uint64_t row_scan(uint64_t x) {
+    x += dpp_u64<0x111, 0xF>(x);
+    x += dpp_u64<0x112, 0xF>(x);
+    x += dpp_u64<0x114, 0xF>(x);
+    x += dpp_u64<0x118, 0xF>(x);
+    return x;
 }
-__device__ __forceinline__ uint32_t last_lane(uint32_t x) { return __builtin_amdgcn_readlane(x, kWave - 1); }
+__device__ __forceinline__ uint32_t row_scan(uint32_t x) { return wave_incl_sum(x); }
+__device__ __forceinline__ uint64_t lane_of(uint64_t x, uint32_t lane) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(x >> 32), lane) << 32 |
+           (uint32_t)__builtin_amdgcn_readlane((uint32_t)x, lane);
+}
+__device__ __forceinline__ uint32_t lane_of(uint32_t x, uint32_t lane) { return __builtin_amdgcn_readlane(x, lane); }
 
 // Exclusive sums over a workgroup of NT threads; *total gets the sum. lds: NT /
 // kWave entries, free again after a barrier.
@@ -286,22 +295,20 @@ template <int NT, typename V>
 __device__ __forceinline__ V group_scan(V x, uint64_t *lds, V *total) {
     const V incl = wave_scan(x);
     if (NT == kWave) {
-        *total = last_lane(incl);
+        *total = lane_of(incl, kWave - 1);
         return incl - x;
     }
-    const uint32_t wave = threadIdx.x / kWave;
+    // the waves' sums, a lane each (16 loads and sums of every thread take 30
+    // registers: 300 rows of 16000, top-k 50, 43 us instead of 37)
+    constexpr uint32_t kWaves = NT / kWave;
+    static_assert(kWaves <= 16, "the waves' sums are a row of lanes");
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     __syncthreads();
-    if (threadIdx.x % kWave == kWave - 1) lds[wave] = incl;
+    if (lane == kWave - 1) lds[wave] = incl;
     __syncthreads();
-    V before = 0, all = 0;
-#pragma unroll
-    for (int w = 0; w < NT / kWave; ++w) {
-        const V v = (V)lds[w];
-        if ((uint32_t)w < wave) before += v;
-        all += v;
-    }
-    *total = all;
-    return before + incl - x;
+    const V upto = row_scan(lane < kWaves ? (V)lds[lane] : (V)0);
+    *total = lane_of(upto, kWaves - 1);
+    return (wave ? lane_of(upto, wave - 1) : (V)0) + incl - x;
 }
 template <int NT, typename V>
 __device__ __forceinline__ V group_sum(V x, uint64_t *lds) {
@@ -316,10 +323,7 @@ __device__ __forceinline__ uint32_t group_max(uint32_t x, uint64_t *lds) {
     __syncthreads();
     if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = x;
     __syncthreads();
-    x = 0;
-#pragma unroll
-    for (int w = 0; w < NT / kWave; ++w) x = umax_(x, (uint32_t)lds[w]);
-    return x;
+    return wave_max_uniform(threadIdx.x % kWave < NT / kWave ? (uint32_t)lds[threadIdx.x % kWave] : 0u);
 }
 
 // ---- rows of a workgroup --------------------------------------------------
@@ -611,9 +615,14 @@ __global__ __launch_bounds__(NT, waves_of(NT)) void k_draw_rows(DrawArgs a, List
 // A stretch of a row: its first `want` candidates in the order of the scores,
 // listed in the order of the row. The first `want` of the row are among those
 // of its stretches. (256 stretches of bfloat16 logits, 200 of each: 14.5 us.)
+// WAVES of a SIMD, to which registers are held: 8 put two workgroups on a
+// compute unit and spill some (2048 stretches: 90 -> 77 us, 256: 16 -> 18, with
+// the launch).
 constexpr int kListThreads = 1024, kListItems = 16;
 constexpr uint32_t kListStretch = kListThreads * kListItems;
-__global__ __launch_bounds__(kListThreads) void k_draw_list(DrawArgs a, Lists w, uint64_t block0) {
+constexpr uint64_t kListOnce = 256;  // stretches that the compute units take at once, one each
+template <int WAVES>
+__global__ __launch_bounds__(kListThreads, WAVES) void k_draw_list(DrawArgs a, Lists w, uint64_t block0) {
     __shared__ unsigned long long s_hist[kSmallBins];
     __shared__ uint64_t lds[kListThreads / kWave + 2];
     const uint64_t block = block0 + blockIdx.x;
@@ -1359,7 +1368,10 @@ hipError_t launch_draw(int64_t rows, int64_t n, const void *scores, int64_t stri
         l.id = (uint32_t *)((char *)work + list_bytes(rows) / 2);
         prof_begin("draw_list", s);
         over((uint64_t)rows * l.stretches, [&](dim3 nb, uint64_t b) {
-            hipLaunchKernelGGL(k_draw_list, nb, dim3(kListThreads), 0, s, a, l, b);
+            if ((uint64_t)rows * l.stretches > kListOnce)
+                hipLaunchKernelGGL(k_draw_list<8>, nb, dim3(kListThreads), 0, s, a, l, b);
+            else
+                hipLaunchKernelGGL(k_draw_list<4>, nb, dim3(kListThreads), 0, s, a, l, b);
         });
         prof_end("draw_list", s);
         DrawArgs d = a;

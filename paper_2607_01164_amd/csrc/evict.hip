@@ -109,20 +109,14 @@ __device__ __forceinline__ void hist_add(uint32_t *hist, uint32_t bin, bool acti
 template <int NT>
 __device__ __forceinline__ uint32_t group_scan(uint32_t x, uint32_t *lds, uint32_t *total) {
     constexpr uint32_t kWaves = NT / kWave;
-    const uint32_t wave = threadIdx.x / kWave;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
     const uint32_t incl = wave_incl_sum(x);
     __syncthreads();
-    if (threadIdx.x % kWave == kWave - 1) lds[wave] = incl;
+    if (lane == kWave - 1) lds[wave] = incl;
     __syncthreads();
-    uint32_t before = 0, all = 0;
-#pragma unroll
-    for (uint32_t w = 0; w < kWaves; ++w) {
-        const uint32_t v = lds[w];
-        if (w < wave) before += v;
-        all += v;
-    }
-    *total = all;
-    return before + incl - x;
+    const uint32_t upto = wave_incl_sum(lane < kWaves ? lds[lane] : 0u);
+    *total = __builtin_amdgcn_readlane(upto, kWaves - 1);
+    return (wave ? (uint32_t)__builtin_amdgcn_readlane(upto, wave - 1) : 0u) + incl - x;
 }
 
 // The cut with its next digit, from that digit's counts: the bin in which
