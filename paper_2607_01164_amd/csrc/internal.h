@@ -169,6 +169,7 @@ __device__ __forceinline__ float readlane_f(float x, uint32_t l) {
 }
 
 __device__ __forceinline__ uint32_t umax_(uint32_t a, uint32_t b) { return a > b ? a : b; }
+__device__ __forceinline__ uint32_t umin_(uint32_t a, uint32_t b) { return a < b ? a : b; }
 
 // Wave-uniform maximum of a 32-bit value (every lane must be active): DPP
 // within each row of 16 lanes, then the four row results by readlane.
@@ -564,6 +565,17 @@ __device__ __forceinline__ uint32_t plan_row(const Record &r, uint32_t lx, uint3
     return point_off[base + (uint32_t)qh + 1u] - start;
 }
 
+// The whole numbers from a to c among v0 .. v1: first and how many (NaN leaves
+// that end's v0 or v1). Cut as whole numbers: float32 holds v0 and v1 up to
+// 2^24 only, past it their nearest would leave some out or pass the end.
+__device__ __forceinline__ uint32_t clip_range(float a, float c, uint32_t v0, uint32_t v1, uint32_t &first) {
+    constexpr float kMost = 0x1.fffffep31f;
+    c = fminf(c, kMost);
+    first = umax_((uint32_t)fminf(fmaxf(a, 0.0f), kMost), v0);
+    const uint32_t last = umin_((uint32_t)fmaxf(c, 0.0f), v1);
+    return c >= 0.0f && first <= last ? last - first + 1u : 0u;
+}
+
 // The voxels a Gaussian's rows can hold on a grid: x0 .. x1 of its box, and
 // the rows y0 .. y0 + ny - 1, z0 .. z0 + nz - 1 that its cutoff ellipsoid
 // reaches. Q >= (U22 dz)^2, and over x and z Q is at least dy^2 U11^2 / (1 +
@@ -587,11 +599,8 @@ __device__ __forceinline__ GridRows grid_rows(const Record &r, const CellBox &b,
     // that is not a number leaves the box's
     auto cut = [](float mu, float h, float lo, float iv, float slack, uint32_t v0, uint32_t v1, uint32_t &first,
                   uint32_t &n) {
-        const float a = fmaxf(ceilf((mu - h - lo) * iv - 0.5f - slack), (float)v0);
-        const float c = fminf(floorf((mu + h - lo) * iv - 0.5f + slack), (float)v1);
-        const bool some = a <= c;
-        first = some ? (uint32_t)a : v0;
-        n = some ? (uint32_t)(c - a) + 1u : 0u;
+        n = clip_range(ceilf((mu - h - lo) * iv - 0.5f - slack), floorf((mu + h - lo) * iv - 0.5f + slack), v0, v1,
+                       first);
     };
     cut(r.f0.y, hy, g.lo[1], bg.ivsz[1], bg.vslack[1], (uint32_t)b.lo.y * ry, ((uint32_t)b.hi.y + 1u) * ry - 1u, o.y0,
         o.ny);
@@ -612,13 +621,8 @@ __device__ __forceinline__ uint32_t grid_row(const Record &r, uint32_t x0, uint3
     float xl, xh;
     if (!slab_xrange(r, dy, dy, dz, dz, bg.T2, xl, xh)) return 0;
     // voxels vx of the box with lo + (vx + 1/2) vsz in [xl, xh]
-    const float vmin = (float)x0, vmax = (float)x1;
-    const float a = fminf(fmaxf((xl - g.lo[0]) * bg.ivsz[0] - 0.5f - bg.vslack[0], vmin), vmax + 1.0f);
-    const float b = fminf(fmaxf((xh - g.lo[0]) * bg.ivsz[0] - 0.5f + bg.vslack[0], vmin - 1.0f), vmax);
-    const float v0 = ceilf(a), v1 = floorf(b);
-    if (v1 < v0) return 0;
-    first = (uint32_t)v0;
-    return (uint32_t)(v1 - v0) + 1u;
+    return clip_range(ceilf((xl - g.lo[0]) * bg.ivsz[0] - 0.5f - bg.vslack[0]),
+                      floorf((xh - g.lo[0]) * bg.ivsz[0] - 0.5f + bg.vslack[0]), x0, x1, first);
 }
 
 struct BackwardBuffers {

@@ -185,11 +185,8 @@ __device__ __forceinline__ void voxel_rows(const Record &r, const QueryParams &q
     const float t = r.f2.y / r.f2.z;
     const float hy = rt * sqrt_hw(fmaf_(t, t, 1.0f)) / r.f2.x, hz = rt / r.f2.z;
     auto cut = [](float mu, float h, float lo, float iv, float slack, int32_t dim, uint32_t &first, uint32_t &n) {
-        const float a = fmaxf(floorf((mu - h - lo) * iv - slack), 0.0f);
-        const float c = fminf(floorf((mu + h - lo) * iv + slack), (float)(dim - 1));
-        const bool some = a <= c;
-        first = some ? (uint32_t)a : 0u;
-        n = some ? (uint32_t)(c - a) + 1u : 0u;
+        n = clip_range(floorf((mu - h - lo) * iv - slack), floorf((mu + h - lo) * iv + slack), 0u, (uint32_t)dim - 1u,
+                       first);
     };
     cut(r.f0.y, hy, g.lo[1], bg.ivsz[1], bg.vslack[1], q.dims[1], y0, ny);
     cut(r.f0.z, hz, g.lo[2], bg.ivsz[2], bg.vslack[2], q.dims[2], z0, nz);
@@ -210,11 +207,8 @@ __device__ __forceinline__ uint32_t voxel_row(const Record &r, const VoxelReach 
     const float w = sqrt_hw(left) * iu * (1.0f + 0x1p-10f) + v.shift;
     const float c = r.f0.x - fmaf_(r.f1.y, dy, r.f1.z * dz) * iu;
     const float m = (fabsf(r.f0.x) + fabsf(c) + w) * 0x1p-20f;
-    const float a = fmaxf(floorf((c - w - m - g.lo[0]) * bg.ivsz[0] - bg.vslack[0]), 0.0f);
-    const float b = fminf(floorf((c + w + m - g.lo[0]) * bg.ivsz[0] + bg.vslack[0]), (float)(q.dims[0] - 1));
-    if (!(a <= b)) return 0;
-    first = (uint32_t)a;
-    return (uint32_t)(b - a) + 1u;
+    return clip_range(floorf((c - w - m - g.lo[0]) * bg.ivsz[0] - bg.vslack[0]),
+                      floorf((c + w + m - g.lo[0]) * bg.ivsz[0] + bg.vslack[0]), 0u, (uint32_t)q.dims[0] - 1u, first);
 }
 
 // A wave takes `pack` Gaussians (consecutive in gorder). Their rows are listed
