@@ -539,6 +539,10 @@ __device__ __forceinline__ bool slab_xrange(const Record &r, float ay, float by,
     return true;
 }
 
+// floor(x) as a whole number of 32 bits, the nearest one where x is none; 0 for
+// NaN.
+__device__ __forceinline__ uint32_t whole_of(float x) { return (uint32_t)fminf(fmaxf(x, 0.0f), 0x1.fffffep31f); }
+
 // The plan entries [start, start + len) of row (cy, cz) of a box spanning
 // cells lx .. lx + nx - 1 along x whose queries can lie within the cutoff
 // T2 of the record (ordered queries): the row's y, z extent widened by the
@@ -555,14 +559,15 @@ __device__ __forceinline__ uint32_t plan_row(const Record &r, uint32_t lx, uint3
     const float z1 = g.lo[2] + (float)(cz + 1u) * bg.cw[1] + bg.slack[1];
     float xl, xh;
     if (!slab_xrange(r, y0 - r.f0.y, y1 - r.f0.y, z0 - r.f0.z, z1 - r.f0.z, bg.T2, xl, xh)) return 0;
-    const float qmin = (float)(kSub * lx), qmax = (float)(kSub * (lx + nx)) - 1.0f;
-    const float ql = fminf(fmaxf(floorf((float)kSub * ((xl - g.lo[0]) * g.invc[0])), qmin), qmax);
-    const float qh = fminf(fmaxf(floorf((float)kSub * ((xh - g.lo[0]) * g.invc[0])), qmin), qmax);
+    // (whole numbers clamp them: float32 holds those up to 2^24 only)
+    const uint32_t qmin = kSub * lx, qmax = kSub * (lx + nx) - 1u;
+    const uint32_t ql = umin_(umax_(whole_of((float)kSub * ((xl - g.lo[0]) * g.invc[0])), qmin), qmax);
+    const uint32_t qh = umin_(umax_(whole_of((float)kSub * ((xh - g.lo[0]) * g.invc[0])), qmin), qmax);
     // the row's quarters are entries base .. base + K of the plan's offsets,
     // the last one the start of the next row of cells
     const uint32_t base = (cz * (uint32_t)g.cells[1] + cy) * bg.K;
-    start = point_off[base + (uint32_t)ql];
-    return point_off[base + (uint32_t)qh + 1u] - start;
+    start = point_off[base + ql];
+    return point_off[base + qh + 1u] - start;
 }
 
 // The whole numbers from a to c among v0 .. v1: first and how many (NaN leaves

@@ -63,3 +63,36 @@ def test_voxels(kind, dims, cells):
                               gs.alloc_backward_work(index, query, DEV))
         # (pairs at the cutoff, 0.01 each, are decided in float32 there)
         assert (np.abs(grads.weight.cpu().numpy() - ref / g.weight) <= tol / g.weight + 0.03).all()
+
+
+@pytest.mark.parametrize("cells", [(2 ** 22 + 1, 1, 1), (2 ** 22 + 2, 2, 1), (2 ** 24 + 3, 1, 1)])
+def test_cells(cells):
+    """Points at either end of an axis of cells, some past it: those of the
+    last cell count, those outside for nothing whatever their influence."""
+    size = tuple(float(c) for c in cells)  # cells of size 1
+    g = two_at_the_ends(cells, 0, 30.0)
+    r = np.random.default_rng(0)
+    n = 3001
+    points = r.uniform(0, 1, (n, 3)) * np.asarray([1.0, size[1], size[2]])
+    points[:, 0] = np.where(r.random(n) < 0.5, r.uniform(-30, 150, n), size[0] + r.uniform(-150, 30, n))
+    points = points.astype(np.float32)
+    gauss, grid, query = device_gaussians(g), gs.make_grid(cells, (0.0, 0.0, 0.0), size), gs.Query.pts(dev(points))
+    index = gs.build_index(gauss, grid, TAU)
+    plan, value, influence = gs.alloc_plan(query, grid, DEV), torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    gs.gs_sample(gauss, index, query, value, influence, plan)
+    work, out = gs.alloc_shares_work(index, query, DEV), torch.empty(2, device=DEV)
+    ones = np.ones(n, np.float32)
+    inside = ((points >= 0) & (points <= np.asarray(size, np.float32))).all(1)
+    assert 0.1 < (~inside).mean() < 0.3
+    ref, tol = bo.shares(g, points, ones, tau=TAU, hi=size)
+    beyond = bo.shares(g, points, np.where(inside, 0, ones), tau=TAU, lo=(-99, -99, -99), hi=(2.0 ** 25,) * 3)[0]
+    assert beyond[0] > 50 and tol.max() < 0.02  # the points past the far end would show
+    gs.gs_shares(gauss, index, query, plan, dev(ones), out, work)
+    assert (np.abs(out.cpu().numpy() - ref) <= tol).all(), (out, ref)
+    # dL/dw with dL/dI = 1: the sum of G over the defined points (pairs at the
+    # cutoff, 0.01 each, are decided in float32 there)
+    gs.gs_shares(gauss, index, query, plan, influence, out, work, gain=influence)
+    grads = gs.Grads.empty(2, DEV)
+    gs.gs_sample_backward(gauss, index, query, plan, value, influence, torch.zeros_like(value), dev(ones), grads,
+                          gs.alloc_backward_work(index, query, DEV))
+    assert (np.abs(grads.weight.cpu().numpy() * g.weight - out.cpu().numpy()) <= 2 * tol + 0.03).all()
