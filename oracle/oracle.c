@@ -707,7 +707,7 @@ static int64_t cell_box(const float *mu, const float *s, const float *q, float v
         volatile float dl = lo_ - lo[j], dh = hi_ - lo[j];
         volatile float tl = dl * invc[j], th = dh * invc[j];
         float fl = floorf(tl), fh = floorf(th);
-        float cmax = (float)(cells[j] - 1);
+        double cmax = (double)(cells[j] - 1);
         if (!isfinite(h) || !isfinite(fl) || !isfinite(fh) || !(fh >= 0.0f) || !(fl <= cmax)) return 0;
         b[j] = (int32_t)(fl > 0.0f ? fl : 0.0f);
         b[3 + j] = (int32_t)(fh < cmax ? fh : cmax);

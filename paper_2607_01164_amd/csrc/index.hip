@@ -290,6 +290,7 @@ __global__ __launch_bounds__(kPreBlock) void k_preprocess(const float *__restric
     R[2][1] = 2.0f * (qy * qz + qw * qx);
     R[2][2] = 1.0f - 2.0f * (qx * qx + qy * qy);
 
+    constexpr float kCellMost = 0x1.fffffep30f;  // the last float32 below 2^31
     int lo_c[3], hi_c[3];
     uint64_t cnt = 1;
 #pragma unroll
@@ -301,10 +302,12 @@ __global__ __launch_bounds__(kPreBlock) void k_preprocess(const float *__restric
         const float tl = (lo - g.lo[j]) * g.invc[j];
         const float th = (hi - g.lo[j]) * g.invc[j];
         const float fl = floorf(tl), fh = floorf(th);
-        const float cmax = (float)(g.cells[j] - 1);
-        if (!finite_f(h) || !finite_f(fl) || !finite_f(fh) || !(fh >= 0.0f) || !(fl <= cmax)) valid = false;
-        lo_c[j] = valid ? (int)(fl > 0.0f ? fl : 0.0f) : 0;
-        hi_c[j] = valid ? (int)(fh < cmax ? fh : cmax) : -1;
+        if (!finite_f(h) || !finite_f(fl) || !finite_f(fh) || !(fh >= 0.0f)) valid = false;
+        // (whole numbers clamp them: float32 holds those up to 2^24 only)
+        const int lc = (int)fminf(fmaxf(fl, 0.0f), kCellMost), hc = (int)fminf(fmaxf(fh, 0.0f), kCellMost);
+        if (lc >= g.cells[j]) valid = false;
+        lo_c[j] = valid ? lc : 0;
+        hi_c[j] = valid ? (hc < g.cells[j] ? hc : g.cells[j] - 1) : -1;
         cnt *= valid ? (uint64_t)(hi_c[j] - lo_c[j] + 1) : 0ull;
     }
     if (!valid) {

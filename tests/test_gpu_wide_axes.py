@@ -96,3 +96,34 @@ def test_cells(cells):
     gs.gs_sample_backward(gauss, index, query, plan, value, influence, torch.zeros_like(value), dev(ones), grads,
                           gs.alloc_backward_work(index, query, DEV))
     assert (np.abs(grads.weight.cpu().numpy() * g.weight - out.cpu().numpy()) <= 2 * tol + 0.03).all()
+
+
+@pytest.mark.parametrize("cells", [(2 ** 24 + 2, 1, 1), (2 ** 25 + 4, 1, 1), (1, 2, 2 ** 24 + 2)])
+def test_index_boxes(cells):
+    """The index lists the last cells of an axis, none past them, and points
+    there are defined: I against float64."""
+    axis = int(np.argmax(cells))
+    size = tuple(float(c) for c in cells)
+    g = two_at_the_ends(cells, axis, 30.0)
+    r = np.random.default_rng(1)
+    n = 501
+    points = r.uniform(0, 1, (n, 3)) * np.asarray(size)
+    points[:, axis] = np.where(r.random(n) < 0.4, r.uniform(0, 150, n), size[axis] - r.uniform(0, 150, n))
+    points = points.astype(np.float32)
+    gauss, grid, query = device_gaussians(g), gs.make_grid(cells, (0.0, 0.0, 0.0), size), gs.Query.pts(dev(points))
+    index = gs.build_index(gauss, grid, TAU)
+    keys = index.keys[:index.n_pairs].cpu().numpy().astype(np.uint32)
+    ncells = int(np.prod(cells))
+    assert keys.max() == ncells - 1 and index.cell_offsets[ncells] == index.n_pairs
+    value, influence = torch.empty(n, device=DEV), torch.empty(n, device=DEV)
+    gs.gs_sample(gauss, index, query, value, influence, gs.alloc_plan(query, grid, DEV))
+    ref, slack = np.zeros(n), np.zeros(n)
+    for i in range(2):
+        q = (bo.whitened(g, i, points) ** 2).sum(1)
+        ref += np.where(q <= bo.cut(TAU), g.weight[i] * np.exp(-0.5 * q), 0)
+        # (pairs at the cutoff are decided in float32)
+        slack += np.where(np.abs(q / bo.cut(TAU) - 1) < 1e-5, TAU * g.weight[i], 0)
+    got = influence.cpu().numpy()
+    sure = ref > TAU * (1 + 1e-3) + slack
+    assert sure[points[:, axis] > size[axis] - 4].sum() > 2  # the last cells among them
+    assert (np.abs(got - ref)[sure] <= slack[sure] + 1e-4 * ref[sure]).all()
