@@ -285,7 +285,8 @@ __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32
     const uint32_t groups = batches < parts ? (batches ? batches : 1u) : parts;
     const uint32_t sub = part / groups, subs = parts / groups;
     const uint32_t rb0 = sub < subs ? part % groups * kWave : Rw;
-    for (uint32_t rb = rb0; rb < Rw; rb += groups * kWave) {
+    const uint32_t stride = groups * kWave;
+    for (uint32_t rb = rb0; rb < Rw; rb = Rw - rb > stride ? rb + stride : Rw) {  // (rb + stride may pass 2^32)
         // lane l sets up row rb + l of the wave's list, of Gaussian i (the
         // permutes run with every lane)
         const uint32_t gr = rb + lane;
