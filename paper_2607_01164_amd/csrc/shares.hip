@@ -35,13 +35,16 @@ constexpr uint32_t kXcdWaves = 128;
 enum { kWalkGrid = 0, kWalkPlan = 1, kWalkVoxels = 2 };
 // queries from which a jittered grid is walked by voxels
 constexpr int64_t kVoxelsLeast = 4096;
-// A Gaussian of more than kStepsMost steps in its first 64 rows, or of more than
-// kRowsMost rows, keeps its wave long after the others are done. Where there
-// are queries for such ones, they are left to the launch that follows, a
-// workgroup of kTeam waves each. (One Gaussian that reaches all of 2 M points
-// or voxels: 5.0 to 10 ms -> 0.73 to 1.5 ms; 9001 Gaussians, 300007 crowded
-// points: 114 -> 93 us; without such ones the launch costs 3 us.) They go
-// to kTeamLists lists: counts in one place wait for each other.
+// A Gaussian of more than kRowsMost rows, or that comes to more than kStepsMost
+// steps with any of its batches of rows, keeps its wave long after the others
+// are done. Where there are queries for such ones, they are left to the launch
+// that follows, a workgroup of kTeam waves each. (One Gaussian that reaches all
+// of 2 M points or voxels: 5.0 to 10 ms -> 0.73 to 1.5 ms; 9001 Gaussians,
+// 300007 crowded points: 114 -> 93 us. Its first batch alone tells little of a
+// Gaussian whose rows begin at that batch's end: one behind 60 rows of another
+// that reaches all of 1 M points, 3.2 ms by its wave, 0.58 by a team. Without
+// such ones the launch costs 4 to 5 us.) They go to kTeamLists lists: counts in
+// one place wait for each other.
 constexpr uint32_t kStepsMost = 256, kRowsMost = 1024;
 constexpr uint32_t kTeam = 8;
 constexpr int64_t kTeamQueries = 65536;
@@ -224,7 +227,7 @@ constexpr uint32_t kEntries = kPieces * kWave + kAhead * 16;  // the last steps 
 
 // The sums of a wave's Gaussians, lane i < nk Gaussian i's (mgid). part of
 // parts: of the steps, or of the rows where there are many, this wave takes its
-// share. LEAVE: Gaussians of too many steps are left out, in `left` by bit.
+// share. LEAVE: Gaussians of too many rows or steps are left out, in `left` by bit.
 template <int WALK, bool LEAVE>
 __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32_t nk, uint32_t part, uint32_t parts,
                                       uint32_t &left, uint2 *s_row, float2 *s_yz, uint32_t *s_x) {
@@ -263,13 +266,17 @@ __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32
             }
         }
     }
+    if (LEAVE) {
+        left = (uint32_t)__ballot(mR > kRowsMost);  // (lanes from nk on have none)
+        mR = mR > kRowsMost ? 0u : mR;
+    }
     const uint32_t mRend = wave_incl_sum(mR);
     const uint32_t Rw = __builtin_amdgcn_readlane(mRend, kWave - 1);
     const bool fdiv = wave_max_uniform(mR) < (1u << 21);
     float mtot = 0.0f;  // lane i < nk: Gaussian i's sum
     float acc = 0.0f;   // of the Gaussian being walked
     uint32_t cur = ~0u, cgid = 0;
-    bool skip = false;
+    uint32_t steps = 0;  // of it, so far
     Record c = {};
     float margin = 0.0f;
     auto finish = [&]() {
@@ -334,7 +341,6 @@ __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32
             }
         }
         __builtin_amdgcn_wave_barrier();
-        const uint32_t limit = whole ? 0u : kStepsMost << (6u - shift);  // pieces of so many steps
         const uint32_t nrows = Rw - rb < (uint32_t)kWave ? Rw - rb : (uint32_t)kWave;
         const uint32_t ia = __builtin_amdgcn_readlane(i, 0), ib = __builtin_amdgcn_readlane(i, nrows - 1);
         for (uint32_t gi = ia; gi <= ib; ++gi) {
@@ -348,17 +354,24 @@ __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32
             if (gi != cur) {
                 if (cur != ~0u) finish();
                 cur = gi;
-                skip = LEAVE && (gR > kRowsMost || rz - ra > limit);
-                if (LEAVE && skip && gR <= kRowsMost && whole) {
-                    const uint32_t all = wave_incl_sum(lane >= la && lane < lb ? len : 0u);
-                    skip = __builtin_amdgcn_readlane(all, kWave - 1) / kWave > kStepsMost;
-                }
-                left |= skip ? 1u << gi : 0u;
+                steps = 0;
                 cgid = __builtin_amdgcn_readlane(mgid, gi);
                 c = load_record_uniform(a.rec, cgid);
                 margin = readfirst_f(cutoff_margin(a.exact, cgid, T));
             }
-            if (LEAVE && skip) continue;
+            if (LEAVE) {
+                if (whole) {
+                    const uint32_t all = wave_incl_sum(lane >= la && lane < lb ? len : 0u);
+                    steps += __builtin_amdgcn_readlane(all, kWave - 1) / kWave;
+                } else {
+                    steps += (rz - ra) >> (6u - shift);
+                }
+                if (steps > kStepsMost) {  // the team walks all of it
+                    left |= 1u << gi;
+                    acc = 0.0f;
+                    continue;
+                }
+            }
             // kAhead queries of a lane: query k[u] if on[u], at voxel x[u] of
             // its row in grids
             auto add = [&](const uint32_t k[kAhead], const bool on[kAhead], const Voxel v[kAhead]) {
