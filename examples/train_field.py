@@ -159,13 +159,16 @@ class Trainer:
         gs.gs_adamw(self.adam, control=self.control, eps=1e-15, seed=self.seed)
 
     def densify(self, max_new):
-        """Prunes and grows the field after a step; moments follow."""
+        """Prunes and grows the field after a step; moments and scores follow (a
+        new Gaussian has none)."""
         old, new = self.now, 1 - self.now
         work = gs.alloc_densify_work(self.n, self.query, self.device)
         n = gs.gs_densify(self.sets[old], self.n, self.gauss.weight, self.grid, self.query, self.value,
                           self.influence, self.target, None, PRUNE_WEIGHT, TAU, self.new_log_scale,
                           math.log(NEW_WEIGHT / (1.0 - NEW_WEIGHT)), max_new, self.sets[new], self.source, work)
         gs.gs_adamw_carry(self.carries[old], self.n, self.source, n)
+        source = self.source[:n].long()
+        self.scores[new][:n] = torch.where(source >= 0, self.scores[old][source.clamp(min=0)], 0.0)
         self.n, self.now = n, new
         self.layout()
 
@@ -194,6 +197,8 @@ class Trainer:
         gs.gs_adamw_carry(self.carries[old], n, self.source, n)
         self.now = new
         self.layout()
+        # the rows have moved: a densification prunes by the activated weights
+        gs.gs_activate(self.raw, SCALE_CAP, self.gauss.scale, self.gauss.value, self.gauss.weight)
 
     def loss(self):
         return gs.read_loss_terms(self.terms)["total"]
@@ -207,8 +212,12 @@ class Trainer:
         return -10.0 * math.log10(float(err))
 
 
-def train(t, steps, densify_every=100, report=None, rebalance_every=0):
-    """`steps` iterations of a Trainer; returns [(step, Gaussians, loss)]."""
+def train(t, steps, densify_every=None, report=None, rebalance_every=0):
+    """`steps` iterations of a Trainer; returns [(step, Gaussians, loss)].
+    densify_every None: 100, or never where rebalance_every holds the number of
+    Gaussians."""
+    if densify_every is None:
+        densify_every = 0 if rebalance_every else 100
     seen = []
     for k in range(1, steps + 1):
         t.step(attend=rebalance_every > 0)
@@ -234,7 +243,7 @@ def main():
                     help="hold the number of Gaussians and move a tenth of them this often (no densification then)")
     a = ap.parse_args()
     t = Trainer(a.gaussians, a.dims, gs.GS_MOMENTS_MXFP8 if a.moments == 8 else gs.GS_MOMENTS_F32)
-    train(t, a.steps, 0 if a.rebalance_every else a.densify_every,
+    train(t, a.steps, None if a.rebalance_every else a.densify_every,
           lambda k, n, x: print(f"step {k:5d}  {n:8d} Gaussians  loss {x:.5f}", flush=True), a.rebalance_every)
     c = gs.read_adam_control(t.control)
     print(f"{c['step']} steps, {c['skipped']} skipped, last gradient norm {c['norm']:.3g}, PSNR {t.psnr():.2f} dB")
