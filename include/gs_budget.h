@@ -12,7 +12,8 @@
  * (nothing here waits), gs_status codes with gs_last_error(), no device memory
  * allocated by the library. Every call may be captured into a HIP graph, and
  * the same inputs give bit-identical results. Calls that share a workspace
- * follow each other.
+ * follow each other. Outputs and the workspace overlap neither inputs nor each
+ * other; a call whose arrays do is refused (GS_ERR_INVALID_ARGUMENT).
  */
 #ifndef GS_BUDGET_H
 #define GS_BUDGET_H
@@ -43,7 +44,8 @@ size_t gs_shares_work_bytes(const gs_index *index, const gs_query *query);
  * gs_sample_planned) filled for this index and query; influence is read from
  * the caller's array, not from the plan. gauss must be the Gaussians that the
  * index was built from, unchanged. decay = 0 overwrites score without reading
- * it (0 <= decay, finite). score overlaps no input.
+ * it (0 <= decay, finite). score and work overlap no input (the Gaussians, the
+ * index's arrays, the query's, the plan, influence and gain).
  * The sums are float32, in an order that the inputs alone fix. Pairs whose Q
  * is so near the cutoff that float32 cannot tell are decided in float64 from
  * gauss (the sampler decides them in float32: of a pair that the two take
@@ -65,7 +67,7 @@ size_t gs_evict_work_bytes(int64_t n);
  * ones stand in out in the order of their indices: source[j] is the input
  * index of row j, rising with j, as gs_adamw_carry takes it, and score_out[j]
  * its score (null: not wanted). out, source and score_out have room for
- * min(budget, n) rows and overlap no input. 0 <= n, budget < 2^31.
+ * min(budget, n) rows. 0 <= n, budget < 2^31.
  */
 gs_status gs_evict(const gs_params *in, int64_t n, const float *score, const uint8_t *pinned, int64_t budget,
                    const gs_params *out, int32_t *source, float *score_out, void *work, size_t work_bytes,
@@ -112,10 +114,10 @@ size_t gs_draw_work_bytes(int64_t rows, int64_t n, int64_t draws);
  * and prob (null: not wanted) q_j / M. All sums are exact, so the draws do
  * not depend on how the work is cut. temperature 0 draws the first of the
  * largest scores, with prob 1. A row in which nothing can be drawn (no
- * candidates, or none with mass) gives id -1 and prob 0. ids and prob overlap
- * no input. Numbers in rising order draw ids in rising order, which reads
- * memory line by line, here and where gs_split copies what was drawn (419430
- * of 2 M Gaussians: 65 -> 55 us and 78 -> 37).
+ * candidates, or none with mass) gives id -1 and prob 0. Numbers in rising
+ * order draw ids in rising order, which reads memory line by line, here and
+ * where gs_split copies what was drawn (419430 of 2 M Gaussians: 65 -> 55 us
+ * and 78 -> 37).
  * 0 <= rows, n < 2^31, 0 <= draws < 2^31, rows n and rows draws below 2^40.
  */
 gs_status gs_draw(int64_t rows, int64_t n, const void *scores, int64_t stride, const int32_t *lengths,
@@ -138,7 +140,8 @@ size_t gs_split_work_bytes(int64_t n);
  * An id outside [0, n) makes a Gaussian that contributes nothing: its mean is
  * NaN, its log-scale 0, its rotation (1, 0, 0, 0), its value logit 0, its
  * weight logit -infinity, its score 0, and source is -1 - id (-1 for a negative
- * id). n + count < 2^31. ids, source, score and the set do not overlap.
+ * id). n + count < 2^31. No two of the set's arrays, ids, source, score and
+ * work overlap.
  */
 gs_status gs_split(const gs_params *set, int64_t n, const int32_t *ids, int64_t count, int32_t *source, float *score,
                    void *work, size_t work_bytes, hipStream_t stream);

@@ -598,6 +598,14 @@ bool overlap(const Span (&a)[N], const Span (&b)[M]) {
             if (overlap(x, y)) return true;
     return false;
 }
+// Whether two of them overlap.
+template <size_t N>
+bool overlap_each_other(const Span (&a)[N]) {
+    for (size_t i = 0; i < N; ++i)
+        for (size_t j = 0; j < i; ++j)
+            if (overlap(a[i], a[j])) return true;
+    return false;
+}
 Span floats(const float *p, int64_t n) { return Span{p, sizeof(float) * (size_t)n}; }
 
 }  // namespace
@@ -1256,11 +1264,19 @@ gs_status gs_shares(const gs_gaussians *gauss, const gs_index *index, const gs_q
             return fail(GS_ERR_WORKSPACE, "gs_shares: plan needs %zu bytes (got %zu)", need, plan_bytes);
         p = plan_layout(const_cast<void *>(plan), nq, gp.ncells);
     }
-    const Span read[] = {floats(gauss->mean, 3 * n), floats(gauss->scale, 3 * n), floats(gauss->rot, 4 * n),
-                         floats(influence, nq), floats(gain, nq)};
-    const Span written[] = {floats(score, n)};
-    if (overlap(read, written)) return fail(GS_ERR_INVALID_ARGUMENT, "gs_shares: score overlaps an input");
     const IndexWork w = index_layout(index->work, n, &index->grid, index->capacity);
+    const size_t pairs = sizeof(uint32_t) * (size_t)index->capacity;
+    const bool points = query->kind == GS_QUERY_POINTS || query->kind == GS_QUERY_JITTER;
+    const bool ids = query->kind == GS_QUERY_VOXELS || query->kind == GS_QUERY_JITTER;
+    const Span read[] = {floats(gauss->mean, 3 * n), floats(gauss->scale, 3 * n), floats(gauss->rot, 4 * n),
+                         floats(gauss->value, n), floats(gauss->weight, n), floats(influence, nq), floats(gain, nq),
+                         Span{index->work, w.bytes}, Span{index->keys, pairs}, Span{index->gids, pairs},
+                         Span{index->cell_offsets, sizeof(uint32_t) * (size_t)(gp.ncells + 1)},
+                         Span{grid ? nullptr : plan, p.bytes}, floats(points ? query->points : nullptr, 3 * nq),
+                         Span{ids ? query->voxel_ids : nullptr, sizeof(uint32_t) * (size_t)nq}};
+    const Span written[] = {floats(score, n), Span{work, sw.bytes}};
+    if (overlap(read, written) || overlap_each_other(written))
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_shares: score or the workspace overlaps an input or the other");
     const float T = cutoff_T(index->tau);
     const SharesExact exact{gauss->mean, gauss->scale, gauss->rot, 2.0 * std::log(1.0 / (double)index->tau)};
     const BwdGeom bg = bwd_geom(gp, qp, T, grid || query->kind == GS_QUERY_JITTER);
@@ -1294,8 +1310,9 @@ gs_status gs_evict(const gs_params *in, int64_t n, const float *score, const uin
                          Span{pinned, (size_t)n}};
     const Span written[] = {floats(out->mean, 3 * keep), floats(out->log_scale, 3 * keep), floats(out->rot, 4 * keep),
                             floats(out->value_logit, keep), floats(out->weight_logit, keep),
-                            Span{source, sizeof(int32_t) * (size_t)keep}, floats(score_out, keep)};
-    if (overlap(read, written)) return fail(GS_ERR_INVALID_ARGUMENT, "gs_evict: an output overlaps an input");
+                            Span{source, sizeof(int32_t) * (size_t)keep}, floats(score_out, keep), Span{work, need}};
+    if (overlap(read, written) || overlap_each_other(written))
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_evict: an output or the workspace overlaps an input or another");
     GS_TRY(launch_evict(*in, n, score, pinned, keep, *out, source, score_out, work, stream), "gs_evict");
     return GS_OK;
 }
@@ -1335,8 +1352,9 @@ gs_status gs_draw(int64_t rows, int64_t n, const void *scores, int64_t stride, c
     const size_t size = p.type == GS_SCORE_BF16 ? 2 : 4, total = (size_t)rows * (size_t)draws;
     const Span read[] = {Span{scores, size * (size_t)((rows - 1) * stride + n)}, Span{uniform, sizeof(double) * total},
                          Span{lengths, sizeof(int32_t) * (size_t)rows}};
-    const Span written[] = {Span{ids, sizeof(int32_t) * total}, Span{prob, sizeof(float) * total}};
-    if (overlap(read, written)) return fail(GS_ERR_INVALID_ARGUMENT, "gs_draw: an output overlaps an input");
+    const Span written[] = {Span{ids, sizeof(int32_t) * total}, Span{prob, sizeof(float) * total}, Span{work, need}};
+    if (overlap(read, written) || overlap_each_other(written))
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_draw: an output or the workspace overlaps an input or another");
     GS_TRY(launch_draw(rows, n, scores, stride, lengths, p, draws, uniform, ids, prob, work, stream), "gs_draw");
     return GS_OK;
 }
@@ -1359,9 +1377,10 @@ gs_status gs_split(const gs_params *set, int64_t n, const int32_t *ids, int64_t 
     const Span rows[] = {floats(set->mean, 3 * all), floats(set->log_scale, 3 * all), floats(set->rot, 4 * all),
                          floats(set->value_logit, all), floats(set->weight_logit, all)};
     const Span read[] = {Span{ids, sizeof(int32_t) * (size_t)count}};
-    const Span written[] = {Span{source, sizeof(int32_t) * (size_t)all}, floats(score, all)};
-    if (overlap(rows, read) || overlap(rows, written) || overlap(read, written) || overlap(written[0], written[1]))
-        return fail(GS_ERR_INVALID_ARGUMENT, "gs_split: ids, source, score and the set overlap");
+    const Span written[] = {Span{source, sizeof(int32_t) * (size_t)all}, floats(score, all), Span{work, need}};
+    if (overlap(rows, read) || overlap(rows, written) || overlap(read, written) || overlap_each_other(rows) ||
+        overlap_each_other(written))
+        return fail(GS_ERR_INVALID_ARGUMENT, "gs_split: ids, source, score, the set and the workspace overlap");
     GS_TRY(launch_split(*set, n, ids, count, source, score, (uint32_t *)work, stream), "gs_split");
     return GS_OK;
 }
