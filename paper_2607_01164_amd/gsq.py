@@ -1057,7 +1057,8 @@ def gs_shares(gauss: Gaussians, index: Index, query: Query, plan: Optional[torch
     _row_of(influence, "influence", torch.float32, nq)
     _row_of(gain, "gain", torch.float32, nq)
     _row_of(score, "score", torch.float32, gauss.n)
-    _one_device(gauss.mean.get_device(), influence=influence, gain=gain, score=score, plan=plan, work=work)
+    _one_device(gauss.mean.get_device(), influence=influence, gain=gain, score=score, plan=plan, work=work,
+                index=index.work, voxel_ids=query.voxel_ids, points=query.points)
     _check(load_library().gs_shares(ctypes.byref(g), ctypes.byref(index.c), ctypes.byref(q), _ptr(plan),
                                     0 if plan is None else plan.numel(), influence.data_ptr(), _ptr(gain),
                                     float(decay), score.data_ptr(), work.data_ptr(), _work_bytes(work),
