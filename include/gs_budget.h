@@ -46,7 +46,8 @@ size_t gs_shares_work_bytes(const gs_index *index, const gs_query *query);
  * index was built from, unchanged. decay = 0 overwrites score without reading
  * it (0 <= decay, finite). score and work overlap no input (the Gaussians, the
  * index's arrays, the query's, the plan, influence and gain).
- * The sums are float32, in an order that the inputs alone fix. Pairs whose Q
+ * The sums are float32, those of a Gaussian that very many queries reach joined
+ * in float64, in an order that the inputs alone fix. Pairs whose Q
  * is so near the cutoff that float32 cannot tell are decided in float64 from
  * gauss (the sampler decides them in float32: of a pair that the two take
  * differently, tau w_i / I is missing in the sum or too much).

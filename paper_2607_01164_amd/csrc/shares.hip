@@ -7,10 +7,10 @@
 // pieces of one width and walks them with the Gaussian's record in scalars, so
 // that a query costs its load and the 24 or so instructions of a pair; lanes
 // are added at a Gaussian's end: no atomics, an order fixed by the inputs. The
-// bound is the arithmetic over the pairs of the rows, of which the cutoff
-// keeps a fourth to a third: a 128^3 jittered grid and 131072 Gaussians, 123
-// million pairs, 151 us. (A
-// lane a row, each with its own record: 583 us.)
+// bound is the arithmetic over the pairs of the rows, of which the cutoff keeps
+// half where rows are of voxels and a fourth to a third where they are of the
+// plan's cells: a 128^3 jittered grid and 131072 Gaussians, 54 million pairs, 151
+// us. (A lane a row, each with its own record: 583 us.)
 #include <type_traits>
 
 #include "budget.h"
@@ -49,6 +49,16 @@ constexpr uint32_t kStepsMost = 256, kRowsMost = 1024;
 constexpr uint32_t kTeam = 8;
 constexpr int64_t kTeamQueries = 65536;
 constexpr uint32_t kTeamBlocks = 512, kTeamLists = 64;
+
+// How a wave takes its Gaussians: all of every one (calls of fewer than
+// kTeamQueries queries); but for those that it leaves to teams; or a team's share
+// of one.
+enum { kFormAll = 0, kFormLeave = 1, kFormTeam = 2 };
+// Steps whose terms a team's lane adds up in float32; its sums of them are held
+// in float64, since a Gaussian can have any number of terms, which are alike, and
+// so are their roundings (one over 2 M points was 4 10^-5 off in float32, over 16
+// M 2 10^-4, now 4 10^-7). The other forms have some 1024 terms a lane at most.
+constexpr uint32_t kSettle = 32;
 
 // waves of one launch (a launch has fewer than 2^32 threads)
 constexpr uint64_t kWavesMost = (uint64_t)1 << 25;
@@ -227,10 +237,12 @@ constexpr uint32_t kEntries = kPieces * kWave + kAhead * 16;  // the last steps 
 
 // The sums of a wave's Gaussians, lane i < nk Gaussian i's (mgid). part of
 // parts: of the steps, or of the rows where there are many, this wave takes its
-// share. LEAVE: Gaussians of too many rows or steps are left out, in `left` by bit.
-template <int WALK, bool LEAVE>
+// share. kFormLeave: Gaussians of too many rows or steps are left out, in `left` by
+// bit.
+template <int WALK, int FORM>
 __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32_t nk, uint32_t part, uint32_t parts,
                                       uint32_t &left, uint2 *s_row, float2 *s_yz, uint32_t *s_x) {
+    constexpr bool LEAVE = FORM == kFormLeave, TEAM = FORM == kFormTeam;
     const uint32_t lane = threadIdx.x % kWave;
     const float T = a.T;
     // positions that leave their voxels: the plan's rows, through its order
@@ -275,16 +287,26 @@ __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32
     const bool fdiv = wave_max_uniform(mR) < (1u << 21);
     float mtot = 0.0f;  // lane i < nk: Gaussian i's sum
     float acc = 0.0f;   // of the Gaussian being walked
+    double held = 0.0;  // and a team's after every kSettle steps
+    auto settle = [&]() {
+        held += (double)acc;
+        acc = 0.0f;
+    };
+    // where a loop of steps from `at` to `end`, `apart` from each other, settles
+    auto stop_of = [&](uint32_t at, uint32_t end, uint32_t apart) {
+        return !TEAM || end - at <= kSettle * apart ? end : at + kSettle * apart;
+    };
     uint32_t cur = ~0u, cgid = 0;
     uint32_t steps = 0;  // of it, so far
     Record c = {};
     float margin = 0.0f;
     auto finish = [&]() {
-        float t = row16_sum(acc);
+        float t = row16_sum(TEAM ? (float)(held + (double)acc) : acc);
         t += swz_xor16(t);
         t += perm_xor32(t, lane);
         if (lane == cur) mtot = t;
         acc = 0.0f;
+        held = 0.0;
     };
     // the parts share the batches of 64 rows; where those are fewer, several
     // parts share a batch's steps
@@ -414,22 +436,28 @@ __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32
             };
             if (!whole) {
                 const uint32_t rows = (uint32_t)kWave >> shift;  // of a step
-                for (uint32_t r0 = ra + sub * kAhead * rows; r0 < rz; r0 += subs * kAhead * rows) {
-                    uint32_t k[kAhead];
-                    bool on[kAhead];
-                    Voxel v[kAhead] = {};
+                const uint32_t apart = subs * kAhead * rows;
+                for (uint32_t r0 = ra + sub * kAhead * rows; r0 < rz;) {
+                    const uint32_t stop = stop_of(r0, rz, apart);
+                    for (; r0 < stop; r0 += apart) {
+                        uint32_t k[kAhead];
+                        bool on[kAhead];
+                        Voxel v[kAhead] = {};
 #pragma unroll
-                    for (uint32_t u = 0; u < kAhead; ++u) {
-                        const uint32_t row = r0 + u * rows + own;
-                        const uint2 w = s_row[row];
-                        on[u] = row < rz && mine < w.y;
-                        k[u] = w.x + mine;
-                        if (WALK == kWalkGrid) {
-                            const float2 yz = s_yz[row];
-                            v[u] = Voxel{s_x[row] + mine, yz.x, yz.y};
+                        for (uint32_t u = 0; u < kAhead; ++u) {
+                            const uint32_t row = r0 + u * rows + own;
+                            const uint2 w = s_row[row];
+                            on[u] = row < rz && mine < w.y;
+                            k[u] = w.x + mine;
+                            if (WALK == kWalkGrid) {
+                                const float2 yz = s_yz[row];
+                                v[u] = Voxel{s_x[row] + mine, yz.x, yz.y};
+                            }
                         }
+                        add(k, on, v);
                     }
-                    add(k, on, v);
+                    if (!TEAM) break;
+                    settle();
                 }
             } else {
                 for (uint32_t row = ra; row < rz; ++row) {
@@ -440,18 +468,24 @@ __device__ __forceinline__ float walk(const SharesArgs &a, uint32_t mgid, uint32
                         x0 = s_x[row];
                         yz = s_yz[row];
                     }
-                    for (uint32_t e0 = sub * kAhead * kWave; e0 < w.y; e0 += subs * kAhead * kWave) {
-                        uint32_t k[kAhead];
-                        bool on[kAhead];
-                        Voxel v[kAhead];
+                    const uint32_t apart = subs * kAhead * kWave;
+                    for (uint32_t e0 = sub * kAhead * kWave; e0 < w.y;) {
+                        const uint32_t stop = stop_of(e0, w.y, apart);
+                        for (; e0 < stop; e0 += apart) {
+                            uint32_t k[kAhead];
+                            bool on[kAhead];
+                            Voxel v[kAhead];
 #pragma unroll
-                        for (uint32_t u = 0; u < kAhead; ++u) {
-                            const uint32_t e = e0 + u * kWave + lane;
-                            on[u] = e < w.y;
-                            k[u] = w.x + e;
-                            v[u] = Voxel{x0 + e, yz.x, yz.y};
+                            for (uint32_t u = 0; u < kAhead; ++u) {
+                                const uint32_t e = e0 + u * kWave + lane;
+                                on[u] = e < w.y;
+                                k[u] = w.x + e;
+                                v[u] = Voxel{x0 + e, yz.x, yz.y};
+                            }
+                            add(k, on, v);
                         }
-                        add(k, on, v);
+                        if (!TEAM) break;
+                        settle();
                     }
                 }
             }
@@ -470,7 +504,7 @@ __device__ __forceinline__ void add_score(const SharesArgs &a, uint32_t gid, flo
 // filled by other waves (6, then 7 or 8 of them: a jittered 128^3 grid 167 -> 156
 // us, 2 M points 172 -> 155; grids lose by it, 120 -> 124 us).
 constexpr int waves_of(int walk) { return walk == kWalkPlan ? 8 : walk == kWalkVoxels ? 7 : 6; }
-template <int WALK, bool LEAVE>
+template <int WALK, int FORM>
 __global__ __launch_bounds__(kWave, waves_of(WALK)) void k_shares(SharesArgs a) {
     __shared__ uint2 s_row[kEntries];   // first query, queries
     __shared__ float2 s_yz[WALK == kWalkGrid ? kEntries : 1];   // grids: y and z, first voxel in x
@@ -481,9 +515,9 @@ __global__ __launch_bounds__(kWave, waves_of(WALK)) void k_shares(SharesArgs a) 
     const uint32_t nk = (uint64_t)a.n_gauss - first < a.pack ? (uint32_t)((uint64_t)a.n_gauss - first) : a.pack;
     const uint32_t gid = lane < nk ? a.gorder[first + lane] : 0u;
     uint32_t left;
-    const float sum = walk<WALK, LEAVE>(a, gid, nk, 0, 1, left, s_row, s_yz, s_x);
+    const float sum = walk<WALK, FORM>(a, gid, nk, 0, 1, left, s_row, s_yz, s_x);
     if (lane >= nk) return;
-    if (LEAVE && (left >> lane & 1u)) {
+    if (FORM == kFormLeave && (left >> lane & 1u)) {
         const uint32_t list = (uint32_t)((a.wave0 + blockIdx.x) % kTeamLists);
         a.teams[kTeamLists + (size_t)list * a.team_room + atomicAdd(&a.teams[list], 1u)] = gid;
     } else
@@ -502,7 +536,7 @@ __global__ __launch_bounds__(kTeam * kWave) void k_shares_team(SharesArgs a) {
     for (uint32_t i = blockIdx.x / kTeamLists; i < count; i += gridDim.x / kTeamLists) {
         const uint32_t gid = a.teams[kTeamLists + (size_t)list * a.team_room + i];
         uint32_t left;
-        const float sum = walk<WALK, false>(a, gid, 1, wave, kTeam, left, s_row[wave],
+        const float sum = walk<WALK, kFormTeam>(a, gid, 1, wave, kTeam, left, s_row[wave],
                                             s_yz[WALK == kWalkGrid ? wave : 0], s_x[WALK == kWalkGrid ? wave : 0]);
         if (lane == 0) s_sum[wave] = sum;
         __syncthreads();
@@ -590,21 +624,21 @@ hipError_t launch_shares(const QueryParams &q, const GridParams &g, const BwdGeo
     for (a.wave0 = 0; a.wave0 < waves; a.wave0 += kWavesMost) {
         const uint64_t left = waves - a.wave0;
         const dim3 wb((uint32_t)(left < kWavesMost ? left : kWavesMost));
-        auto launch = [&](auto walk, auto leave) {
-            hipLaunchKernelGGL((k_shares<decltype(walk)::value, decltype(leave)::value>), wb, dim3(kWave), 0, s, a);
+        auto launch = [&](auto walk, auto form) {
+            hipLaunchKernelGGL((k_shares<decltype(walk)::value, decltype(form)::value>), wb, dim3(kWave), 0, s, a);
         };
-        auto each = [&](auto leave) {
+        auto each = [&](auto form) {
             if (kind == kWalkGrid)
-                launch(std::integral_constant<int, kWalkGrid>(), leave);
+                launch(std::integral_constant<int, kWalkGrid>(), form);
             else if (kind == kWalkVoxels)
-                launch(std::integral_constant<int, kWalkVoxels>(), leave);
+                launch(std::integral_constant<int, kWalkVoxels>(), form);
             else
-                launch(std::integral_constant<int, kWalkPlan>(), leave);
+                launch(std::integral_constant<int, kWalkPlan>(), form);
         };
         if (a.teams)
-            each(std::true_type());
+            each(std::integral_constant<int, kFormLeave>());
         else
-            each(std::false_type());
+            each(std::integral_constant<int, kFormAll>());
     }
     prof_end("shares", s);
     if (a.teams) {
