@@ -119,6 +119,8 @@ size_t gs_draw_work_bytes(int64_t rows, int64_t n, int64_t draws);
  * order draw ids in rising order, which reads memory line by line, here and
  * where gs_split copies what was drawn (419430 of 2 M Gaussians: 65 -> 55 us
  * and 78 -> 37).
+ * A row of up to 16384 candidates, or one of which top_k leaves up to 1024, is
+ * drawn by one workgroup: many draws from it take 1 to 4 ns each.
  * 0 <= rows, n < 2^31, 0 <= draws < 2^31, rows n and rows draws below 2^40.
  */
 gs_status gs_draw(int64_t rows, int64_t n, const void *scores, int64_t stride, const int32_t *lengths,
