@@ -256,7 +256,7 @@ __device__ __forceinline__ float bperm_f(uint32_t src, float v) {
 // test is all a non-contributing pair costs; contributing pairs go to a
 // per-wave LDS queue, and every 64 queued pairs are processed with all
 // lanes busy.
-template <uint32_t PACK>
+template <uint32_t PACK, bool WIDE>
 __global__ __launch_bounds__(kBwdBlock) void k_backward_gauss(GridParams g, BwdGeom bg,
                                                            const Record *__restrict__ rec,
                                                            const CellBox *__restrict__ box,
@@ -337,7 +337,7 @@ __global__ __launch_bounds__(kBwdBlock) void k_backward_gauss(GridParams g, BwdG
         if (gr < Rw) {
             uint32_t yy, zz;
             row_yz(gr - (f_end - f_R), f_ny, fdiv, yy, zz);  // row within its Gaussian
-            len = plan_row(fr, f_lx, f_nx, f_ly + yy, f_lz + zz, g, bg, point_off, start);
+            len = plan_row<WIDE>(fr, f_lx, f_nx, f_ly + yy, f_lz + zz, g, bg, point_off, start);
         }
         const uint32_t nrows = (Rw - rb) < (uint32_t)kWave ? (Rw - rb) : (uint32_t)kWave;
         const uint32_t incl = wave_incl_sum(len);   // end of row l in the batch's concatenation
@@ -837,12 +837,15 @@ hipError_t launch_backward(const QueryParams &q, const GridParams &g, const BwdG
         else if (grid)
             hipLaunchKernelGGL(k_backward_grid<kPack>, wb, tb, 0, s, q, g, bg, rec, box, gorder, n_gauss, b.ab, T,
                                b.moments);
+        else if (bg.K > 1u << 24)  // quarters of a row that float32 does not hold
+            hipLaunchKernelGGL((k_backward_gauss<1, true>), dim3((uint32_t)((n_gauss + kBwdWaves - 1) / kBwdWaves)), tb,
+                               0, s, g, bg, rec, box, gorder, n_gauss, point_off, plan_pos, b.ab, T, b.moments);
         else if (pack == 1)
-            hipLaunchKernelGGL(k_backward_gauss<1>, wb, tb, 0, s, g, bg, rec, box, gorder, n_gauss, point_off,
+            hipLaunchKernelGGL((k_backward_gauss<1, false>), wb, tb, 0, s, g, bg, rec, box, gorder, n_gauss, point_off,
                                plan_pos, b.ab, T, b.moments);
         else
-            hipLaunchKernelGGL(k_backward_gauss<kPack>, wb, tb, 0, s, g, bg, rec, box, gorder, n_gauss, point_off,
-                               plan_pos, b.ab, T, b.moments);
+            hipLaunchKernelGGL((k_backward_gauss<kPack, false>), wb, tb, 0, s, g, bg, rec, box, gorder, n_gauss,
+                               point_off, plan_pos, b.ab, T, b.moments);
         prof_end("bwd_gauss", s);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     } else {
